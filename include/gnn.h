@@ -456,6 +456,95 @@ gnn_status_t gnn_softmax_xent(int32_t n, int32_t c, const float *Z, const int32_
 gnn_status_t gnn_sum_squared_error(int64_t count, const float *Z, const float *T, float *dZ, float *loss_out,
                                    void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ---- between the layers: dropout, layer norm, residual connections, gated feed-forward blocks ---- */
+
+/*
+ * gnn_dropout_t - which elements of an [n, f] array are dropped: a HOST struct that names the generator.
+ *   p      probability of an element to be dropped, 0 <= p < 1; the others are multiplied by 1 / (1 - p)
+ *   site   which dropout of a network this is: calls with different sites drop independently
+ *   state  DEVICE pointer to {seed, step}, 8-byte aligned; may be NULL where p is 0.  Read by the kernels, so that a captured
+ *          graph draws anew on every replay once the step is advanced (gnn_rng_advance, on the stream, after the backward pass).
+ * Element (i, c) is dropped where word c % 4 of the Philox4x32-10 block (Salmon, Moraes, Dror, Shaw, "Parallel random
+ * numbers: as easy as 1, 2, 3", SC 2011) with key = seed and counter = (c / 4, i, site, low 32 bits of step) is below
+ * round(p 2^32).  The mask depends on nothing else and is never stored: backward forms it again from the same struct, and every
+ * operator below that is given the same struct and shape drops the same elements.  What is dropped becomes 0, infinities and NaN too.
+ */
+typedef struct {
+    float p;
+    uint32_t site;
+    const uint64_t *state;
+} gnn_dropout_t;
+
+/* step += by, in device memory. */
+gnn_status_t gnn_rng_advance(uint64_t *state, uint64_t by, void *hip_stream);
+
+/*
+ * gnn_dropout - Y = R + dropout(X), all [n, f]; R NULL: Y = dropout(X).  drop NULL (or p = 0): nothing is dropped.
+ *   The gradient with respect to X is the same call on dY without R, that with respect to R is dY.
+ *   Y may be X or R.  Errors: INVALID_ARG (NULL X / Y, negative n, f < 1, p outside [0, 1), state NULL or misaligned).
+ */
+gnn_status_t gnn_dropout(int32_t n, int32_t f, const float *X, const float *R, const gnn_dropout_t *drop, float *Y,
+                         void *hip_stream);
+
+typedef enum { GNN_ACT_NONE = 0, GNN_ACT_RELU = 1, GNN_ACT_ELU = 2 } gnn_act_t;
+
+/*
+ * gnn_layer_norm_fwd - Y = dropout(act(gamma xhat + beta)), xhat = (x - mean) rstd over the f columns of a row,
+ *   rstd = 1 / sqrt(variance + eps) with the variance divided by f.  X, Y [n, f]; gamma, beta [f] or NULL (1 and 0);
+ *   ELU with alpha = 1; drop NULL: no dropout; stat_out [n][2] = (mean, rstd), which backward reads.  Y may be X (where no
+ *   backward pass follows: that needs X).
+ * gnn_layer_norm_bwd - from X, stat and dY [n, f] the gradients dX [n, f], dgamma and dbeta [f]; any of them may be NULL.  The
+ *   activation's derivative is taken from gamma xhat + beta, formed again as in forward (ReLU' = 0 at 0), the mask of dropout
+ *   likewise: act, drop, gamma and beta as in forward.  dX may be dY.  The sums over the rows have a fixed order.
+ *   workspace: gnn_layer_norm_workspace_bytes(n, f), which does not fall as n grows; not used where dgamma and dbeta are NULL
+ *   (then it may be NULL).
+ * Errors: INVALID_ARG (NULL X / Y / stat / dY, negative n, f < 1, eps not positive and finite, act no gnn_act_t, drop as in
+ *   gnn_dropout, workspace NULL or not 256-byte aligned), BUFFER_TOO_SMALL.
+ */
+gnn_status_t gnn_layer_norm_fwd(int32_t n, int32_t f, const float *X, const float *gamma, const float *beta, float eps,
+                                gnn_act_t act, const gnn_dropout_t *drop, float *Y, float *stat_out, void *hip_stream);
+gnn_status_t gnn_layer_norm_bwd(int32_t n, int32_t f, const float *X, const float *stat, const float *gamma,
+                                const float *beta, gnn_act_t act, const gnn_dropout_t *drop, const float *dY, float *dX,
+                                float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t gnn_layer_norm_workspace_bytes(int32_t n, int32_t f);
+
+/*
+ * gnn_add_layer_norm_fwd - the end of one residual block and the norm that begins the next:
+ *   H = R + dropout(X), Y = gamma xhat(H) + beta.  X, R, H, Y [n, f]; H may be X or R; stat_out as above, of H.
+ * gnn_add_layer_norm_bwd - dR = dH + (gradient of the norm at H, from dY), dX = dropout(dR); dH [n, f] is what flows back
+ *   into H from elsewhere, NULL: nothing.  dX NULL: not written (without dropout it is dR).  dR and dX may each be dY or dH, but
+ *   not the same array.  dgamma and dbeta may be NULL.  workspace: gnn_layer_norm_workspace_bytes(n, f).
+ * Errors: as gnn_layer_norm_fwd / _bwd; NULL R, H, dR are INVALID_ARG as well.
+ */
+gnn_status_t gnn_add_layer_norm_fwd(int32_t n, int32_t f, const float *X, const float *R, const gnn_dropout_t *drop,
+                                    const float *gamma, const float *beta, float eps, float *H, float *Y, float *stat_out,
+                                    void *hip_stream);
+gnn_status_t gnn_add_layer_norm_bwd(int32_t n, int32_t f, const float *H, const float *stat, const float *gamma,
+                                    const gnn_dropout_t *drop, const float *dY, const float *dH, float *dR, float *dX,
+                                    float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The activation of a gate: 1 / (1 + exp(-a)), a / (1 + exp(-a)), a Phi(a) with Phi the normal distribution (by erf). */
+typedef enum { GNN_GATE_SIGMOID = 0, GNN_GATE_SILU = 1, GNN_GATE_GELU = 2 } gnn_gate_t;
+
+/*
+ * gnn_gated_fwd - the two projections of a gated feed-forward block, the activation and the product:
+ *   [A | U] = X W + 1 b^T,  H = act(A) .* U.   X [n, f_in], W [f_in, 2 f_out] = [W_gate | W_up], b [2 f_out] or NULL, H [n, f_out].
+ *   (The projection back is gnn_gemm, or the product of the next layer.)
+ *   Z [n, 2 f_out] or NULL: receives [A | U], which backward may read instead of forming it again.
+ * gnn_gated_bwd - with D = [dH .* U .* act'(A) | dH .* act(A)]:  dW = X^T D [f_in, 2 f_out], db = D^T 1 [2 f_out] (NULL: not
+ *   wanted), dX = D W^T [n, f_in] (NULL: not wanted).  Z as forward left it, or NULL: [A | U] is formed again from X, W and b.
+ *   dX must not overlap X or dH.
+ *   workspace: gnn_gated_workspace_bytes(backward, n, f_in, f_out), backward 0 or 1; what it returns does not fall as n grows.
+ * Errors: INVALID_ARG (NULL X / W / H / dH / dW, negative n, f_in < 1 or f_out < 1, gate no gnn_gate_t, workspace NULL or not
+ *   256-byte aligned), BUFFER_TOO_SMALL, UNSUPPORTED (2 f_out or the number of tiles beyond 2^31).
+ */
+gnn_status_t gnn_gated_fwd(gnn_gate_t gate, int32_t n, int32_t f_in, int32_t f_out, const float *X, const float *W,
+                           const float *b, float *H, float *Z, void *workspace, size_t workspace_bytes, void *hip_stream);
+gnn_status_t gnn_gated_bwd(gnn_gate_t gate, int32_t n, int32_t f_in, int32_t f_out, const float *X, const float *W,
+                           const float *b, const float *Z, const float *dH, float *dW, float *db, float *dX,
+                           void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t gnn_gated_workspace_bytes(int32_t backward, int32_t n, int32_t f_in, int32_t f_out);
+
 const char *gnn_status_string(gnn_status_t status);
 
 #ifdef __cplusplus

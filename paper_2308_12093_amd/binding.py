@@ -34,6 +34,8 @@ GNN_BWD_AUTO, GNN_BWD_FUSED_PROPAGATE, GNN_BWD_SPLIT_PROPAGATE = 0, 1, 2
  GNN_CACHE_GAT_FEAT_EDGE) = range(6)
 GNN_SELECT_PAPER_RULE, GNN_SELECT_CALIBRATED = 0, 1
 GNN_AGG_GCN_SYM, GNN_AGG_MEAN, GNN_AGG_GIN_SUM = 0, 1, 2
+GNN_ACT_NONE, GNN_ACT_RELU, GNN_ACT_ELU = 0, 1, 2
+GNN_GATE_SIGMOID, GNN_GATE_SILU, GNN_GATE_GELU = 0, 1, 2
 
 _vp = ctypes.c_void_p
 _i32 = ctypes.c_int32
@@ -60,6 +62,10 @@ class gnn_plan_info_t(ctypes.Structure):
                 ("cache_bytes", _sz), ("workspace_bytes", _sz),
                 ("transient_fwd", _i64), ("transient_bwd", _i64),
                 ("spmm_width_fwd", _i64), ("spmm_width_bwd", _i64)]
+
+
+class gnn_dropout_t(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("site", ctypes.c_uint32), ("state", _vp)]
 
 
 _BUFS = [_vp, _sz, _vp, _sz, _vp]
@@ -103,6 +109,19 @@ _PROTOS = {
     "gnn_gemm_workspace_bytes": (_sz, [_i32, _i32, _i64, _i64, _i64]),
     "gnn_softmax_xent": (ctypes.c_int, [_i32, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "gnn_sum_squared_error": (ctypes.c_int, [_i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gnn_rng_advance": (ctypes.c_int, [_vp, ctypes.c_uint64, _vp]),
+    "gnn_dropout": (ctypes.c_int, [_i32, _i32, _vp, _vp, ctypes.POINTER(gnn_dropout_t), _vp, _vp]),
+    "gnn_layer_norm_fwd": (ctypes.c_int, [_i32, _i32, _vp, _vp, _vp, ctypes.c_float, ctypes.c_int,
+                                          ctypes.POINTER(gnn_dropout_t), _vp, _vp, _vp]),
+    "gnn_layer_norm_bwd": (ctypes.c_int, [_i32, _i32, _vp, _vp, _vp, _vp, ctypes.c_int, ctypes.POINTER(gnn_dropout_t)] +
+                           [_vp] * 5 + [_sz, _vp]),
+    "gnn_layer_norm_workspace_bytes": (_sz, [_i32, _i32]),
+    "gnn_add_layer_norm_fwd": (ctypes.c_int, [_i32, _i32, _vp, _vp, ctypes.POINTER(gnn_dropout_t), _vp, _vp, ctypes.c_float] +
+                               [_vp] * 4),
+    "gnn_add_layer_norm_bwd": (ctypes.c_int, [_i32, _i32, _vp, _vp, _vp, ctypes.POINTER(gnn_dropout_t)] + [_vp] * 7 + [_sz, _vp]),
+    "gnn_gated_fwd": (ctypes.c_int, [ctypes.c_int, _i32, _i32, _i32] + [_vp] * 6 + [_sz, _vp]),
+    "gnn_gated_bwd": (ctypes.c_int, [ctypes.c_int, _i32, _i32, _i32] + [_vp] * 9 + [_sz, _vp]),
+    "gnn_gated_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32]),
 }
 EXPORTS = tuple(_PROTOS)
 for _name, (_res, _args) in _PROTOS.items():
@@ -364,3 +383,64 @@ def gnn_sum_squared_error(count, Z, T, dZ, loss_out, workspace):
 def gnn_softmax_xent(n, c, Z, labels, dZ, loss_out, workspace):
     _check(lib.gnn_softmax_xent(n, c, _ptr(Z), _ptr(labels), _ptr(dZ), _ptr(loss_out), _ptr(workspace),
                                 _nbytes(workspace), _stream()), "gnn_softmax_xent")
+
+
+# ---- between the layers --------------------------------------------------------------
+class Dropout:
+    """A ``gnn_dropout_t`` and the device tensor it points to: ``state`` int64 [2], {seed, step}."""
+
+    def __init__(self, p, state=None, site=0):
+        self.state = state
+        self.c = gnn_dropout_t(p, site, _ptr(state))
+
+
+def _drop(drop):
+    return None if drop is None else ctypes.byref(drop.c)
+
+
+def gnn_rng_advance(state, by=1):
+    _check(lib.gnn_rng_advance(_ptr(state), by, _stream()), "gnn_rng_advance")
+
+
+def gnn_dropout(n, f, X, R, drop, Y):
+    _check(lib.gnn_dropout(n, f, _ptr(X), _ptr(R), _drop(drop), _ptr(Y), _stream()), "gnn_dropout")
+
+
+def gnn_layer_norm_workspace_bytes(n, f):
+    return lib.gnn_layer_norm_workspace_bytes(n, f)
+
+
+def gnn_layer_norm_fwd(n, f, X, gamma, beta, eps, act, drop, Y, stat_out):
+    _check(lib.gnn_layer_norm_fwd(n, f, _ptr(X), _ptr(gamma), _ptr(beta), float(eps), int(act), _drop(drop), _ptr(Y),
+                                  _ptr(stat_out), _stream()), "gnn_layer_norm_fwd")
+
+
+def gnn_layer_norm_bwd(n, f, X, stat, gamma, beta, act, drop, dY, dX, dgamma, dbeta, workspace):
+    _check(lib.gnn_layer_norm_bwd(n, f, _ptr(X), _ptr(stat), _ptr(gamma), _ptr(beta), int(act), _drop(drop), _ptr(dY),
+                                  _ptr(dX), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), _nbytes(workspace), _stream()),
+           "gnn_layer_norm_bwd")
+
+
+def gnn_add_layer_norm_fwd(n, f, X, R, drop, gamma, beta, eps, H, Y, stat_out):
+    _check(lib.gnn_add_layer_norm_fwd(n, f, _ptr(X), _ptr(R), _drop(drop), _ptr(gamma), _ptr(beta), float(eps), _ptr(H),
+                                      _ptr(Y), _ptr(stat_out), _stream()), "gnn_add_layer_norm_fwd")
+
+
+def gnn_add_layer_norm_bwd(n, f, H, stat, gamma, drop, dY, dH, dR, dX, dgamma, dbeta, workspace):
+    _check(lib.gnn_add_layer_norm_bwd(n, f, _ptr(H), _ptr(stat), _ptr(gamma), _drop(drop), _ptr(dY), _ptr(dH), _ptr(dR),
+                                      _ptr(dX), _ptr(dgamma), _ptr(dbeta), _ptr(workspace), _nbytes(workspace), _stream()),
+           "gnn_add_layer_norm_bwd")
+
+
+def gnn_gated_workspace_bytes(backward, n, f_in, f_out):
+    return lib.gnn_gated_workspace_bytes(int(backward), n, f_in, f_out)
+
+
+def gnn_gated_fwd(gate, n, f_in, f_out, X, W, b, H, Z, workspace):
+    _check(lib.gnn_gated_fwd(int(gate), n, f_in, f_out, _ptr(X), _ptr(W), _ptr(b), _ptr(H), _ptr(Z), _ptr(workspace),
+                             _nbytes(workspace), _stream()), "gnn_gated_fwd")
+
+
+def gnn_gated_bwd(gate, n, f_in, f_out, X, W, b, Z, dH, dW, db, dX, workspace):
+    _check(lib.gnn_gated_bwd(int(gate), n, f_in, f_out, _ptr(X), _ptr(W), _ptr(b), _ptr(Z), _ptr(dH), _ptr(dW), _ptr(db),
+                             _ptr(dX), _ptr(workspace), _nbytes(workspace), _stream()), "gnn_gated_bwd")

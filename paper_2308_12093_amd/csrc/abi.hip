@@ -1,5 +1,8 @@
 // extern "C" entry points: argument checks, then the internal launchers.
 // Every check runs before the first launch, so a failing call has no side effect.
+#include <math.h>
+
+#include "dropout.h"
 #include "plan.h"
 
 using namespace gnn;
@@ -31,6 +34,35 @@ gnn_status_t check_graph(const gnn_plan_t *plan, const gnn_graph_t *g, bool need
         if (g->nnz > 0 && need_perm && !g->csc_perm) return GNN_ERR_BAD_GRAPH;
     }
     return GNN_OK;
+}
+
+// a caller's dropout as the kernels take it; NULL and p = 0 drop nothing
+gnn_status_t take_dropout(const gnn_dropout_t *d, Dropout *out) {
+    *out = Dropout{nullptr, 0, 0, 1.f};
+    if (!d) return GNN_OK;
+    if (!(d->p >= 0.f && d->p < 1.f)) return GNN_ERR_INVALID_ARG;
+    if (d->p == 0.f) return GNN_OK;
+    if (!d->state || reinterpret_cast<uintptr_t>(d->state) % sizeof(uint64_t)) return GNN_ERR_INVALID_ARG;
+    *out = Dropout{d->state, d->site, (uint32_t)llrint((double)d->p * 4294967296.0), (float)(1.0 / (1.0 - (double)d->p))};
+    return GNN_OK;
+}
+
+gnn_status_t check_norm_sums(int32_t n, int32_t f, const float *dgamma, const float *dbeta, const void *workspace,
+                             size_t workspace_bytes) {
+    if (!dgamma && !dbeta) return GNN_OK;
+    if (!workspace || bad_align(workspace)) return GNN_ERR_INVALID_ARG;
+    return workspace_bytes < norm_workspace_bytes(n, f) ? GNN_ERR_BUFFER_TOO_SMALL : GNN_OK;
+}
+
+bool bad_gated(int gate, int32_t n, int32_t f_in, int32_t f_out) {
+    return (gate != GNN_GATE_SIGMOID && gate != GNN_GATE_SILU && gate != GNN_GATE_GELU) || n < 0 || f_in <= 0 || f_out <= 0;
+}
+
+gnn_status_t check_gated_workspace(bool backward, int32_t n, int32_t f_in, int32_t f_out, const void *workspace,
+                                   size_t workspace_bytes) {
+    if (f_out > INT32_MAX / 4) return GNN_ERR_UNSUPPORTED;
+    if (!workspace || bad_align(workspace)) return GNN_ERR_INVALID_ARG;
+    return workspace_bytes < gated_workspace_bytes(backward, n, f_in, f_out) ? GNN_ERR_BUFFER_TOO_SMALL : GNN_OK;
 }
 
 }  // namespace
@@ -386,6 +418,94 @@ gnn_status_t gnn_sum_squared_error(int64_t count, const float *Z, const float *T
     if (count > 0 && (!Z || !T || !dZ)) return GNN_ERR_INVALID_ARG;
     if (workspace_bytes < 4096) return GNN_ERR_BUFFER_TOO_SMALL;
     return squared_error_launch(count, Z, T, dZ, loss_out, workspace, as_stream(hip_stream));
+}
+
+// ---- between the layers ---------------------------------------------------------------
+
+gnn_status_t gnn_rng_advance(uint64_t *state, uint64_t by, void *hip_stream) {
+    if (!state || reinterpret_cast<uintptr_t>(state) % sizeof(uint64_t)) return GNN_ERR_INVALID_ARG;
+    return rng_advance_launch(state, by, as_stream(hip_stream));
+}
+
+gnn_status_t gnn_dropout(int32_t n, int32_t f, const float *X, const float *R, const gnn_dropout_t *drop, float *Y,
+                         void *hip_stream) {
+    Dropout d;
+    if (n < 0 || f <= 0) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_dropout(drop, &d));
+    if (n == 0) return GNN_OK;
+    if (!X || !Y) return GNN_ERR_INVALID_ARG;
+    return dropout_launch(n, f, X, R, d, Y, as_stream(hip_stream));
+}
+
+size_t gnn_layer_norm_workspace_bytes(int32_t n, int32_t f) { return norm_workspace_bytes(n > 0 ? n : 0, f > 0 ? f : 1); }
+
+gnn_status_t gnn_layer_norm_fwd(int32_t n, int32_t f, const float *X, const float *gamma, const float *beta, float eps,
+                                gnn_act_t act, const gnn_dropout_t *drop, float *Y, float *stat_out, void *hip_stream) {
+    Dropout d;
+    if (n < 0 || f <= 0 || !(eps > 0.f && eps < INFINITY)) return GNN_ERR_INVALID_ARG;
+    if (act != GNN_ACT_NONE && act != GNN_ACT_RELU && act != GNN_ACT_ELU) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_dropout(drop, &d));
+    if (n == 0) return GNN_OK;
+    if (!X || !Y || !stat_out) return GNN_ERR_INVALID_ARG;
+    return norm_forward_launch(n, f, X, nullptr, gamma, beta, eps, act, d, nullptr, Y, stat_out, as_stream(hip_stream));
+}
+
+gnn_status_t gnn_layer_norm_bwd(int32_t n, int32_t f, const float *X, const float *stat, const float *gamma,
+                                const float *beta, gnn_act_t act, const gnn_dropout_t *drop, const float *dY, float *dX,
+                                float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    Dropout d;
+    if (n < 0 || f <= 0) return GNN_ERR_INVALID_ARG;
+    if (act != GNN_ACT_NONE && act != GNN_ACT_RELU && act != GNN_ACT_ELU) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_dropout(drop, &d));
+    if (n > 0 && (!X || !stat || !dY)) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(check_norm_sums(n, f, dgamma, dbeta, workspace, workspace_bytes));
+    return norm_backward_launch(n, f, X, stat, gamma, beta, act, d, false, dY, nullptr, nullptr, dX, dgamma, dbeta, workspace,
+                                as_stream(hip_stream));
+}
+
+gnn_status_t gnn_add_layer_norm_fwd(int32_t n, int32_t f, const float *X, const float *R, const gnn_dropout_t *drop,
+                                    const float *gamma, const float *beta, float eps, float *H, float *Y, float *stat_out,
+                                    void *hip_stream) {
+    Dropout d;
+    if (n < 0 || f <= 0 || !(eps > 0.f && eps < INFINITY)) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_dropout(drop, &d));
+    if (n == 0) return GNN_OK;
+    if (!X || !R || !H || !Y || !stat_out || H == Y) return GNN_ERR_INVALID_ARG;
+    return norm_forward_launch(n, f, X, R, gamma, beta, eps, kActNone, d, H, Y, stat_out, as_stream(hip_stream));
+}
+
+gnn_status_t gnn_add_layer_norm_bwd(int32_t n, int32_t f, const float *H, const float *stat, const float *gamma,
+                                    const gnn_dropout_t *drop, const float *dY, const float *dH, float *dR, float *dX,
+                                    float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    Dropout d;
+    if (n < 0 || f <= 0) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_dropout(drop, &d));
+    if (n > 0 && (!H || !stat || !dY || !dR || dX == dR)) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(check_norm_sums(n, f, dgamma, dbeta, workspace, workspace_bytes));
+    return norm_backward_launch(n, f, H, stat, gamma, nullptr, kActNone, d, true, dY, dH, dR, dX, dgamma, dbeta, workspace,
+                                as_stream(hip_stream));
+}
+
+size_t gnn_gated_workspace_bytes(int32_t backward, int32_t n, int32_t f_in, int32_t f_out) {
+    return gated_workspace_bytes(backward != 0, n > 0 ? n : 1, f_in > 0 ? f_in : 1, f_out > 0 ? f_out : 1);
+}
+
+gnn_status_t gnn_gated_fwd(gnn_gate_t gate, int32_t n, int32_t f_in, int32_t f_out, const float *X, const float *W,
+                           const float *b, float *H, float *Z, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (bad_gated(gate, n, f_in, f_out)) return GNN_ERR_INVALID_ARG;
+    if (n == 0) return GNN_OK;
+    if (!X || !W || !H) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(check_gated_workspace(false, n, f_in, f_out, workspace, workspace_bytes));
+    return gated_forward_launch(gate, n, f_in, f_out, X, W, b, H, Z, workspace, as_stream(hip_stream));
+}
+
+gnn_status_t gnn_gated_bwd(gnn_gate_t gate, int32_t n, int32_t f_in, int32_t f_out, const float *X, const float *W,
+                           const float *b, const float *Z, const float *dH, float *dW, float *db, float *dX,
+                           void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (bad_gated(gate, n, f_in, f_out) || !dW) return GNN_ERR_INVALID_ARG;
+    if (n > 0 && (!X || !W || !dH)) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(check_gated_workspace(true, n, f_in, f_out, workspace, workspace_bytes));
+    return gated_backward_launch(gate, n, f_in, f_out, X, W, b, Z, dH, dW, db, dX, workspace, as_stream(hip_stream));
 }
 
 }  // extern "C"

@@ -148,6 +148,25 @@ gnn_status_t squared_error_launch(int64_t count, const float *Z, const float *T,
 gnn_status_t softmax_xent_launch(int n, int c, const float *Z, const int32_t *labels, float *dZ, float *loss,
                                  void *workspace, hipStream_t st);
 
+// ---- between the layers (norm.hip, gated.hip) ----------------------------------------
+struct Dropout;                        // dropout.h
+gnn_status_t rng_advance_launch(uint64_t *state, uint64_t by, hipStream_t st);
+gnn_status_t dropout_launch(int n, int f, const float *X, const float *R, const Dropout &drop, float *Y, hipStream_t st);
+// without R: Y = dropout(act(norm(X))), H is not written; with R: H = R + dropout(X), Y = norm(H), act has to be kActNone
+gnn_status_t norm_forward_launch(int n, int f, const float *X, const float *R, const float *gamma, const float *beta,
+                                 float eps, int act, const Dropout &drop, float *H, float *Y, float *stat, hipStream_t st);
+// workspace: norm_workspace_bytes, with dgamma or dbeta only; before: the dropout stands before the norm
+size_t norm_workspace_bytes(int64_t n, int64_t f);
+gnn_status_t norm_backward_launch(int n, int f, const float *X, const float *stat, const float *gamma, const float *beta,
+                                  int act, const Dropout &drop, bool before, const float *dY, const float *dH, float *dR,
+                                  float *dX, float *dgamma, float *dbeta, void *workspace, hipStream_t st);
+size_t gated_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k);
+gnn_status_t gated_forward_launch(int gate, int n, int m, int k, const float *X, const float *W, const float *b, float *H,
+                                  float *Z, void *workspace, hipStream_t st);
+gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X, const float *W, const float *b,
+                                   const float *Z, const float *dH, float *dW, float *db, float *dX, void *workspace,
+                                   hipStream_t st);
+
 // ---- preprocessing (prep.hip) -------------------------------------------------------
 size_t scan_workspace_bytes(int64_t n);
 // in-place exclusive scan of `count` <= n + 1 integers; workspace scan_workspace_bytes(n)

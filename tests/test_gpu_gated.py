@@ -1,0 +1,193 @@
+"""The gated feed-forward block against its definition in double precision.
+
+Bounds in units of u = 2^-24.  The products take at most eight roundings per 16 indices and term, as the library's other products, so
+[A | U] is within ez = (8 ceil(m / 16) + 8) u (|X||W| + |b|).  The activations have slopes of at most 1.13 and second derivatives of
+at most 0.8 and are taken within 16 u of themselves (relative to max(1, |a|) for their slopes)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import blocks
+from paper_2308_12093_amd import binding as B
+from tests._util import dev, host
+from tests.test_gpu_norm import shifted, space, within
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+GATES = {"sigmoid": B.GNN_GATE_SIGMOID, "silu": B.GNN_GATE_SILU, "gelu": B.GNN_GATE_GELU}
+NAN = float("nan")
+
+
+class Case:
+    def __init__(self, n, m, k, gate, bias=True, scale=1.0, seed=0):
+        rng = np.random.default_rng(n + 7 * m + 31 * k + seed)
+        f32 = lambda *s: rng.standard_normal(s).astype(np.float32)  # noqa: E731
+        self.n, self.m, self.k, self.gate = n, m, k, gate
+        self.X, self.W = f32(n, m) * np.float32(scale), f32(m, 2 * k) / np.float32(np.sqrt(m))
+        self.b = f32(2 * k) / 4 if bias else None
+        self.dH = f32(n, k)
+        self.define()
+
+    def define(self):
+        k, gate = self.k, self.gate
+        self.H, self.Z = blocks.gated_forward(self.X, self.W, self.b, gate)
+        aX, aW = np.abs(self.X).astype(np.float64), np.abs(self.W).astype(np.float64)
+        mag = aX @ aW + (0.0 if self.b is None else np.abs(self.b))
+        ez = (8 * ((self.m + 15) // 16) + 8) * U * mag
+        self.Z_most = ez
+        a, u, ea, eu = self.Z[:, :k], self.Z[:, k:], ez[:, :k], ez[:, k:]
+        g, dg = blocks.gate(gate, a)
+        eg = 1.13 * ea + 16 * U * np.abs(g)
+        edg = 0.8 * ea + 16 * U * np.maximum(1.0, np.abs(a))
+        self.H_most = eg * np.abs(u) + (np.abs(g) + eg) * eu + 2 * U * np.abs(self.H)
+        self.dW, self.db, self.dX, D = blocks.gated_backward(self.X, self.W, self.Z, self.dH, gate)
+        d = np.abs(self.dH)
+        eD = np.concatenate([d * (edg * np.abs(u) + (np.abs(dg) + edg) * eu), d * eg], 1) + 4 * U * np.abs(D)
+        aD = np.abs(D) + eD
+        self.dX_most = eD @ aW.T + (8 * ((2 * k + 15) // 16) + 8) * U * (aD @ aW.T)
+        C = 64 + 8 * ((min(self.n, 4096) + 15) // 16)      # sums over the nodes: in float for 4096 of them at most, then in double
+        self.dW_most = aX.T @ eD + C * U * (aX.T @ aD)
+        self.db_most = eD.sum(0) + C * U * aD.sum(0)
+
+
+def run(c, keep, by=0, want_dx=True):
+    n, m, k = c.n, c.m, c.k
+    X, W, dH, b = shifted(c.X, by), shifted(c.W, by), shifted(c.dH, by), None if c.b is None else shifted(c.b, by)
+    H, Z, dW, db, dX = space(n, k, by), space(n, 2 * k, by), space(m, 2 * k, by), space(1, 2 * k, by), space(n, m, by)
+    gate = GATES[c.gate]
+    for back in (False, True):
+        ws = B.alloc(B.gnn_gated_workspace_bytes(back, n, m, k))
+        ws.fill_(255)
+        if not back:
+            B.gnn_gated_fwd(gate, n, m, k, X, W, b, H[0], Z[0] if keep else None, ws)
+        else:
+            B.gnn_gated_bwd(gate, n, m, k, X, W, b, Z[0] if keep else None, dH, dW[0], db[0], dX[0] if want_dx else None, ws)
+    for _, end in (H, Z, dW, db, dX):
+        assert bool((end == 7.0).all())
+    return H[0], Z[0], dW[0], db[0][0], dX[0]
+
+
+def check(c, got, keep):
+    for t, name in zip(got, ("H", "Z", "dW", "db", "dX")):
+        if name != "Z" or keep:
+            within(t, getattr(c, name), getattr(c, name + "_most"), name)
+
+
+SHAPES = [(1, 1, 1), (1, 256, 512), (2, 3, 5), (5, 16, 16), (7, 64, 33), (31, 100, 47), (33, 33, 65), (64, 512, 100), (129, 47, 130), (200, 5, 300),
+          (300, 203, 259), (1000, 64, 64), (2049, 32, 96), (3001, 130, 70), (10000, 96, 48), (20011, 40, 129), (66001, 24, 36), (40000, 128, 256),
+          (9000, 300, 515), (5000, 700, 33), (1, 2050, 7), (17, 1030, 1026)]
+
+
+@pytest.mark.parametrize("gate", ["sigmoid", "silu", "gelu"])
+@pytest.mark.parametrize("n,m,k", SHAPES)
+def test_gated_block(n, m, k, gate):
+    big = n * (m + 2 * k) > 1 << 21
+    c = Case(n, m, k, gate)
+    for keep, by in ((True, 0), (False, 1)):
+        check(c, run(c, keep, by), keep)
+    if not big:
+        c = Case(n, m, k, gate, bias=False)
+        check(c, run(c, False, 0), False)
+
+
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 32, 33, 64, 65, 127, 128, 129, 255, 256, 257, 511, 513])
+def test_few_rows(n):
+    c = Case(n, 72, 40, "silu")
+    for keep in (False, True):
+        check(c, run(c, keep), keep)
+
+
+@pytest.mark.parametrize("gate", ["sigmoid", "silu", "gelu"])
+def test_far_from_zero(gate):
+    """Gates that are shut or open all the way: exp and erf at their ends."""
+    c = Case(400, 48, 50, gate, scale=60.0)
+    assert np.abs(c.Z).max() > 100
+    for keep in (False, True):
+        check(c, run(c, keep), keep)
+
+
+@pytest.mark.parametrize("n,m,k", [(4, 16, 16), (3000, 64, 64), (700, 130, 200)])
+def test_without_an_input_gradient(n, m, k):
+    c = Case(n, m, k, "gelu")
+    got = run(c, True)
+    again = run(c, True, want_dx=False)
+    assert all(torch.equal(a, b) for a, b in zip(got[:4], again[:4])) and bool(torch.isnan(again[4]).all())
+
+
+@pytest.mark.parametrize("n,m,k", [(3, 24, 20), (500, 64, 96), (5000, 64, 64)])
+def test_what_is_not_finite_stays_where_it_belongs(n, m, k):
+    """An infinite or NaN input spoils its row of H and dX, a NaN gradient the weights that it meets; every other row is exact."""
+    c = Case(n, m, k, "silu")
+    X = c.X.copy()
+    X[1, 2], X[n - 1, 0] = np.inf, np.nan
+    c.X, keep_X = X, c.X
+    H, _, _, _, dX = (host(t) for t in run(c, False))
+    c.X = keep_X
+    rest = [i for i in range(n) if i not in (1, n - 1)]
+    assert np.isnan(H[n - 1]).all() and not np.isfinite(H[1]).all()
+    assert (np.abs(H[rest] - c.H[rest]) <= c.H_most[rest]).all()
+    assert (np.abs(dX[rest] - c.dX[rest]) <= c.dX_most[rest]).all()
+    dH = c.dH.copy()
+    dH[0, 3] = np.nan
+    c.dH, keep_dH = dH, c.dH
+    dW, db = (host(t) for t in run(c, True)[2:4])
+    c.dH = keep_dH
+    cols = [j for j in range(2 * k) if j % k != 3]
+    assert np.isnan(dW[:, [3, k + 3]]).all() and np.isnan(db[[3, k + 3]]).all()
+    assert (np.abs(dW[:, cols] - c.dW[:, cols]) <= c.dW_most[:, cols]).all()
+
+
+def test_an_infinite_product_is_infinite():
+    """As with the fp32 instruction: parts of an infinity would make NaN of it."""
+    for n in (2, 4000):
+        c = Case(n, 32, 32, "sigmoid", bias=False)
+        W = np.abs(c.W)
+        X = np.abs(c.X)
+        X[0, 5] = np.inf
+        c.X, c.W = X, W
+        H = host(run(c, False)[0])
+        assert np.isposinf(H[0]).all() and np.isfinite(H[1:]).all()
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** 60])
+def test_magnitudes_far_from_one(scale):
+    for n in (20, 3000):
+        c = Case(n, 40, 40, "sigmoid", bias=False, scale=scale)
+        H, _, dW, _, _ = run(c, False)
+        within(H, c.H, c.H_most, "H")
+
+
+def test_no_rows():
+    dW, db = torch.full((4, 6), NAN, device="cuda"), torch.full((6,), NAN, device="cuda")
+    ws = B.alloc(B.gnn_gated_workspace_bytes(True, 0, 4, 3))
+    B.gnn_gated_bwd(0, 0, 4, 3, None, None, None, None, None, dW, db, None, ws)
+    assert not dW.any() and not db.any()
+
+
+@pytest.mark.parametrize("n,m,k", [(300, 64, 96), (5000, 64, 64), (1, 100, 60)])
+def test_a_captured_step_replays(n, m, k):
+    c = Case(n, m, k, "silu")
+    X, W, b, dH = dev(c.X), dev(c.W), dev(c.b), dev(c.dH)
+    out = dict(H=torch.empty(n, k, device="cuda"), Z=torch.empty(n, 2 * k, device="cuda"), dW=torch.empty(m, 2 * k, device="cuda"),
+               db=torch.empty(2 * k, device="cuda"), dX=torch.empty(n, m, device="cuda"))
+    ws = B.alloc(max(B.gnn_gated_workspace_bytes(back, n, m, k) for back in (0, 1)))
+
+    def step(dW=out["dW"]):
+        B.gnn_gated_fwd(1, n, m, k, X, W, b, out["H"], out["Z"], ws)
+        B.gnn_gated_bwd(1, n, m, k, X, W, b, out["Z"], dH, dW, out["db"], out["dX"], ws)
+
+    step()
+    want = {name: t.clone() for name, t in out.items()}
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    for _ in range(3):
+        for t in out.values():
+            t.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[name], want[name]) for name in out)
+        step(torch.empty_like(out["dW"]))                  # eager, on the same workspace

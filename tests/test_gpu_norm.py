@@ -1,0 +1,399 @@
+"""Dropout, layer norm and the two around a residual connection against their definitions in double precision.
+
+Bounds, in units of u = 2^-24 (half a step of a float): a sum of f floats takes at most L = f / 64 + 12 roundings per term (a
+serial part of a row that 64 lanes share, then a tree), so
+  mean        L u mean|x|                                       =: em
+  rstd        relative (L / 2 + 5) u                            =: r
+  xhat        em rstd + |xhat| (r + 2 u)                        =: ex
+  z           |gamma| ex + 3 u (|gamma xhat| + |beta|)          =: ez
+and an activation with slope of at most 1, taken within 4 u of itself, keeps ez.  The gradients follow by the same rules; a column's
+sum over the rows takes at most C = 300 roundings in float per term.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import blocks
+from paper_2308_12093_amd import binding as B
+from tests._util import dev, host
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+EPS = 1e-5
+ACTS = {"none": B.GNN_ACT_NONE, "relu": B.GNN_ACT_RELU, "elu": B.GNN_ACT_ELU}
+SEED, STEP, SITE = 0x9E3779B97F4A7C15, (5 << 32) + 17, 4
+NAN = float("nan")
+
+
+def state(seed=SEED, step=STEP):
+    return torch.from_numpy(np.array([seed, step], dtype=np.uint64).view(np.int64)).cuda()
+
+
+def shifted(a, by):
+    """The same values in memory that starts `by` floats after a 16-byte boundary."""
+    room = torch.full((a.size + by,), NAN, dtype=torch.float32, device="cuda")
+    room[by:] = dev(a).reshape(-1)
+    return room[by:].view(a.shape)
+
+
+def space(n, f, by=0):
+    """A NaN-filled output with 16 floats behind it that have to stay as they are."""
+    room = torch.full((n * f + by + 16,), NAN, device="cuda")
+    room[n * f + by:] = 7.0
+    return room[by:by + n * f].view(n, f), room[n * f + by:]
+
+
+def within(got, want, most, name):
+    got = host(got).astype(np.float64)
+    assert np.isfinite(got).all(), f"{name}: not finite"
+    over = np.abs(got - want) - most
+    worst = np.unravel_index(np.argmax(over), over.shape)
+    assert over[worst] <= 0, f"{name}{worst}: {got[worst]!r}, {want[worst]!r} expected within {most[worst]:.3g}"
+
+
+class Case:
+    """Inputs of one shape, the definition's results and how far a kernel may be from them."""
+
+    def __init__(self, n, f, act="none", p=0.0, offset=0.0, residual=False, seed=0):
+        rng = np.random.default_rng(1000 * n + f + seed)
+        f32 = lambda *s: rng.standard_normal(s).astype(np.float32)  # noqa: E731
+        self.n, self.f, self.act, self.p, self.residual = n, f, act, p, residual
+        self.X = f32(n, f) * np.float32(2.0) + np.float32(offset)
+        self.R = f32(n, f) if residual else None
+        self.gamma, self.beta = 1 + f32(f) / 4, f32(f) / 4
+        self.dY, self.dH = f32(n, f), f32(n, f) if residual else None
+        self.factor = blocks.dropout_factor(n, f, p, SEED, STEP, SITE)
+        self.drop = B.Dropout(p, state(), SITE) if p else None
+
+    def define(self, H=None):
+        """H: what a residual forward pass has left (the norm's own input)."""
+        scale = 1.0 / (1.0 - float(np.float32(self.p)))
+        if self.residual:
+            self.H = self.R.astype(np.float64) + blocks.dropout(self.X, self.factor)
+            self.H_most = 3 * U * (np.abs(self.R) + scale * np.abs(self.X))
+        x = self.H if H is None and self.residual else self.X if H is None else H
+        eh = self.H_most if H is None and self.residual else np.zeros_like(x, dtype=np.float64)
+        f, g, b = self.f, np.abs(self.gamma.astype(np.float64)), np.abs(self.beta.astype(np.float64))
+        after = 1.0 if self.residual else self.factor
+        L = f / 64 + 12
+        xhat, _, rstd = blocks.normalise(x, EPS)
+        ah = np.abs(xhat)
+        em = L * U * np.abs(x).mean(1, keepdims=True) + eh.mean(1, keepdims=True)
+        # an error d of the inputs or the mean changes the variance by mean(|x - mean| d) and d^2
+        d = em + eh
+        r = (L / 2 + 5) * U + rstd * (ah * d).mean(1, keepdims=True) + rstd ** 2 * (d * d).mean(1, keepdims=True)
+        ex = d * rstd + ah * (r + 2 * U)
+        ez = g * ex + 3 * U * (g * ah + b)
+        self.Y, z = blocks.layer_norm_forward(x, self.gamma, self.beta, EPS, self.act, after)
+        self.z = z
+        self.Y_most = (scale if self.p and not self.residual else 1.0) * (ez + 4 * U * np.abs(z))
+        dz = self.dY * (after * blocks._activation(z, self.act)[1])
+        edz = np.abs(dz) * (5 * U + (ez if self.act == "elu" else 0.0))
+        gz, egz = dz * self.gamma, edz * g + U * np.abs(dz * self.gamma)
+        s1, s2 = np.abs(gz).mean(1, keepdims=True), np.abs((gz * xhat).mean(1, keepdims=True))
+        e1 = egz.mean(1, keepdims=True) + L * U * s1
+        e2 = (egz * ah + np.abs(gz) * ex).mean(1, keepdims=True) + L * U * np.abs(gz * xhat).mean(1, keepdims=True)
+        self.dX, self.dgamma, self.dbeta = blocks.layer_norm_backward(x, self.gamma, self.beta, EPS, self.dY, self.act, after)
+        self.dX_most = rstd * (egz + e1 + ah * e2 + ex * s2 + 4 * U * (np.abs(gz) + s1 + ah * s2)) + np.abs(self.dX) * r
+        C = 300
+        self.dgamma_most = (edz * ah + np.abs(dz) * ex).sum(0) + C * U * np.abs(dz * xhat).sum(0)
+        self.dbeta_most = edz.sum(0) + C * U * np.abs(dz).sum(0)
+        if self.residual:
+            self.dR = self.dH + self.dX
+            self.dR_most = self.dX_most + 2 * U * np.abs(self.dR)
+            self.dX, self.dX_most = self.dR * self.factor, self.factor * self.dR_most + 2 * U * np.abs(self.dR * self.factor)
+
+
+def run_norm(c, by=0, gamma=True):
+    n, f = c.n, c.f
+    X, dY = shifted(c.X, by), shifted(c.dY, by)
+    ga, be = (shifted(c.gamma, by), shifted(c.beta, by)) if gamma else (None, None)
+    Y, end = space(n, f, by)
+    stat, dX, (dg, db) = torch.full((n, 2), NAN, device="cuda"), space(n, f, by), (space(1, f, by) for _ in range(2))
+    B.gnn_layer_norm_fwd(n, f, X, ga, be, EPS, ACTS[c.act], c.drop, Y, stat)
+    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(n, f))
+    ws.fill_(255)                                          # NaN in float and in double
+    B.gnn_layer_norm_bwd(n, f, X, stat, ga, be, ACTS[c.act], c.drop, dY, dX[0], dg[0], db[0], ws)
+    for e in (end, dX[1], dg[1], db[1]):
+        assert bool((e == 7.0).all())
+    return Y, dX[0], dg[0][0], db[0][0]
+
+
+def check_norm(c, got):
+    Y, dX, dg, db = got
+    within(Y, c.Y, c.Y_most, "Y")
+    if c.p:
+        assert np.array_equal(host(Y) == 0, (c.factor == 0) | (host(Y) == 0)) and not host(Y)[c.factor == 0].any()
+    within(dX, c.dX, c.dX_most, "dX")
+    within(dg, c.dgamma, c.dgamma_most, "dgamma")
+    within(db, c.dbeta, c.dbeta_most, "dbeta")
+
+
+WIDTHS = [1, 2, 3, 4, 5, 7, 16, 31, 47, 64, 100, 128, 203, 256, 257, 512, 515, 1000, 1024, 1030, 2048, 2052, 4100, 8192, 8200, 20001]
+
+
+@pytest.mark.parametrize("f", WIDTHS)
+@pytest.mark.parametrize("n", [1, 37])
+def test_layer_norm(n, f):
+    for act, p in (("none", 0.0), ("elu", 0.3)):
+        c = Case(n, f, act, p)
+        c.define()
+        for by in (0, 1):
+            check_norm(c, run_norm(c, by))
+
+
+@pytest.mark.parametrize("n,f", [(2, 64), (5, 48), (255, 12), (1023, 64), (4097, 100), (70001, 16), (300, 777), (20000, 256), (131073, 5),
+                                 (9001, 1024), (2049, 2100)])
+def test_layer_norm_of_many_rows(n, f):
+    for act, p in (("elu", 0.5), ("none", 0.0)):
+        c = Case(n, f, act, p)
+        c.define()
+        check_norm(c, run_norm(c))
+
+
+@pytest.mark.parametrize("n,f", [(500, 64), (333, 203)])
+def test_relu_backward_takes_the_signs_of_forward(n, f):
+    """No gamma xhat + beta lies within rounding of zero: where one would, its dY is set to zero."""
+    c = Case(n, f, "relu", 0.25)
+    c.define()
+    c.dY[np.abs(c.z) < 1e-4] = 0.0
+    c.define()
+    check_norm(c, run_norm(c))
+
+
+@pytest.mark.parametrize("offset", [100.0, -3000.0])
+def test_layer_norm_of_rows_far_from_zero(offset):
+    c = Case(300, 130, "elu", 0.0, offset)
+    c.define()
+    check_norm(c, run_norm(c))
+
+
+def test_layer_norm_without_weights_and_of_constant_rows():
+    c = Case(70, 65)
+    c.gamma, c.beta = np.ones(65, np.float32), np.zeros(65, np.float32)
+    c.X[::3] = np.float32(1.7)                             # no variance: xhat is 0 within the mean's rounding
+    c.define()
+    check_norm(c, run_norm(c, gamma=False))
+
+
+def test_a_row_that_is_not_finite_spoils_itself_alone():
+    c = Case(40, 96, "elu")
+    c.define()
+    c.X[7, 3], c.X[21, 95] = np.inf, np.nan
+    Y, dX = (host(t) for t in run_norm(c)[:2])
+    for t, want, most in ((Y, c.Y, c.Y_most), (dX, c.dX, c.dX_most)):
+        bad = np.isnan(t).any(1)
+        assert bad[[7, 21]].all() and bad.sum() == 2
+        rest = np.delete(np.arange(40), [7, 21])
+        assert (np.abs(t[rest] - want[rest]) <= most[rest]).all()
+
+
+def test_layer_norm_in_place_and_with_parts_of_its_gradients():
+    c = Case(77, 200, "elu", 0.4)
+    c.define()
+    want = run_norm(c)
+    X, dY, ga, be = dev(c.X), dev(c.dY), dev(c.gamma), dev(c.beta)
+    stat = torch.empty(77, 2, device="cuda")
+    Y = X.clone()
+    B.gnn_layer_norm_fwd(77, 200, Y, ga, be, EPS, ACTS["elu"], c.drop, Y, stat)
+    assert torch.equal(Y, want[0])
+    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(77, 200))
+    dg, db = torch.empty(200, device="cuda"), torch.empty(200, device="cuda")
+    both = dY.clone()
+    B.gnn_layer_norm_bwd(77, 200, X, stat, ga, be, ACTS["elu"], c.drop, both, both, dg, db, ws)
+    assert torch.equal(both, want[1]) and torch.equal(dg, want[2]) and torch.equal(db, want[3])
+    alone = torch.empty(77, 200, device="cuda")
+    B.gnn_layer_norm_bwd(77, 200, X, stat, ga, be, ACTS["elu"], c.drop, dY, alone, None, None, None)
+    assert torch.equal(alone, want[1])
+    for which in range(2):
+        one = torch.empty(200, device="cuda")
+        B.gnn_layer_norm_bwd(77, 200, X, stat, ga, be, ACTS["elu"], c.drop, dY, None, *((one, None) if which == 0 else (None, one)), ws)
+        assert torch.equal(one, want[2 + which])
+
+
+def test_weights_of_no_rows_have_gradients_of_zero():
+    dg, db = torch.full((33,), NAN, device="cuda"), torch.full((33,), NAN, device="cuda")
+    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(0, 33))
+    B.gnn_layer_norm_bwd(0, 33, None, None, None, None, 0, None, None, None, dg, db, ws)
+    B.gnn_add_layer_norm_bwd(0, 33, None, None, None, None, None, None, None, None, None, db, ws)
+    assert not dg.any() and not db.any()
+
+
+# ---------------------------------------------------------------- around a residual connection
+def run_add(c, by=0):
+    n, f = c.n, c.f
+    X, R, dY, dH = (shifted(a, by) for a in (c.X, c.R, c.dY, c.dH))
+    ga, be = shifted(c.gamma, by), shifted(c.beta, by)
+    H, Y, dR, dX = (space(n, f, by) for _ in range(4))
+    dg, db, stat = (*(space(1, f, by) for _ in range(2)), torch.full((n, 2), NAN, device="cuda"))
+    B.gnn_add_layer_norm_fwd(n, f, X, R, c.drop, ga, be, EPS, H[0], Y[0], stat)
+    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(n, f))
+    ws.fill_(255)
+    B.gnn_add_layer_norm_bwd(n, f, H[0], stat, ga, c.drop, dY, dH, dR[0], dX[0], dg[0], db[0], ws)
+    for _, e in (H, Y, dR, dX, dg, db):
+        assert bool((e == 7.0).all())
+    return H[0], Y[0], dR[0], dX[0], dg[0][0], db[0][0]
+
+
+@pytest.mark.parametrize("n,f", [(1, 1), (1, 300), (13, 3), (29, 47), (1000, 64), (333, 203), (64, 1030), (20000, 128), (17, 2052),
+                                 (10, 8200), (40001, 12)])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.6])
+def test_add_layer_norm(n, f, p):
+    c = Case(n, f, p=p, residual=True)
+    for by in (0, 3) if n < 5000 else (0,):
+        H, Y, dR, dX, dg, db = run_add(c, by)
+        c.define()
+        within(H, c.H, c.H_most, "H")
+        within(Y, c.Y, c.Y_most, "Y")
+        c.define(host(H))                                  # backward from the H that forward left
+        for got, name in ((dR, "dR"), (dX, "dX"), (dg, "dgamma"), (db, "dbeta")):
+            within(got, getattr(c, name), getattr(c, name + "_most"), name)
+
+
+def test_add_layer_norm_over_its_own_inputs():
+    c = Case(100, 72, p=0.3, residual=True)
+    H, Y, dR, dX, dg, db = run_add(c)
+    ga, be, stat, y = dev(c.gamma), dev(c.beta), torch.empty(100, 2, device="cuda"), torch.empty(100, 72, device="cuda")
+    for over in (0, 1):
+        X, R = dev(c.X), dev(c.R)
+        B.gnn_add_layer_norm_fwd(100, 72, X, R, c.drop, ga, be, EPS, (X, R)[over], y, stat)
+        assert torch.equal((X, R)[over], H) and torch.equal(y, Y)
+    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(100, 72))
+    g, b = torch.empty(72, device="cuda"), torch.empty(72, device="cuda")
+    for over in (0, 1):
+        dY, dH = dev(c.dY), dev(c.dH)
+        B.gnn_add_layer_norm_bwd(100, 72, H, stat, ga, c.drop, dY, dH, (dY, dH)[over], (dH, dY)[over], g, b, ws)
+        assert torch.equal((dY, dH)[over], dR) and torch.equal((dH, dY)[over], dX) and torch.equal(g, dg) and torch.equal(b, db)
+    # nothing flows back into H from elsewhere; the masked gradient is not asked for
+    zero, alone = torch.zeros(100, 72, device="cuda"), torch.empty(100, 72, device="cuda")
+    want = torch.empty(100, 72, device="cuda")
+    B.gnn_add_layer_norm_bwd(100, 72, H, stat, ga, c.drop, dev(c.dY), zero, want, None, g, b, ws)
+    B.gnn_add_layer_norm_bwd(100, 72, H, stat, ga, c.drop, dev(c.dY), None, alone, None, None, None, None)
+    assert torch.equal(alone, want)
+
+
+# ---------------------------------------------------------------- dropout
+@pytest.mark.parametrize("n,f", [(1, 1), (1, 1000003), (3, 2), (1000, 16), (77, 47), (2048, 64), (100003, 3), (5, 4099), (300, 512)])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 0.999])
+def test_dropout(n, f, p):
+    c = Case(n, f, p=p, residual=True)
+    kept = blocks.dropout(c.X, c.factor)
+    for by in (0, 1, 2):
+        X, R = shifted(c.X, by), shifted(c.R, by)
+        for r in (None, R):
+            Y, end = space(n, f, by)
+            B.gnn_dropout(n, f, X, r, c.drop, Y)
+            want = kept if r is None else c.R + kept
+            within(Y, want, 3 * U * (np.abs(kept) + np.abs(want)), "Y")
+            assert bool((end == 7.0).all())
+            if r is None:
+                assert not host(Y)[c.factor == 0].any()
+        for over in (X, R):
+            a, b = X.clone(), R.clone()
+            out = a if over is X else b
+            B.gnn_dropout(n, f, a, b, c.drop, out)
+            assert torch.equal(out, Y)
+
+
+def test_dropped_infinities_are_zero():
+    c = Case(50, 33, p=0.5)
+    X = np.full((50, 33), np.inf, np.float32)
+    X[::2] = np.nan
+    Y = torch.empty(50, 33, device="cuda")
+    B.gnn_dropout(50, 33, dev(X), None, c.drop, Y)
+    Y = host(Y)
+    assert not Y[c.factor == 0].any() and not np.isfinite(Y[c.factor > 0]).any()
+
+
+def test_every_operator_drops_the_same_elements():
+    """dropout(act(norm(X))) in one call and in two; the mask of a call with the same site in a residual block."""
+    c = Case(123, 50, "elu", 0.35, residual=True)
+    ga, be, stat = dev(c.gamma), dev(c.beta), torch.empty(123, 2, device="cuda")
+    both, one, two = (torch.empty(123, 50, device="cuda") for _ in range(3))
+    B.gnn_layer_norm_fwd(123, 50, dev(c.X), ga, be, EPS, ACTS["elu"], c.drop, both, stat)
+    B.gnn_layer_norm_fwd(123, 50, dev(c.X), ga, be, EPS, ACTS["elu"], None, one, stat)
+    B.gnn_dropout(123, 50, one, None, c.drop, two)
+    assert torch.equal(both, two)
+    B.gnn_add_layer_norm_fwd(123, 50, dev(c.X), dev(c.R), c.drop, ga, be, EPS, one, both, stat)
+    B.gnn_dropout(123, 50, dev(c.X), dev(c.R), c.drop, two)
+    assert torch.equal(one, two)
+
+
+def test_an_array_of_more_than_two_to_the_32_bytes_and_rows_of_it():
+    """4.3 GB; the last rows against the definition."""
+    n, f = (1 << 20) + 7, 1030
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    X = torch.randn(n, f, generator=gen, device="cuda")
+    Y, stat = torch.empty_like(X), torch.empty(n, 2, device="cuda")
+    d = B.Dropout(0.5, state(), SITE)
+    B.gnn_layer_norm_fwd(n, f, X, None, None, EPS, ACTS["elu"], d, Y, stat)
+    tail = host(X[-5:])
+    factor = blocks.dropout(np.ones((5, f)), np.ones((5, f)))
+    words = blocks.philox4x32((np.arange((f + 3) // 4)[None, :], np.arange(n - 5, n)[:, None], SITE, STEP % (1 << 32)),
+                              (SEED & 0xFFFFFFFF, SEED >> 32))
+    words = np.stack(words, -1).reshape(5, -1)[:, :f]
+    factor = np.where(words < np.uint64(1 << 31), 0.0, 2.0)
+    want, z = blocks.layer_norm_forward(tail, np.ones(f), np.zeros(f), EPS, "elu", factor)
+    within(Y[-5:], want, np.full((5, f), 2 * (f / 64 + 12) * 8 * U * np.abs(z).max()), "last rows")
+
+
+# ---------------------------------------------------------------- streams and graphs
+def step_of(t, c, drop, n, f, ws):
+    B.gnn_add_layer_norm_fwd(n, f, t["X"], t["R"], drop, t["ga"], t["be"], EPS, t["H"], t["Y"], t["stat"])
+    B.gnn_add_layer_norm_bwd(n, f, t["H"], t["stat"], t["ga"], drop, t["dY"], t["dH"], t["dR"], t["dX"], t["dg"], t["db"], ws)
+    B.gnn_layer_norm_fwd(n, f, t["H"], t["ga"], t["be"], EPS, ACTS["elu"], drop, t["Y2"], t["stat"])
+    B.gnn_layer_norm_bwd(n, f, t["H"], t["stat"], t["ga"], t["be"], ACTS["elu"], drop, t["dY"], t["dX2"], t["dg2"], t["db2"], ws)
+
+
+def test_a_captured_step_draws_anew_on_every_replay():
+    n, f = 700, 96
+    c = Case(n, f, p=0.4, residual=True)
+    t = dict(X=dev(c.X), R=dev(c.R), ga=dev(c.gamma), be=dev(c.beta), dY=dev(c.dY), dH=dev(c.dH), stat=torch.empty(n, 2, device="cuda"))
+    t.update({k: torch.empty(n, f, device="cuda") for k in ("H", "Y", "dR", "dX", "Y2", "dX2")})
+    t.update({k: torch.empty(f, device="cuda") for k in ("dg", "db", "dg2", "db2")})
+    results = ("H", "Y", "dR", "dX", "Y2", "dX2", "dg", "db", "dg2", "db2")
+    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(n, f))
+    want = []
+    rng = state(11, 2 ** 32 - 2)                           # the low word of the step wraps on the way
+    for _ in range(4):
+        step_of(t, c, B.Dropout(0.4, rng, 3), n, f, ws)
+        B.gnn_rng_advance(rng)
+        want.append({k: t[k].clone() for k in results})
+    assert host(rng).view(np.uint64).tolist() == [11, 2 ** 32 + 2]
+    assert not torch.equal(want[0]["H"], want[1]["H"])
+    rng.copy_(state(11, 2 ** 32 - 2))
+    drop = B.Dropout(0.4, rng, 3)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step_of(t, c, drop, n, f, ws)
+            B.gnn_rng_advance(rng)
+    torch.cuda.synchronize()
+    for w in want:
+        for k in results:
+            t[k].fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in results:
+            assert torch.equal(t[k], w[k]), k
+        # eager work between the replays, on the same workspace
+        B.gnn_layer_norm_bwd(n, f, t["X"], t["stat"], t["ga"], t["be"], 0, None, t["dY"], None, t["dg2"], t["db2"], ws)
+
+
+def test_calls_go_to_the_current_stream():
+    n, f = 3000, 64
+    X, Y, Z = (torch.empty(n, f, device="cuda") for _ in range(3))
+    stat = torch.empty(n, 2, device="cuda")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        X.normal_()
+        B.gnn_layer_norm_fwd(n, f, X, None, None, EPS, 0, None, Y, stat)
+        B.gnn_dropout(n, f, Y, X, B.Dropout(0.5, torch.zeros(2, dtype=torch.int64, device="cuda")), Z)
+        got = Z.sum(1)
+    s.synchronize()
+    want = host(X) + blocks.dropout(host(Y), blocks.dropout_factor(n, f, 0.5, 0, 0))
+    assert np.abs(host(Z) - want).max() < 1e-5 and bool(torch.isfinite(got).all())
