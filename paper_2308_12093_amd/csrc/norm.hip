@@ -7,6 +7,8 @@ namespace {
 // Four consecutive floats of a row of f, at any 4-byte aligned address; zeros past the row's end.
 typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
 
+typedef float floatx2u __attribute__((ext_vector_type(2), aligned(4)));
+
 __device__ __forceinline__ float4 load4(const float *row, int c, int f) {
     if (c + 4 <= f) {
         const float4u v = *reinterpret_cast<const float4u *>(row + c);
@@ -58,124 +60,428 @@ dropout_kernel(int n, int f, const float *X, const float *R, Dropout drop, float
     }
 }
 
-// One wavefront per row, which it reads three times.  With R: H = R + dropout(X) first, and no dropout after.
+// ---- layer norm -------------------------------------------------------------------------------------------
+// A row is the work of `lanes` lanes (a power of two up to a block's 256), R times four columns each, and stays in their
+// registers: mean and variance are two sums over the same registers, so that the variance is one of differences.  Every array
+// passes through memory once.  U rows at a time keep loads under way where a row is short; weights are loaded once per block.
+struct Norm {
+    int n, f, lanes;
+    const float *X, *R;                // R: H = R + dropout(X), Y = norm(H); without: Y = dropout(act(norm(X)))
+    const float *gamma, *beta;
+    float eps;
+    int act;
+    Dropout drop;
+    float *H, *Y, *stat;
+};
+
+// the sums of each of U values over the lanes of a row, in all of them
+template <int U, bool WIDE>
+__device__ __forceinline__ void row_sums(float (&v)[U], int lanes, float *red) {
+    for (int d = (WIDE ? 64 : lanes) >> 1; d > 0; d >>= 1)
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] += __shfl_xor(v[u], d, 64);
+    if constexpr (WIDE) {                                  // the row's wavefronts: two or four
+        const int wave = threadIdx.x / 64, first = threadIdx.x / lanes * (lanes / 64);
+        __syncthreads();
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int u = 0; u < U; ++u) red[4 * u + wave] = v[u];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float s = red[4 * u + first] + red[4 * u + first + 1];
+            if (lanes == 256) s += red[4 * u + 2] + red[4 * u + 3];
+            v[u] = s;
+        }
+    }
+}
+
+template <bool ALIGNED>
+__device__ __forceinline__ float4 read4(const float *row, int c, int f, bool valid) {
+    if (!valid || c >= f) return make_float4(0.f, 0.f, 0.f, 0.f);
+    if constexpr (ALIGNED) return *reinterpret_cast<const float4 *>(row + c);
+    else return load4(row, c, f);
+}
+template <bool ALIGNED>
+__device__ __forceinline__ void write4(float *row, int c, int f, float4 v) {
+    if (c >= f) return;
+    if constexpr (ALIGNED) *reinterpret_cast<float4 *>(row + c) = v;
+    else store4(row, c, f, v);
+}
+
+template <int R, int U, bool ADD, bool ALIGNED, bool WIDE>
 __global__ void __launch_bounds__(256)
-norm_forward_kernel(int n, int f, const float *X, const float *R, const float *__restrict__ gamma,
-                    const float *__restrict__ beta, float eps, int act, Dropout drop, float *H, float *Y, float *stat) {
-    const DropoutWords words(drop);
-    const int lane = threadIdx.x % 64;
-    const long row = (long)blockIdx.x * 4 + threadIdx.x / 64;
-    if (row >= n) return;
-    const float *x = X + row * f;
+norm_forward_kernel(Norm a) {
+    __shared__ float red[4 * U];
+    const DropoutWords words(a.drop);
+    const int f = a.f, lanes = a.lanes, gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
+    float4 ga[R], be[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int c = 4 * (r * lanes + gl);
+        ga[r] = a.gamma ? read4<ALIGNED>(a.gamma, c, f, true) : make_float4(1.f, 1.f, 1.f, 1.f);
+        be[r] = a.beta ? read4<ALIGNED>(a.beta, c, f, true) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (long base = (long)blockIdx.x * groups * U; base < a.n; base += (long)gridDim.x * groups * U) {
+        float4 x[U][R];
+        long row[U];
+        float mean[U], rstd[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            row[u] = base + u * groups + grp;
+#pragma unroll
+            for (int r = 0; r < R; ++r) x[u][r] = read4<ALIGNED>(a.X + row[u] * f, 4 * (r * lanes + gl), f, row[u] < a.n);
+        }
+        if constexpr (ADD) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int g = r * lanes + gl;
+                    const float4 o = read4<ALIGNED>(a.R + row[u] * f, 4 * g, f, row[u] < a.n);
+                    float4 v = words.apply(x[u][r], (uint32_t)row[u], g);
+                    v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
+                    x[u][r] = v;
+                    if (row[u] < a.n) write4<ALIGNED>(a.H + row[u] * f, 4 * g, f, v);
+                }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            mean[u] = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) mean[u] += (x[u][r].x + x[u][r].y) + (x[u][r].z + x[u][r].w);
+        }
+        row_sums<U, WIDE>(mean, lanes, red);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            mean[u] /= (float)f;
+            rstd[u] = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int c = 4 * (r * lanes + gl);
+                const float4 v = x[u][r];
+                const float d0 = c < f ? v.x - mean[u] : 0.f, d1 = c + 1 < f ? v.y - mean[u] : 0.f;
+                const float d2 = c + 2 < f ? v.z - mean[u] : 0.f, d3 = c + 3 < f ? v.w - mean[u] : 0.f;
+                x[u][r] = make_float4(d0, d1, d2, d3);
+                rstd[u] += fmaf(d0, d0, d1 * d1) + fmaf(d2, d2, d3 * d3);
+            }
+        }
+        row_sums<U, WIDE>(rstd, lanes, red);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            rstd[u] = 1.f / sqrtf(rstd[u] / (float)f + a.eps);
+            if (row[u] >= a.n) continue;
+            if (gl == 0) *reinterpret_cast<floatx2u *>(a.stat + 2 * row[u]) = floatx2u{mean[u], rstd[u]};
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int g = r * lanes + gl;
+                const float4 d = x[u][r];
+                float4 y = make_float4(fmaf(d.x * rstd[u], ga[r].x, be[r].x), fmaf(d.y * rstd[u], ga[r].y, be[r].y),
+                                       fmaf(d.z * rstd[u], ga[r].z, be[r].z), fmaf(d.w * rstd[u], ga[r].w, be[r].w));
+                if constexpr (!ADD) {
+                    y = make_float4(activation(y.x, a.act), activation(y.y, a.act), activation(y.z, a.act), activation(y.w, a.act));
+                    y = words.apply(y, (uint32_t)row[u], g);
+                }
+                write4<ALIGNED>(a.Y + row[u] * f, 4 * g, f, y);
+            }
+        }
+    }
+}
+
+struct NormBack {
+    int n, f, lanes;
+    const float *X, *stat, *gamma, *beta;
+    int act;
+    Dropout drop;
+    const float *dY, *dH;
+    float *dR, *dX;
+    float *part;                       // [block][2 f]: sums of dZ xhat and of dZ, or NULL
+};
+
+// ADD: dR = dH + the norm's gradient, dX = dropout(dR); without: dX = the norm's gradient of act'(dropout(dY)).
+template <int R, int U, bool ADD, bool ALIGNED, bool WIDE>
+__global__ void __launch_bounds__(256)
+norm_backward_kernel(NormBack a) {
+    __shared__ float red[8 * U];
+    __shared__ float4 across[256];
+    const DropoutWords words(a.drop);
+    const int f = a.f, lanes = a.lanes, gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
+    const bool write = ADD || a.dX;                        // uniform
+    float4 ga[R], be[R], dg[R], db[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int c = 4 * (r * lanes + gl);
+        ga[r] = a.gamma ? read4<ALIGNED>(a.gamma, c, f, true) : make_float4(1.f, 1.f, 1.f, 1.f);
+        be[r] = a.beta ? read4<ALIGNED>(a.beta, c, f, true) : make_float4(0.f, 0.f, 0.f, 0.f);
+        dg[r] = db[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (long base = (long)blockIdx.x * groups * U; base < a.n; base += (long)gridDim.x * groups * U) {
+        float4 x[U][R], d[U][R];
+        long row[U];
+        float rstd[U], s[2 * U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            row[u] = base + u * groups + grp;
+            const bool valid = row[u] < a.n;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int c = 4 * (r * lanes + gl);
+                x[u][r] = read4<ALIGNED>(a.X + row[u] * f, c, f, valid);
+                d[u][r] = read4<ALIGNED>(a.dY + row[u] * f, c, f, valid);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            floatx2u st = floatx2u{0.f, 0.f};
+            if (row[u] < a.n) st = *reinterpret_cast<const floatx2u *>(a.stat + 2 * row[u]);
+            rstd[u] = st.y;
+            s[2 * u] = s[2 * u + 1] = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int g = r * lanes + gl, c = 4 * g;
+                float4 &v = x[u][r], &e = d[u][r];
+                // dY past the row's end is zero; so has to be xhat, for what it is multiplied with
+                v = make_float4(c < f ? (v.x - st.x) * st.y : 0.f, c + 1 < f ? (v.y - st.x) * st.y : 0.f,
+                                c + 2 < f ? (v.z - st.x) * st.y : 0.f, c + 3 < f ? (v.w - st.x) * st.y : 0.f);
+                if constexpr (!ADD) {
+                    e = words.apply(e, (uint32_t)row[u], g);
+                    if (a.act != kActNone)
+                        e = make_float4(e.x * slope(fmaf(v.x, ga[r].x, be[r].x), a.act), e.y * slope(fmaf(v.y, ga[r].y, be[r].y), a.act),
+                                        e.z * slope(fmaf(v.z, ga[r].z, be[r].z), a.act), e.w * slope(fmaf(v.w, ga[r].w, be[r].w), a.act));
+                }
+                dg[r] = make_float4(fmaf(e.x, v.x, dg[r].x), fmaf(e.y, v.y, dg[r].y), fmaf(e.z, v.z, dg[r].z), fmaf(e.w, v.w, dg[r].w));
+                db[r] = make_float4(db[r].x + e.x, db[r].y + e.y, db[r].z + e.z, db[r].w + e.w);
+                e = make_float4(e.x * ga[r].x, e.y * ga[r].y, e.z * ga[r].z, e.w * ga[r].w);
+                s[2 * u] += (e.x + e.y) + (e.z + e.w);
+                s[2 * u + 1] += fmaf(e.x, v.x, e.y * v.y) + fmaf(e.z, v.z, e.w * v.w);
+            }
+        }
+        if (!write) continue;
+        row_sums<2 * U, WIDE>(s, lanes, red);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (row[u] >= a.n) continue;
+            const float s1 = s[2 * u] / (float)f, s2 = s[2 * u + 1] / (float)f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int g = r * lanes + gl;
+                const float4 v = x[u][r], e = d[u][r];
+                float4 o = make_float4(rstd[u] * ((e.x - s1) - v.x * s2), rstd[u] * ((e.y - s1) - v.y * s2),
+                                       rstd[u] * ((e.z - s1) - v.z * s2), rstd[u] * ((e.w - s1) - v.w * s2));
+                if constexpr (ADD) {
+                    if (a.dH) {
+                        const float4 h = read4<ALIGNED>(a.dH + row[u] * f, 4 * g, f, true);
+                        o = make_float4(o.x + h.x, o.y + h.y, o.z + h.z, o.w + h.w);
+                    }
+                    write4<ALIGNED>(a.dR + row[u] * f, 4 * g, f, o);
+                    if (!a.dX) continue;
+                    o = words.apply(o, (uint32_t)row[u], g);
+                }
+                write4<ALIGNED>(a.dX + row[u] * f, 4 * g, f, o);
+            }
+        }
+    }
+    if (!a.part) return;
+    // the block's rows: over the groups of a wavefront by shuffles, over the wavefronts through LDS
+    float *part = a.part + (size_t)blockIdx.x * 2 * f;
+#pragma unroll
+    for (int i = 0; i < 2 * R; ++i) {
+        float4 v = i < R ? dg[i] : db[i - R];
+        for (int k = lanes; k < 64; k <<= 1) {
+            v.x += __shfl_xor(v.x, k, 64);
+            v.y += __shfl_xor(v.y, k, 64);
+            v.z += __shfl_xor(v.z, k, 64);
+            v.w += __shfl_xor(v.w, k, 64);
+        }
+        if (lanes < 256) {
+            __syncthreads();
+            across[threadIdx.x] = v;
+            __syncthreads();
+            for (int k = lanes < 64 ? 64 : lanes; k < 256; k += lanes < 64 ? 64 : lanes)
+                if ((int)threadIdx.x < lanes) {
+                    const float4 o = across[threadIdx.x + k];
+                    v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
+                }
+        }
+        const int c = 4 * ((i < R ? i : i - R) * lanes + gl);
+        if ((int)threadIdx.x < lanes && c < f) {
+            float *to = part + (i < R ? 0 : f) + c;
+            to[0] = v.x;
+            if (c + 1 < f) to[1] = v.y;
+            if (c + 2 < f) to[2] = v.z;
+            if (c + 3 < f) to[3] = v.w;
+        }
+    }
+}
+
+// Rows beyond 4096 columns: a block per row, which it reads several times (16 KB and more, from the caches).
+constexpr int kNormRow = 4096;
+
+__device__ __forceinline__ float block_sum(float v, float *red) {
+    v = wave_sum(v);
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
+    __syncthreads();
+    return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+__global__ void __launch_bounds__(256)
+norm_forward_long_kernel(Norm a) {
+    __shared__ float red[4];
+    const DropoutWords words(a.drop);
+    const long row = blockIdx.x;
+    const int f = a.f;
+    const float *x = (a.R ? a.H : a.X) + row * f;
     float sum = 0.f;
-    for (int c = 4 * lane; c < f; c += 256) {
-        float4 v = load4(x, c, f);
-        if (R) {
-            const float4 r = load4(R + row * f, c, f);
+    for (int c = 4 * threadIdx.x; c < f; c += 1024) {
+        float4 v = load4(a.X + row * f, c, f);
+        if (a.R) {
+            const float4 r = load4(a.R + row * f, c, f);
             v = words.apply(v, (uint32_t)row, c / 4);
             v = make_float4(v.x + r.x, v.y + r.y, v.z + r.z, v.w + r.w);
-            store4(H + row * f, c, f, v);
-            if (c + 4 > f) v = load4(H + row * f, c, f);
+            store4(a.H + row * f, c, f, v);
         }
         sum += (v.x + v.y) + (v.z + v.w);
     }
-    if (R) x = H + row * f;
-    const float mean = wave_sum(sum) / (float)f;
+    const float mean = block_sum(sum, red) / (float)f;
     float square = 0.f;
-    for (int c = 4 * lane; c < f; c += 256)
+    for (int c = 4 * threadIdx.x; c < f; c += 1024)        // a thread reads back what it has written itself
         for (int j = 0; j < 4 && c + j < f; ++j) square = fmaf(x[c + j] - mean, x[c + j] - mean, square);
-    const float rstd = 1.f / sqrtf(wave_sum(square) / (float)f + eps);
-    if (lane == 0) { stat[2 * row] = mean; stat[2 * row + 1] = rstd; }
-    for (int c = 4 * lane; c < f; c += 256) {
+    const float rstd = 1.f / sqrtf(block_sum(square, red) / (float)f + a.eps);
+    if (threadIdx.x == 0) { a.stat[2 * row] = mean; a.stat[2 * row + 1] = rstd; }
+    for (int c = 4 * threadIdx.x; c < f; c += 1024) {
         float z[4] = {0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < 4 && c + j < f; ++j)
-            z[j] = activation(fmaf((x[c + j] - mean) * rstd, gamma ? gamma[c + j] : 1.f, beta ? beta[c + j] : 0.f), act);
+            z[j] = activation(fmaf((x[c + j] - mean) * rstd, a.gamma ? a.gamma[c + j] : 1.f, a.beta ? a.beta[c + j] : 0.f), a.act);
         float4 y = make_float4(z[0], z[1], z[2], z[3]);
-        if (!R) y = words.apply(y, (uint32_t)row, c / 4);
-        store4(Y + row * f, c, f, y);
+        if (!a.R) y = words.apply(y, (uint32_t)row, c / 4);
+        store4(a.Y + row * f, c, f, y);
     }
 }
 
-// dY through the dropout and the activation behind the norm
-__device__ __forceinline__ void norm_gradient(const DropoutWords &words, bool after, const float *x, const float *dy, long row,
-                                              int c, int f, float mean, float rstd, const float *gamma, const float *beta,
-                                              int act, float (&xhat)[4], float (&dz)[4]) {
-    float4 d = load4(dy, c, f);
+// xhat and dZ (dY through the dropout and the activation behind the norm) of four columns
+__device__ __forceinline__ void norm_gradient(const NormBack &a, const DropoutWords &words, bool after, long row, int c,
+                                              float mean, float rstd, float (&xhat)[4], float (&dz)[4]) {
+    const float *x = a.X + row * a.f;
+    float4 d = load4(a.dY + row * a.f, c, a.f);
     if (after) d = words.apply(d, (uint32_t)row, c / 4);
     const float g[4] = {d.x, d.y, d.z, d.w};
     for (int j = 0; j < 4; ++j) {
-        xhat[j] = c + j < f ? (x[c + j] - mean) * rstd : 0.f;
-        const float z = c + j < f ? fmaf(xhat[j], gamma ? gamma[c + j] : 1.f, beta ? beta[c + j] : 0.f) : 0.f;
-        dz[j] = c + j < f ? g[j] * slope(z, act) : 0.f;
+        const bool in = c + j < a.f;
+        xhat[j] = in ? (x[c + j] - mean) * rstd : 0.f;
+        const float z = in ? fmaf(xhat[j], a.gamma ? a.gamma[c + j] : 1.f, a.beta ? a.beta[c + j] : 0.f) : 0.f;
+        dz[j] = in ? g[j] * slope(z, a.act) : 0.f;
     }
 }
 
-// One wavefront per row: dR = dH + rstd (g - mean(g) - xhat mean(g xhat)), g = dZ gamma; dX = dR, dropped with `before`.
 __global__ void __launch_bounds__(256)
-norm_backward_kernel(int n, int f, const float *X, const float *__restrict__ stat, const float *__restrict__ gamma,
-                     const float *__restrict__ beta, int act, Dropout drop, bool before, const float *dY, const float *dH,
-                     float *dR, float *dX) {
-    const DropoutWords words(drop);
-    const int lane = threadIdx.x % 64;
-    const long row = (long)blockIdx.x * 4 + threadIdx.x / 64;
-    if (row >= n) return;
-    const float mean = stat[2 * row], rstd = stat[2 * row + 1];
-    float s1 = 0.f, s2 = 0.f;
-    float xhat[4], dz[4];
-    for (int c = 4 * lane; c < f; c += 256) {
-        norm_gradient(words, !before, X + row * f, dY + row * f, row, c, f, mean, rstd, gamma, beta, act, xhat, dz);
+norm_backward_long_kernel(NormBack a, bool before) {
+    __shared__ float red[4];
+    const DropoutWords words(a.drop);
+    const long row = blockIdx.x;
+    const int f = a.f;
+    const float mean = a.stat[2 * row], rstd = a.stat[2 * row + 1];
+    float s1 = 0.f, s2 = 0.f, xhat[4], dz[4];
+    for (int c = 4 * threadIdx.x; c < f; c += 1024) {
+        norm_gradient(a, words, !before, row, c, mean, rstd, xhat, dz);
         for (int j = 0; j < 4 && c + j < f; ++j) {
-            const float g = dz[j] * (gamma ? gamma[c + j] : 1.f);
+            const float g = dz[j] * (a.gamma ? a.gamma[c + j] : 1.f);
             s1 += g;
             s2 = fmaf(g, xhat[j], s2);
         }
     }
-    s1 = wave_sum(s1) / (float)f;
-    s2 = wave_sum(s2) / (float)f;
-    for (int c = 4 * lane; c < f; c += 256) {
-        norm_gradient(words, !before, X + row * f, dY + row * f, row, c, f, mean, rstd, gamma, beta, act, xhat, dz);
+    s1 = block_sum(s1, red) / (float)f;
+    s2 = block_sum(s2, red) / (float)f;
+    for (int c = 4 * threadIdx.x; c < f; c += 1024) {
+        norm_gradient(a, words, !before, row, c, mean, rstd, xhat, dz);
         float o[4] = {0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < 4 && c + j < f; ++j) {
-            o[j] = rstd * ((dz[j] * (gamma ? gamma[c + j] : 1.f) - s1) - xhat[j] * s2);
-            if (dH) o[j] += dH[row * f + c + j];
+            o[j] = rstd * ((dz[j] * (a.gamma ? a.gamma[c + j] : 1.f) - s1) - xhat[j] * s2);
+            if (a.dH) o[j] += a.dH[row * f + c + j];
         }
         float4 v = make_float4(o[0], o[1], o[2], o[3]);
-        if (dR) store4(dR + row * f, c, f, v);
+        if (a.dR) store4(a.dR + row * f, c, f, v);
         if (before) v = words.apply(v, (uint32_t)row, c / 4);
-        if (dX) store4(dX + row * f, c, f, v);
+        if (a.dX) store4(a.dX + row * f, c, f, v);
     }
 }
 
-constexpr int kNormBlocks = 256;       // partial rows of the weights' gradients
-
-// part[block] = [sum dZ xhat | sum dZ] over every kNormBlocks-th row
+// part[y] = [sum dZ xhat | sum dZ] over every gridDim.y-th row, 1024 columns per block
 __global__ void __launch_bounds__(256)
-norm_sums_kernel(int n, int f, const float *X, const float *__restrict__ stat, const float *__restrict__ gamma,
-                 const float *__restrict__ beta, int act, Dropout drop, bool after, const float *dY, double *part) {
-    const DropoutWords words(drop);
-    for (int c = 4 * threadIdx.x; c < f; c += 1024) {
-        double a[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0};
-        for (long row = blockIdx.x; row < n; row += gridDim.x) {
-            float xhat[4], dz[4];
-            norm_gradient(words, after, X + row * f, dY + row * f, row, c, f, stat[2 * row], stat[2 * row + 1], gamma, beta,
-                          act, xhat, dz);
-            for (int j = 0; j < 4; ++j) { a[j] += (double)dz[j] * xhat[j]; b[j] += dz[j]; }
+norm_sums_long_kernel(NormBack a, bool after) {
+    const DropoutWords words(a.drop);
+    const int f = a.f, c = 4 * ((int)blockIdx.x * 256 + threadIdx.x);
+    if (c >= f) return;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (long row = blockIdx.y; row < a.n; row += gridDim.y) {
+        float xhat[4], dz[4];
+        norm_gradient(a, words, after, row, c, a.stat[2 * row], a.stat[2 * row + 1], xhat, dz);
+        for (int j = 0; j < 4; ++j) {
+            s[j] = fmaf(dz[j], xhat[j], s[j]);
+            s[4 + j] += dz[j];
         }
-        for (int j = 0; j < 4 && c + j < f; ++j) {
-            part[(size_t)blockIdx.x * 2 * f + c + j] = a[j];
-            part[(size_t)blockIdx.x * 2 * f + f + c + j] = b[j];
-        }
+    }
+    for (int j = 0; j < 4 && c + j < f; ++j) {
+        a.part[(size_t)blockIdx.y * 2 * f + c + j] = s[j];
+        a.part[(size_t)blockIdx.y * 2 * f + f + c + j] = s[4 + j];
     }
 }
 
+// dgamma, dbeta = the sums of the partial rows, in double: 16 columns a block, 16 lanes each, in a fixed order
 __global__ void __launch_bounds__(256)
-norm_sums_final_kernel(int f, int blocks, const double *__restrict__ part, float *dgamma, float *dbeta) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= 2 * f) return;
-    double s = 0.0;
-    for (int b = 0; b < blocks; ++b) s += part[(size_t)b * 2 * f + c];
-    float *out = c < f ? dgamma : dbeta;
-    if (out) out[c < f ? c : c - f] = (float)s;
+norm_sums_final_kernel(int f, int blocks, const float *__restrict__ part, float *dgamma, float *dbeta) {
+    __shared__ double red[16][17];
+    const int o = threadIdx.x % 16, sl = threadIdx.x / 16;
+    const long c = (long)blockIdx.x * 16 + o, w = 2 * (long)f;
+    double a0 = 0.0, a1 = 0.0, a2 = 0.0, a3 = 0.0;
+    if (c < w) {
+        long b = sl;
+        for (; b + 48 < blocks; b += 64) {
+            a0 += part[b * w + c];
+            a1 += part[(b + 16) * w + c];
+            a2 += part[(b + 32) * w + c];
+            a3 += part[(b + 48) * w + c];
+        }
+        for (; b < blocks; b += 16) a0 += part[b * w + c];
+    }
+    red[sl][o] = (a0 + a1) + (a2 + a3);
+    __syncthreads();
+    if (sl == 0 && c < w) {
+        double t = 0.0;
+        for (int k = 0; k < 16; ++k) t += red[k][o];
+        float *out = c < f ? dgamma : dbeta;
+        if (out) out[c < f ? c : c - f] = (float)t;
+    }
+}
+
+// How a row is dealt to lanes: as few of four columns as hold it, then more per lane.
+struct Shape {
+    int lanes, per;                    // lanes a row; times four columns of each
+    bool wide;
+};
+Shape norm_shape(int f) {
+    const int groups = (f + 3) / 4;
+    int lanes = 1;
+    while (lanes < 64 && lanes < groups) lanes <<= 1;
+    int per = 1;
+    while (per < 4 && lanes * per < groups) per <<= 1;
+    while (lanes * per < groups) lanes <<= 1;              // up to kNormRow: 256 lanes
+    return Shape{lanes, per, lanes > 64};
+}
+// Blocks of the backward pass, one partial row of sums each: a group of lanes adds at most 256 rows in float.
+constexpr int kNormChain = 256;
+int64_t norm_blocks(int64_t n, int f) {
+    if (n <= 0) return 0;
+    if (f > kNormRow) {                                    // a grid's y; more rows of this length no memory holds
+        const int64_t blocks = ceil_div(n, kNormChain) > 64 ? ceil_div(n, kNormChain) : (n < 64 ? n : 64);
+        return blocks < 65535 ? blocks : 65535;
+    }
+    const Shape s = norm_shape(f);
+    const int64_t groups = 256 / s.lanes;
+    const int64_t most = ceil_div(n, groups * 4);          // four rows a group at least
+    int64_t blocks = ceil_div(n, groups * kNormChain);
+    if (blocks < 1024) blocks = most < 1024 ? most : 1024;
+    return blocks;
 }
 
 __global__ void rng_advance_kernel(uint64_t *state, uint64_t by) { state[1] += by; }
@@ -195,32 +501,72 @@ gnn_status_t dropout_launch(int n, int f, const float *X, const float *R, const 
     return launch_status();
 }
 
+#define NORM_CASE(KERNEL_, ADD_, PER_, U_, WIDE_)                                                            \
+    if (shape.per == PER_ && shape.wide == WIDE_ && add == ADD_) {                                               \
+        if (aligned) hipLaunchKernelGGL((KERNEL_<PER_, U_, ADD_, true, WIDE_>), grid, dim3(256), 0, st, a);      \
+        else hipLaunchKernelGGL((KERNEL_<PER_, U_, ADD_, false, WIDE_>), grid, dim3(256), 0, st, a);             \
+    }
+
 gnn_status_t norm_forward_launch(int n, int f, const float *X, const float *R, const float *gamma, const float *beta,
                                  float eps, int act, const Dropout &drop, float *H, float *Y, float *stat, hipStream_t st) {
     if (n <= 0) return GNN_OK;
-    hipLaunchKernelGGL(norm_forward_kernel, dim3((unsigned)ceil_div(n, 4)), dim3(256), 0, st, n, f, X, R, gamma, beta, eps, act,
-                       drop, H, Y, stat);
+    Norm a{n, f, 0, X, R, gamma, beta, eps, act, drop, H, Y, stat};
+    if (f > kNormRow) {
+        hipLaunchKernelGGL(norm_forward_long_kernel, dim3((unsigned)n), dim3(256), 0, st, a);
+        return launch_status();
+    }
+    const Shape shape = norm_shape(f);
+    a.lanes = shape.lanes;
+    const bool add = R != nullptr;
+    const bool aligned = f % 4 == 0 && aligned16(X) && aligned16(Y) && aligned16(gamma) && aligned16(beta) &&
+                         (!add || (aligned16(R) && aligned16(H)));
+    const int u = shape.wide || shape.per == 4 ? 1 : shape.per == 2 ? 2 : 4;
+    int64_t blocks = ceil_div(n, 256 / shape.lanes * u);
+    if (blocks > 2048) blocks = 2048;
+    const dim3 grid((unsigned)blocks);
+    NORM_CASE(norm_forward_kernel, false, 1, 4, false) NORM_CASE(norm_forward_kernel, false, 2, 2, false)
+    NORM_CASE(norm_forward_kernel, false, 4, 1, false) NORM_CASE(norm_forward_kernel, false, 4, 1, true)
+    NORM_CASE(norm_forward_kernel, true, 1, 4, false) NORM_CASE(norm_forward_kernel, true, 2, 2, false)
+    NORM_CASE(norm_forward_kernel, true, 4, 1, false) NORM_CASE(norm_forward_kernel, true, 4, 1, true)
     return launch_status();
 }
 
-size_t norm_workspace_bytes(int64_t n, int64_t f) { return align_up((size_t)kNormBlocks * 2 * f * sizeof(double)); }
+// not what this n takes, but what serves every smaller one as well
+size_t norm_workspace_bytes(int64_t n, int64_t f) {
+    const int64_t blocks = norm_blocks(n, (int)f);
+    return align_up((size_t)(blocks > 1024 ? blocks : 1024) * 2 * f * sizeof(float));
+}
 
 gnn_status_t norm_backward_launch(int n, int f, const float *X, const float *stat, const float *gamma, const float *beta,
                                   int act, const Dropout &drop, bool before, const float *dY, const float *dH, float *dR,
                                   float *dX, float *dgamma, float *dbeta, void *workspace, hipStream_t st) {
-    double *part = static_cast<double *>(workspace);
-    if (dgamma || dbeta) {                                 // before dX, which may lie over dY
-        hipLaunchKernelGGL(norm_sums_kernel, dim3(kNormBlocks), dim3(256), 0, st, n, f, X, stat, gamma, beta, act, drop,
-                           !before, dY, part);
-        GNN_TRY(launch_status());
-        hipLaunchKernelGGL(norm_sums_final_kernel, dim3((unsigned)ceil_div(2 * (int64_t)f, 256)), dim3(256), 0, st, f, kNormBlocks,
-                           part, dgamma, dbeta);
-        GNN_TRY(launch_status());
+    const bool sums = dgamma || dbeta, add = before;
+    if (!sums && !dX && !dR) return GNN_OK;
+    const int64_t blocks = norm_blocks(n, f);
+    NormBack a{n, f, 0, X, stat, gamma, beta, act, drop, dY, dH, dR, dX, sums ? static_cast<float *>(workspace) : nullptr};
+    if (n > 0 && f > kNormRow) {
+        if (sums) {                                        // before dX, which may lie over dY
+            hipLaunchKernelGGL(norm_sums_long_kernel, dim3((unsigned)ceil_div(f, 1024), (unsigned)blocks), dim3(256), 0, st, a, !before);
+            GNN_TRY(launch_status());
+        }
+        if (dR || dX) hipLaunchKernelGGL(norm_backward_long_kernel, dim3((unsigned)n), dim3(256), 0, st, a, before);
+    } else if (n > 0) {
+        const Shape shape = norm_shape(f);
+        a.lanes = shape.lanes;
+        const bool aligned = f % 4 == 0 && aligned16(X) && aligned16(dY) && aligned16(gamma) && aligned16(beta) &&
+                             aligned16(dX) && aligned16(dR) && aligned16(dH);
+        const dim3 grid((unsigned)blocks);
+        NORM_CASE(norm_backward_kernel, false, 1, 2, false) NORM_CASE(norm_backward_kernel, false, 2, 1, false)
+        NORM_CASE(norm_backward_kernel, false, 4, 1, false) NORM_CASE(norm_backward_kernel, false, 4, 1, true)
+        NORM_CASE(norm_backward_kernel, true, 1, 2, false) NORM_CASE(norm_backward_kernel, true, 2, 1, false)
+        NORM_CASE(norm_backward_kernel, true, 4, 1, false) NORM_CASE(norm_backward_kernel, true, 4, 1, true)
     }
-    if (n <= 0 || (!dR && !dX)) return GNN_OK;
-    hipLaunchKernelGGL(norm_backward_kernel, dim3((unsigned)ceil_div(n, 4)), dim3(256), 0, st, n, f, X, stat, gamma, beta, act,
-                       drop, before, dY, dH, dR, dX);
+    GNN_TRY(launch_status());
+    if (!sums) return GNN_OK;
+    hipLaunchKernelGGL(norm_sums_final_kernel, dim3((unsigned)ceil_div(2 * (int64_t)f, 16)), dim3(256), 0, st, f, (int)blocks,
+                       a.part, dgamma, dbeta);
     return launch_status();
 }
+#undef NORM_CASE
 
 }  // namespace gnn
