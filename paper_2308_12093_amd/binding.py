@@ -146,7 +146,8 @@ def _ptr(t):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    """The current stream's handle: torch's own accessor for launchers (0.3 us; by way of a Stream object 2.8)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _nbytes(t):
