@@ -887,6 +887,13 @@ double gemm_side_us(const TnPlans &tn, int64_t M, int64_t N, int64_t K) {
     return (t.tm * t.tn > 4 ? 0.9e-6 : 0.6e-6) * (double)reads * (double)cols * (double)K;
 }
 
+bool gemm_fits(int64_t M, int64_t N, int64_t K) {
+    if (M > INT32_MAX / 2 || N > INT32_MAX / 2 || K > INT32_MAX / 2) return false;
+    const Tiling tl = pick_tiling(M, N);
+    const int64_t total = ceil_div(M, tile_m(false, tl)) * ceil_div(N, tile_n(false, tl));
+    return total <= INT32_MAX / 4 && total * ceil_div(K, 32) <= INT32_MAX / 4;
+}
+
 bool gemm_takes_bits(int tb, int64_t M, int64_t N, int64_t K, const float *A, const float *B) {
     const bool rows16 = K % 4 == 0 && aligned16(A) && (!tb || aligned16(B));
     return M > 0 && N > 0 && K >= 4 && K <= 2048 && !few_rows(tb, M, N, K) &&
