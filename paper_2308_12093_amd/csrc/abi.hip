@@ -60,7 +60,7 @@ bool bad_gated(int gate, int32_t n, int32_t f_in, int32_t f_out) {
 
 gnn_status_t check_gated_workspace(bool backward, int32_t n, int32_t f_in, int32_t f_out, const void *workspace,
                                    size_t workspace_bytes) {
-    if (f_out > INT32_MAX / 4 || !gated_fits(backward, n, f_in, f_out)) return GNN_ERR_UNSUPPORTED;
+    if (!gated_fits(backward, n, f_in, f_out)) return GNN_ERR_UNSUPPORTED;
     if (!workspace || bad_align(workspace)) return GNN_ERR_INVALID_ARG;
     return workspace_bytes < gated_workspace_bytes(backward, n, f_in, f_out) ? GNN_ERR_BUFFER_TOO_SMALL : GNN_OK;
 }

@@ -134,12 +134,6 @@ gnn_status_t gemm_split_launch(int tb, int64_t M, int64_t N, int64_t K, const fl
                                int64_t ldc, const float *bias, int act, void *workspace, hipStream_t st,
                                const float *A2, const float *B2, const uint16_t *a_bits);
 
-// products over all nodes on split parts (gemm_tn_split.hip): see there
-bool gemm_tn_split_fits(int64_t M, int64_t N, int64_t K);
-size_t gemm_tn_split_workspace_bytes(int64_t M, int64_t N, int64_t K);
-gnn_status_t gemm_tn_split_launch(int64_t M, int64_t N, int64_t K, const float *A, const float *B, float *C, float *sums,
-                                  void *workspace, hipStream_t st);
-
 // ---- element-wise and reductions (elementwise.hip) ---------------------------------
 // out = G * [Y > 0]
 // out = G * act'(x) with the derivative taken from the activation's output Y (kActRelu or kActElu)
@@ -167,12 +161,6 @@ size_t norm_workspace_bytes(int64_t n, int64_t f);
 gnn_status_t norm_backward_launch(int n, int f, const float *X, const float *stat, const float *gamma, const float *beta,
                                   int act, const Dropout &drop, bool before, const float *dY, const float *dH, float *dR,
                                   float *dX, float *dgamma, float *dbeta, void *workspace, hipStream_t st);
-// the gated block's [A | U] with split parts (gemm_split.hip): see there
-struct Gated;                          // gated.h
-size_t gemm_gated_workspace_bytes(int64_t half, int64_t K);
-bool gemm_gated_fits(int64_t M, int64_t half);
-gnn_status_t gemm_gated_launch(int64_t M, int64_t K, const float *X, const float *W, const float *bias, const Gated &out,
-                               void *workspace, hipStream_t st);
 bool gated_fits(bool backward, int64_t n, int64_t m, int64_t k);
 size_t gated_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k);
 gnn_status_t gated_forward_launch(int gate, int n, int m, int k, const float *X, const float *W, const float *b, float *H,

@@ -15,21 +15,18 @@ struct Gated {
 };
 
 // act(a) and, where asked for, act'(a).  Phi by erfc, which keeps its relative precision where the gate shuts.
-template <bool SLOPE>
-__device__ __forceinline__ void gate_of(int gate, float a, float &g, float &dg) {
-    if (gate == GNN_GATE_GELU) {
+template <int GATE, bool SLOPE>
+__device__ __forceinline__ void gate_of(float a, float &g, float &dg) {
+    if constexpr (GATE == GNN_GATE_GELU) {
         const float below = 0.5f * erfcf(a * -0.70710678118654752f);
         g = a * below;
         if constexpr (SLOPE) dg = fmaf(a * 0.39894228040143268f, expf(-0.5f * a * a), below);
-        return;
-    }
-    const float s = 1.f / (1.f + expf(-a));
-    const float t = gate == GNN_GATE_SILU ? a : 1.f;
-    g = t * s;
-    // s' = s (1 - s); 1 - s would lose what is left of an open gate, so exp(-a) s takes its place where a > 0
-    if constexpr (SLOPE) {
-        const float shut = a > 0.f ? 1.f / (1.f + expf(a)) : 1.f - s;
-        dg = gate == GNN_GATE_SILU ? s * fmaf(a, shut, 1.f) : s * shut;
+    } else {
+        // one exponential for s(a) = 1 / (1 + exp(-a)) and s(-a) = 1 - s(a), neither of which loses its precision then
+        const float e = expf(-fabsf(a)), t = __builtin_amdgcn_rcpf(1.f + e), r = e * t;
+        const float s = a > 0.f ? t : r, shut = a > 0.f ? r : t;
+        g = GATE == GNN_GATE_SILU ? a * s : s;
+        if constexpr (SLOPE) dg = GATE == GNN_GATE_SILU ? s * fmaf(a, shut, 1.f) : s * shut;
     }
 }
 

@@ -1,6 +1,6 @@
 // The gated feed-forward block H = act(X W_gate + b_gate) .* (X W_up + b_up), forward and backward.  Its large products are
 // those of gemm_split.hip (forward, and backward where [A | U] was not kept, with the block's own epilogue) and gemm.hip.
-#include "gated.h"
+#include "gemm_half.h"
 
 namespace gnn {
 namespace {
@@ -14,7 +14,7 @@ constexpr int KB = 32;                 // reduction indices of a step: lane half
 // Few rows: four wavefronts per 32 rows and 32 columns of H share the reduction, operands straight from memory into
 // registers two steps ahead (the two lane halves of v_mfma_f32_32x32x2_f32 take 16 consecutive indices each), one launch, no
 // scratch.  A wavefront has the sums of the gate and of the other projection for the same elements.
-template <bool BACK>
+template <bool BACK, int GATE>
 __global__ void __launch_bounds__(256)
 gated_few_kernel(int M, int K, const float *__restrict__ X, const float *__restrict__ W, const float *__restrict__ bias, Gated g,
                  int tiles_n) {
@@ -85,7 +85,7 @@ gated_few_kernel(int M, int K, const float *__restrict__ X, const float *__restr
         const int m = m0 + 8 * wave + 4 * half + v;
         if (m >= M) continue;
         float act, slope = 0.f;
-        gate_of<BACK>(g.gate, s[0][v], act, slope);
+        gate_of<GATE, BACK>(s[0][v], act, slope);
         const size_t at = (size_t)m * g.half + j, two = (size_t)m * 2 * g.half + j;
         if constexpr (BACK) {
             const float dh = g.dH[at];
@@ -101,73 +101,171 @@ gated_few_kernel(int M, int K, const float *__restrict__ X, const float *__restr
     }
 }
 
-// D from the [A | U] that forward has kept, VEC columns a thread
-template <int VEC>
+// D from the [A | U] that forward has kept, and the largest magnitudes of its rows and columns.  A block takes `rows` rows
+// (kTopRows where these are wanted) and 64 VEC columns of each half, `lanes` lanes a row.
+template <int VEC, int GATE>
 __global__ void __launch_bounds__(256)
-gated_gradient_kernel(long n, int k, int gate, const float *__restrict__ Z, const float *__restrict__ dH, float *__restrict__ D) {
-    const int groups = k / VEC;
-    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n * groups; i += (long)gridDim.x * 256) {
-        const long row = i / groups, at = row * 2 * k + (i - row * groups) * VEC;
-        float a[VEC], u[VEC], d[VEC];
-        if constexpr (VEC == 4) {
-            const float4 x = *reinterpret_cast<const float4 *>(Z + at), y = *reinterpret_cast<const float4 *>(Z + at + k);
-            const float4 z = *reinterpret_cast<const float4 *>(dH + i * VEC);
-            a[0] = x.x; a[1] = x.y; a[2] = x.z; a[3] = x.w;
-            u[0] = y.x; u[1] = y.y; u[2] = y.z; u[3] = y.w;
-            d[0] = z.x; d[1] = z.y; d[2] = z.z; d[3] = z.w;
-        } else {
-            a[0] = Z[at]; u[0] = Z[at + k]; d[0] = dH[i];
+gated_gradient_kernel(long n, int k, int lanes, int rows, const float *__restrict__ Z, const float *__restrict__ dH,
+                      float *__restrict__ D, Tops tops) {
+    __shared__ unsigned across[256][2 * VEC];
+    const int gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes, c = (blockIdx.y * 64 + gl) * VEC;
+    const long r0 = (long)blockIdx.x * rows, r1 = min(n, r0 + rows);
+    unsigned top[2 * VEC];
+#pragma unroll
+    for (int v = 0; v < 2 * VEC; ++v) top[v] = 0;
+    constexpr int U = 4;                                   // rows under way
+    for (long first = r0; first < r1; first += U * groups) {
+        float a[U][VEC], u[U][VEC], d[U][VEC];
+        unsigned most[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp, at = row * 2 * k + c;
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) a[i][v] = u[i][v] = d[i][v] = 0.f;
+            if (row >= r1 || c >= k) continue;
+            if constexpr (VEC == 4) {
+                const float4 x = *reinterpret_cast<const float4 *>(Z + at), y = *reinterpret_cast<const float4 *>(Z + at + k);
+                const float4 z = *reinterpret_cast<const float4 *>(dH + row * k + c);
+                a[i][0] = x.x; a[i][1] = x.y; a[i][2] = x.z; a[i][3] = x.w;
+                u[i][0] = y.x; u[i][1] = y.y; u[i][2] = y.z; u[i][3] = y.w;
+                d[i][0] = z.x; d[i][1] = z.y; d[i][2] = z.z; d[i][3] = z.w;
+            } else {
+                a[i][0] = Z[at]; u[i][0] = Z[at + k]; d[i][0] = dH[row * k + c];
+            }
         }
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-            float g, dg;
-            gate_of<true>(gate, a[v], g, dg);
-            a[v] = d[v] * u[v] * dg;
-            u[v] = d[v] * g;
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp, at = row * 2 * k + c;
+            most[i] = 0;
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                float g, dg;
+                gate_of<GATE, true>(a[i][v], g, dg);
+                a[i][v] = d[i][v] * u[i][v] * dg;
+                u[i][v] = d[i][v] * g;
+                const unsigned ta = __float_as_uint(a[i][v]) & 0x7fffffffu, tu = __float_as_uint(u[i][v]) & 0x7fffffffu;
+                top[v] = max(top[v], ta);
+                top[VEC + v] = max(top[VEC + v], tu);
+                most[i] = max(most[i], max(ta, tu));
+            }
+            if (row >= r1 || c >= k) continue;
+            if constexpr (VEC == 4) {
+                *reinterpret_cast<float4 *>(D + at) = make_float4(a[i][0], a[i][1], a[i][2], a[i][3]);
+                *reinterpret_cast<float4 *>(D + at + k) = make_float4(u[i][0], u[i][1], u[i][2], u[i][3]);
+            } else {
+                D[at] = a[i][0]; D[at + k] = u[i][0];
+            }
         }
-        if constexpr (VEC == 4) {
-            *reinterpret_cast<float4 *>(D + at) = make_float4(a[0], a[1], a[2], a[3]);
-            *reinterpret_cast<float4 *>(D + at + k) = make_float4(u[0], u[1], u[2], u[3]);
-        } else {
-            D[at] = a[0]; D[at + k] = u[0];
+        if (!tops.rows) continue;
+        for (int q = lanes >> 1; q > 0; q >>= 1)
+#pragma unroll
+            for (int i = 0; i < U; ++i) most[i] = max(most[i], (unsigned)__shfl_xor((int)most[i], q, 64));
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp;
+            if (gl == 0 && row < r1) tops.rows[(size_t)blockIdx.y * n + row] = most[i];
         }
     }
+    if (!tops.cols) return;
+#pragma unroll
+    for (int v = 0; v < 2 * VEC; ++v) across[threadIdx.x][v] = top[v];
+    __syncthreads();
+    if (grp == 0 && c < k)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            for (int q = 1; q < groups; ++q) {
+                top[v] = max(top[v], across[q * lanes + gl][v]);
+                top[VEC + v] = max(top[VEC + v], across[q * lanes + gl][VEC + v]);
+            }
+            tops.cols[(size_t)blockIdx.x * 2 * k + c + v] = top[v];
+            tops.cols[(size_t)blockIdx.x * 2 * k + k + c + v] = top[VEC + v];
+        }
 }
 
-bool gated_few(int64_t n, int64_t m, int64_t k) {
-    return m < 4 || ceil_div(n, 32) * ceil_div(k, 32) <= 512 || !gemm_gated_fits(n, k);
-}
+// the other kernels read four indices at a time, of f_in and of 2 f_out
+bool too_narrow(int64_t m, int64_t k) { return m < 4 || k < 2; }
+bool gated_few(int64_t n, int64_t m, int64_t k) { return too_narrow(m, k) || ceil_div(n, 32) * ceil_div(k, 32) <= 512; }
 
-// [A | U] and what becomes of it
-gnn_status_t project(int64_t n, int64_t m, const float *X, const float *W, const float *b, const Gated &g, void *workspace,
-                     hipStream_t st) {
-    if (!gated_few(n, m, g.half)) return gemm_gated_launch(n, m, X, W, b, g, workspace, st);
+#define BY_GATE(GATE_, KERNEL_, ARG_)                                        \
+    ((GATE_) == GNN_GATE_SIGMOID ? KERNEL_<ARG_, GNN_GATE_SIGMOID>           \
+     : (GATE_) == GNN_GATE_SILU  ? KERNEL_<ARG_, GNN_GATE_SILU> : KERNEL_<ARG_, GNN_GATE_GELU>)
+
+gnn_status_t few(int64_t n, int64_t m, const float *X, const float *W, const float *b, const Gated &g, hipStream_t st) {
     const int64_t tiles_n = ceil_div(g.half, 32), blocks = ceil_div(n, 32) * tiles_n;
-    auto kernel = g.D ? gated_few_kernel<true> : gated_few_kernel<false>;
+    auto kernel = g.D ? BY_GATE(g.gate, gated_few_kernel, true) : BY_GATE(g.gate, gated_few_kernel, false);
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, (int)n, (int)m, X, W, b, g, (int)tiles_n);
     return launch_status();
 }
 
+gnn_status_t gradient(int64_t n, int k, int gate, const float *Z, const float *dH, float *D, const Tops &tops, int *parts,
+                      hipStream_t st) {
+    const bool vec = k % 4 == 0 && aligned16(Z) && aligned16(dH);
+    int lanes = 1;
+    while (lanes < 64 && lanes * (vec ? 4 : 1) < k) lanes <<= 1;
+    const int rows = tops.cols ? kTopRows : 4 * (256 / lanes);
+    *parts = (int)ceil_div(k, vec ? 256 : 64);
+    auto kernel = vec ? BY_GATE(gate, gated_gradient_kernel, 4) : BY_GATE(gate, gated_gradient_kernel, 1);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(n, rows), (unsigned)*parts), dim3(256), 0, st, (long)n, k, lanes, rows, Z,
+                       dH, D, tops);
+    return launch_status();
+}
+
+// scratch of a backward pass behind D
+struct Backward {
+    unsigned *x_rows, *x_cols, *d_rows, *d_cols;
+    void *rest;
+    size_t bytes;
+    Backward(char *at, int64_t n, int64_t m, int64_t k) {
+        Carver carve(at);
+        x_rows = carve.take<unsigned>(n * ceil_div(m, 64));
+        x_cols = carve.take<unsigned>(ceil_div(n, kTopRows) * m);
+        d_rows = carve.take<unsigned>(n * ceil_div(k, 32));      // gated_row_parts(k), or those of `gradient`
+        d_cols = carve.take<unsigned>(ceil_div(n, kTopRows) * 2 * k);
+        rest = carve.take<char>(0);
+        size_t most = gemm_half_workspace_bytes(2 * k, m);
+        for (size_t b : {gemm_half_workspace_bytes(m, 2 * k), gemm_half_tn_workspace_bytes(m, 2 * k, n)})
+            if (b > most) most = b;
+        bytes = carve.off + most;
+    }
+};
+
 }  // namespace
 
 bool gated_fits(bool backward, int64_t n, int64_t m, int64_t k) {
-    if (gated_few(n, m, k) ? ceil_div(n, 32) * ceil_div(k, 32) >= (int64_t)1 << 24 : !gemm_fits(n, 2 * k, m)) return false;
-    return !backward || (gemm_fits(n, m, 2 * k) && gemm_tn_split_fits(m, 2 * k, n));
+    if (m > 1 << 21 || k > 1 << 21) return false;          // 64 columns a block in y
+    if (gated_few(n, m, k)) return ceil_div(n, 32) * ceil_div(k, 32) < (int64_t)1 << 24 && (!backward || gemm_fits(n, m, 2 * k));
+    return n <= 1 << 28 && gemm_half_fits(n, 2 * k) && (!backward || (gemm_half_fits(n, m) && gemm_half_tn_fits(m, 2 * k, n)));
 }
 
-// What n rows take, or fewer: a product of few rows needs no scratch, one of more the parts of W.
+// What n rows take, or fewer: a product of few rows needs less.
 size_t gated_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k) {
-    size_t most = gated_few(n, m, k) ? kAlign : gemm_gated_workspace_bytes(k, m);
-    if (!backward) return most;
-    for (size_t b : {gemm_workspace_bytes(0, 1, n, m, 2 * k), gemm_tn_split_workspace_bytes(m, 2 * k, n)})
-        if (b > most) most = b;
-    return align_up((size_t)n * 2 * k * sizeof(float)) + most;
+    if (!backward) return gated_few(n, m, k) ? kAlign : row_tops_bytes(n, ceil_div(m, 64)) + gemm_half_workspace_bytes(2 * k, m);
+    const size_t d = align_up((size_t)n * 2 * k * sizeof(float));
+    size_t most = 0;
+    // the rows up to which the kernels for few rows run
+    const int64_t rows = too_narrow(m, k) ? n : 32 * (512 / ceil_div(k, 32)), small = n < rows ? n : rows;
+    if (small > 0) {
+        const size_t tn = gemm_workspace_bytes(1, 0, m, 2 * k, small);     // a row of sums per chunk is an m-th of it
+        most = tn + align_up(tn / m);
+        const size_t x = gemm_workspace_bytes(0, 1, small, m, 2 * k);
+        if (x > most) most = x;
+    }
+    if (!gated_few(n, m, k)) {
+        const Backward w(nullptr, n, m, k);
+        if (w.bytes > most) most = w.bytes;
+    }
+    return d + most;
 }
 
 gnn_status_t gated_forward_launch(int gate, int n, int m, int k, const float *X, const float *W, const float *b, float *H,
                                   float *Z, void *workspace, hipStream_t st) {
     if (n <= 0) return GNN_OK;
-    return project(n, m, X, W, b, Gated{k, gate, H, Z, nullptr, nullptr}, workspace, st);
+    const Gated g{k, gate, H, Z, nullptr, nullptr};
+    if (gated_few(n, m, k)) return few(n, m, X, W, b, g, st);
+    Carver carve(workspace);
+    const Tops tops{carve.take<unsigned>((size_t)n * ceil_div(m, 64)), nullptr};
+    GNN_TRY(tops_launch(n, m, X, tops, st));
+    return gemm_half_gated_launch(n, m, X, tops.rows, W, b, g, Tops{nullptr, nullptr}, carve.take<char>(0), st);
 }
 
 gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X, const float *W, const float *b,
@@ -179,19 +277,31 @@ gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X
     }
     Carver carve(workspace);
     float *d = carve.take<float>((size_t)n * 2 * k);
-    void *rest = carve.take<char>(0);
-    if (Z) {
-        const bool vec = k % 4 == 0 && aligned16(Z) && aligned16(dH);
-        int64_t blocks = ceil_div((int64_t)n * k / (vec ? 4 : 1), 256);
-        if (blocks > 1 << 20) blocks = 1 << 20;
-        auto kernel = vec ? gated_gradient_kernel<4> : gated_gradient_kernel<1>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, (long)n, k, gate, Z, dH, d);
-        GNN_TRY(launch_status());
-    } else {
-        GNN_TRY(project(n, m, X, W, b, Gated{k, gate, nullptr, nullptr, dH, d}, rest, st));
+    const Gated g{k, gate, nullptr, nullptr, dH, d};
+    int parts = 0;
+    if (gated_few(n, m, k)) {
+        void *rest = carve.take<char>(0);
+        if (Z) GNN_TRY(gradient(n, k, gate, Z, dH, d, Tops{nullptr, nullptr}, &parts, st));
+        else GNN_TRY(few(n, m, X, W, b, g, st));
+        if (dX) GNN_TRY(gemm_launch(0, 1, n, m, 2 * (int64_t)k, d, W, dX, nullptr, 0, rest, st));
+        const TnPlans tn = gemm_tn_plans(m, 2 * (int64_t)k, n);
+        GemmExtras extras{};
+        extras.sums = db;
+        extras.tn = &tn;
+        extras.workspace = static_cast<char *>(rest) + gemm_tn_workspace_bytes(tn, m, 2 * (int64_t)k);
+        return gemm_launch(1, 0, m, 2 * (int64_t)k, n, X, d, dW, nullptr, 0, rest, st, nullptr, 0, 0, nullptr, nullptr, &extras);
     }
-    if (dX) GNN_TRY(gemm_launch(0, 1, n, m, 2 * (int64_t)k, d, W, dX, nullptr, 0, rest, st));
-    return gemm_tn_split_launch(m, 2 * (int64_t)k, n, X, d, dW, db, rest, st);
+    const Backward w(static_cast<char *>(workspace) + carve.off, n, m, k);
+    const Tops of_d{w.d_rows, w.d_cols};
+    GNN_TRY(tops_launch(n, m, X, Tops{Z ? nullptr : w.x_rows, w.x_cols}, st));
+    if (Z) {
+        GNN_TRY(gradient(n, k, gate, Z, dH, d, of_d, &parts, st));
+    } else {
+        GNN_TRY(gemm_half_gated_launch(n, m, X, w.x_rows, W, b, g, of_d, w.rest, st));
+        parts = gated_row_parts(k);
+    }
+    if (dX) GNN_TRY(gemm_half_launch(n, m, 2 * (int64_t)k, d, w.d_rows, parts, W, dX, w.rest, st));
+    return gemm_half_tn_launch(m, 2 * (int64_t)k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
 }
 
 }  // namespace gnn

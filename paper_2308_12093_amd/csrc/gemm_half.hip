@@ -1,0 +1,497 @@
+// Products of fp32 matrices on the fp16 matrix instruction (half_parts.h), for the gated block: X W with the gate behind it, and
+// D W^T.
+#include "half_parts.h"
+
+namespace gnn {
+namespace {
+
+using namespace half_parts;
+
+// ---- parts of B -------------------------------------------------------------------------------------------
+// out: [32-column tile][step][instruction][part][lane][8]; lane (half, l): column 32 tile + l, indices 32 step + 16 half +
+// 8 instruction + 0..7; zeros past N and K.  exps[32 tile + l]: the column's power of two.
+// halves: B is [B_gate | B_up], and `halves` consecutive tiles hold columns of the one and the same columns of the other.
+// A block of 1024 threads finds the largest magnitudes of its tile's columns and writes kPartSteps steps of it.
+constexpr int kPartSteps = 16;
+
+template <bool TB>
+__global__ void __launch_bounds__(1024)
+half_weights_kernel(int N, int K, int steps, HalfOperand b, int halves, char *__restrict__ out, int *__restrict__ exps) {
+    __shared__ unsigned top[32];
+    const int t = threadIdx.x, lane = t % 64, l = lane % 32, half = lane / 32, ins = t / 64 % 2, sub = t / 128;
+    int n = blockIdx.x * 32 + l;
+    if (halves) {
+        const int c = blockIdx.x % halves, pair = halves / 2, j = ((int)blockIdx.x / halves * pair + c % pair) * 32 + l;
+        n = j < N / 2 ? j + (c < pair ? 0 : N / 2) : N;
+    }
+    auto fetch = [&](int step, float (&x)[8]) __attribute__((always_inline)) {
+        const int k0 = step * KB + 16 * half + 8 * ins;
+        const float *at = b.p + k0 * b.sk + n * b.sn;
+        if (TB && n < N && k0 + 8 <= K) {
+            const float4u u = *reinterpret_cast<const float4u *>(at), v = *reinterpret_cast<const float4u *>(at + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { x[j] = u[j]; x[4 + j] = v[j]; }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = n < N && k0 + j < K ? at[j * (TB ? 1 : b.sk)] : 0.f;
+        }
+    };
+    if (t < 32) top[t] = 0;
+    __syncthreads();
+    unsigned most = 0;
+    float x[8];
+    for (int s = sub; s < steps; s += 8) {
+        fetch(s, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+    }
+    most = max(most, (unsigned)__shfl_xor((int)most, 32, 64));
+    if (half == 0) atomicMax(&top[l], most);
+    __syncthreads();
+    const int e = exponent_of(top[l]);
+    if (blockIdx.y == 0 && t < 32) exps[blockIdx.x * 32 + t] = e;
+    const float scale = power_of_two(e), scale2 = power_of_two(e + 11);
+    char *to = out + (size_t)blockIdx.x * steps * kTileBytes + lane * 16;
+    const int end = min(steps, ((int)blockIdx.y + 1) * kPartSteps);
+    for (int s = blockIdx.y * kPartSteps + sub; s < end; s += 8) {
+        half8 part[2];
+        fetch(s, x);
+        halves8(x, scale, scale2, part);
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            *reinterpret_cast<half8 *>(to + (size_t)s * kTileBytes + (ins * 2 + p) * kFragBytes) = part[p];
+    }
+}
+
+// ---- rows times weights -----------------------------------------------------------------------------------
+struct HalfProduct {
+    int M, N, K, steps;
+    const float *A;
+    const unsigned *row_tops;          // [top_parts][M]
+    int top_parts;
+    HalfOperand B;
+    const char *parts;
+    const int *exps;
+    float *C;
+    const float *bias;
+    bool stream;                       // outputs beyond the caches: non-temporal stores
+    int tiles_m, tiles_n;
+    Gated gated;
+    Tops tops;                         // of D
+};
+
+// What becomes of a tile: C as it is, or [A | U] of a gated block (see Gated), the first half of whose tiles are columns of A
+// and the other half the same columns of U, so that a lane has both of an element.
+enum { kPlain, kGateForward, kGateBackward };
+
+// A block of four wavefronts owns 128 rows and 32 NT columns, a wavefront 32 rows of them.  Per step of 32 indices the block copies the
+// parts of its columns to LDS and each wavefront its rows, without touching registers, a step ahead; one barrier a step.  A lane
+// reads 16 consecutive floats of its row back and splits them.  A row's eight 16-byte pieces of a step lie in the order piece ^ (row / 2
+// mod 8), so that the reads of sixteen rows fall on different banks; whole lines are copied.  Rows read by the lanes themselves,
+// 16 bytes each, cost the L1 64 accesses an instruction instead of 8: 65536 x 512 x 2048 551 us.
+// Each buffer is an array of its own: the compiler then knows which copies a read has to wait for.
+// GATE (gnn_gate_t) is known to the compiler: with all three in it the epilogue of 32 elements a lane outgrew the instruction cache
+// (2^17 x 128 -> 256 backward 213 us).
+// ALIGNED: K is a multiple of 4, below 2^24, and A 16-byte aligned; otherwise lanes read their rows themselves.
+template <int NT, int OUT, bool ALIGNED, int GATE>
+__global__ void __launch_bounds__(256, OUT == kGateBackward ? 2 : 3)
+gemm_half_kernel(HalfProduct g) {
+    constexpr int STAGE = NT * kTileBytes;
+    __shared__ __align__(16) char even[STAGE];
+    __shared__ __align__(16) char odd[STAGE];
+    __shared__ __align__(16) char rows[ALIGNED ? 4 * 4096 : 16];
+    __shared__ int s_exp[4][32];
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t / 64), lane = t % 64, l = lane % 32, half = lane / 32;
+    const long tile = xcd_tile((long)g.tiles_m * g.tiles_n);
+    if (tile >= (long)g.tiles_m * g.tiles_n) return;
+    const int ct0 = (int)(tile % g.tiles_n) * NT, row0 = ((int)(tile / g.tiles_n) * 4 + wave) * 32;
+    auto column = [&](int c) __attribute__((always_inline)) {       // of this lane in tile c; N where there is none
+        if constexpr (OUT == kPlain) return min((ct0 + c) * 32 + l, g.N);
+        const int j = (ct0 / 2 + c % (NT / 2)) * 32 + l;
+        return j < g.gated.half ? j + (c < NT / 2 ? 0 : g.gated.half) : g.N;
+    };
+    const size_t ro = (size_t)min(row0 + l, g.M - 1) * g.K;      // rows past the end re-read the last one
+
+    // Four indices at a time, at any 4-byte aligned address; the ones that would run over the row's end are read from
+    // its last four floats instead (K >= 4) and put in place by `settle`, so no load stands behind a branch.
+    floatx4 raw[4];
+    auto load = [&](int step) __attribute__((always_inline)) {
+        const int k = min(step, g.steps - 1) * KB + 16 * half;     // the last step again after the last: no branch, no use
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const float4u *>(g.A + ro + min(k + 4 * i, g.K - 4));
+    };
+    auto settle = [&](int step) __attribute__((always_inline)) {
+        const int k0 = step * KB;
+        if (k0 + KB <= g.K) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            // floats past the end: 0 none .. 4 all; a shift by one, by two and by four places
+            const int over = min(max(k0 + 16 * half + 4 * i + 4 - g.K, 0), 4);
+            const bool one = over & 1, two = over & 2, all = over & 4;
+            floatx4 v = raw[i];
+            v = floatx4{one ? v.y : v.x, one ? v.z : v.y, one ? v.w : v.z, one ? 0.f : v.w};
+            v = floatx4{two ? v.z : v.x, two ? v.w : v.y, two ? 0.f : v.z, two ? 0.f : v.w};
+            raw[i] = floatx4{all ? 0.f : v.x, all ? 0.f : v.y, all ? 0.f : v.z, all ? 0.f : v.w};
+        }
+    };
+    // global -> LDS, 1 KB per wavefront and instruction, from a uniform base and a 32-bit offset
+    auto copy = [](const void *base, unsigned offset, char *to) __attribute__((always_inline)) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)((const char *)base + offset),
+                                         (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+    };
+    // the 4 NT fragments of a step are dealt to the four wavefronts
+    auto stage = [&](int step, char *buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int f = wave + 4 * i;
+            copy(g.parts + ((size_t)(ct0 + f / 4) * g.steps + step) * kTileBytes + f % 4 * kFragBytes, lane * 16, buf + f * kFragBytes);
+        }
+    };
+    // eight rows an instruction; pieces past the row's end re-read its last
+    const int first = min(row0, g.M - 1);
+    const float *base = g.A + (size_t)first * g.K;
+    unsigned mine[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine[i] = (unsigned)min(8 * i + lane / 8, g.M - 1 - first) * (unsigned)g.K;
+    auto stage_rows = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int piece = 4 * (lane % 8 ^ (4 * (i % 2) + lane / 16));
+            copy(base + step * KB, 4 * (mine[i] + min(piece, g.K - 4 - step * KB)), rows + wave * 4096 + i * 1024);
+        }
+    };
+    stage(0, even);
+    if constexpr (ALIGNED) stage_rows(0);
+    else load(0);
+    float scale, scale2;
+    {
+        unsigned top = 0;
+        for (int p = 0; p < g.top_parts; ++p) top = max(top, g.row_tops[(size_t)p * g.M + min(row0 + l, g.M - 1)]);
+        const int e = exponent_of(top);
+        scale = power_of_two(e);
+        scale2 = power_of_two(e + 11);
+        if (half == 0) s_exp[wave][l] = e;
+    }
+    // what the epilogue of a backward pass reads, under way from the start: with short rows there is little else to wait beside
+    float dh[OUT == kGateBackward ? NT / 2 : 1][16];
+    if constexpr (OUT == kGateBackward)
+#pragma unroll
+        for (int c = 0; c < NT / 2; ++c)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                dh[c][v] = g.gated.dH[(size_t)min(row0 + 4 * half + 8 * (v / 4) + v % 4, g.M - 1) * g.gated.half +
+                                      min((ct0 / 2 + c) * 32 + l, g.gated.half - 1)];
+    floatx16 acc[NT];
+    auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[c][v] = 0.f;
+    };
+    clear();
+    auto turn = [&](int step, const char *buf, char *next) __attribute__((always_inline)) {
+        // this wavefront's copies of the step have arrived; after the barrier everyone's have, and the other buffer,
+        // read in the step before, is free
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (step + 1 < g.steps) stage(step + 1, next);
+        if constexpr (ALIGNED) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                raw[i] = *reinterpret_cast<const floatx4 *>(rows + wave * 4096 + l * 128 + ((4 * half + i) ^ (l / 2 % 8)) * 16);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // read before the next step's rows overwrite them
+            if (step + 1 < g.steps) stage_rows(step + 1);
+        }
+        half8 a[2][2];
+        settle(step);
+#pragma unroll
+        for (int ins = 0; ins < 2; ++ins) {
+            const floatx4 u = raw[2 * ins], v = raw[2 * ins + 1];
+            halves8({u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]}, scale, scale2, a[ins]);
+        }
+        if constexpr (!ALIGNED) load(step + 1);
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            half8 b[2][2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                b[i / 2][i % 2] = *reinterpret_cast<const half8 *>(buf + (c * 4 + i) * kFragBytes + lane * 16);
+            multiply(acc[c], a, b);
+        }
+    };
+    for (int step = 0; step < g.steps; step += 2) {
+        turn(step, even, odd);
+        if (step + 1 < g.steps) turn(step + 1, odd, even);
+    }
+    float finite = 0.f;
+#pragma unroll
+    for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) finite = fmaf(acc[c][v], 0.f, finite);
+    const bool again = __any(finite != 0.f);               // 0 x (inf or NaN) is NaN
+    if (again) {
+        clear();
+        for (int step = 0; step < g.steps; ++step) {
+            load(step);
+            settle(step);
+            const int k0 = step * KB + 16 * half;
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+#pragma unroll
+                for (int c = 0; c < NT; ++c) {
+                    const int n = column(c);
+                    const float bv = k0 + j < g.K && n < g.N ? g.B.p[(k0 + j) * g.B.sk + n * g.B.sn] : 0.f;
+                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(raw[j / 4][j % 4], bv, acc[c], 0, 0, 0);
+                }
+        }
+    }
+    int eb[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) eb[c] = again ? 0 : g.exps[(ct0 + c) * 32 + l];
+    auto out = [&](float *at, float o) __attribute__((always_inline)) {
+        if (g.stream) __builtin_nontemporal_store(o, at);
+        else *at = o;
+    };
+    // accumulator register v of lane (half, l): row 8 (v / 4) + 4 half + v % 4, column l of its 32 x 32 tile
+    auto value = [&](int c, int v) __attribute__((always_inline)) {
+        const int ea = again ? 0 : s_exp[wave][8 * (v / 4) + 4 * half + v % 4];
+        return ldexpf(acc[c][v], -(ea + eb[c]));
+    };
+    if constexpr (OUT == kPlain) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int row = row0 + 8 * (v / 4) + 4 * half + v % 4;
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {                 // the columns of a row one after the other
+                const int n = (ct0 + c) * 32 + l;
+                if (row < g.M && n < g.N) out(g.C + (size_t)row * g.N + n, value(c, v));
+            }
+        }
+    } else {
+        const int k = g.gated.half;
+        unsigned col_top[NT], row_top[16];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) col_top[c] = 0;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) row_top[v] = 0;
+#pragma unroll
+        for (int c = 0; c < NT / 2; ++c) {
+            const int j = (ct0 / 2 + c) * 32 + l, jj = min(j, k - 1);
+            const float ba = g.bias ? g.bias[jj] : 0.f, bu = g.bias ? g.bias[k + jj] : 0.f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int row = row0 + 4 * half + 8 * (v / 4) + v % 4;
+                const bool in = row < g.M && j < k;
+                const float a = value(c, v) + ba, u = value(c + NT / 2, v) + bu;
+                float act, slope = 0.f;
+                gate_of<GATE, OUT == kGateBackward>(a, act, slope);
+                if constexpr (OUT == kGateBackward) {
+                    const float da = in ? dh[c][v] * u * slope : 0.f, du = in ? dh[c][v] * act : 0.f;
+                    if (in) {
+                        out(g.gated.D + (size_t)row * 2 * k + j, da);
+                        out(g.gated.D + (size_t)row * 2 * k + k + j, du);
+                    }
+                    const unsigned ta = __float_as_uint(da) & 0x7fffffffu, tu = __float_as_uint(du) & 0x7fffffffu;
+                    col_top[c] = max(col_top[c], ta);
+                    col_top[c + NT / 2] = max(col_top[c + NT / 2], tu);
+                    row_top[v] = max(row_top[v], max(ta, tu));
+                } else if (in) {
+                    out(g.gated.H + (size_t)row * k + j, act * u);
+                    if (g.gated.Z) {
+                        out(g.gated.Z + (size_t)row * 2 * k + j, a);
+                        out(g.gated.Z + (size_t)row * 2 * k + k + j, u);
+                    }
+                }
+            }
+        }
+        if constexpr (OUT == kGateBackward) {
+            // over the 32 lanes of a row: each step a lane hands on half of its rows and keeps the other half; in the end lanes
+            // 2 v and 2 v + 1 have row v
+#pragma unroll
+            for (int d = 16, rows = 8; rows >= 1; d >>= 1, rows >>= 1) {
+                const bool upper = l & d;
+#pragma unroll
+                for (int v = 0; v < rows; ++v) {
+                    const unsigned give = upper ? row_top[v] : row_top[v + rows], keep = upper ? row_top[v + rows] : row_top[v];
+                    row_top[v] = max(keep, (unsigned)__shfl_xor((int)give, d, 64));
+                }
+            }
+            row_top[0] = max(row_top[0], (unsigned)__shfl_xor((int)row_top[0], 1, 64));
+            const int v = l / 2, row = row0 + 4 * half + 8 * (v / 4) + v % 4;
+            if (l % 2 == 0 && row < g.M) g.tops.rows[(size_t)(ct0 / NT) * g.M + row] = row_top[0];
+            unsigned *s = reinterpret_cast<unsigned *>(even);      // the block's rows: kTopRows of them
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                col_top[c] = max(col_top[c], (unsigned)__shfl_xor((int)col_top[c], 32, 64));
+                if (half == 0) s[(wave * NT + c) * 32 + l] = col_top[c];
+            }
+            __syncthreads();
+            const int c = t / 32, j = (ct0 / 2 + c % (NT / 2)) * 32 + t % 32;
+            if (t < NT * 32 && j < k)
+                g.tops.cols[(size_t)(tile / g.tiles_n) * 2 * k + (c < NT / 2 ? 0 : k) + j] =
+                    max(max(s[t], s[NT * 32 + t]), max(s[2 * NT * 32 + t], s[3 * NT * 32 + t]));
+        }
+    }
+}
+
+// ---- largest magnitudes -----------------------------------------------------------------------------------
+// A block reads `rows` rows (kTopRows where the columns' are wanted) and 64 VEC columns, `lanes` lanes a row.
+template <int VEC>
+__global__ void __launch_bounds__(256)
+tops_kernel(long n, int m, int lanes, int rows, const float *__restrict__ X, Tops tops) {
+    __shared__ unsigned across[256][VEC];
+    const int gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes, c = (blockIdx.y * 64 + gl) * VEC;
+    const long r0 = (long)blockIdx.x * rows, r1 = min(n, r0 + rows);
+    unsigned top[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) top[v] = 0;
+    constexpr int U = 8;                                   // rows under way
+    for (long first = r0; first < r1; first += U * groups) {
+        unsigned x[U][VEC], most[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp;
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) x[i][v] = 0;
+            if (row >= r1 || c >= m) continue;
+            if constexpr (VEC == 4) {
+                const uintx4 u = *reinterpret_cast<const uintx4 *>(X + row * m + c);
+                x[i][0] = u.x; x[i][1] = u.y; x[i][2] = u.z; x[i][3] = u.w;
+            } else {
+                x[i][0] = __float_as_uint(X[row * m + c]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            most[i] = 0;
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                x[i][v] &= 0x7fffffffu;
+                top[v] = max(top[v], x[i][v]);
+                most[i] = max(most[i], x[i][v]);
+            }
+        }
+        if (!tops.rows) continue;
+        for (int d = lanes >> 1; d > 0; d >>= 1)
+#pragma unroll
+            for (int i = 0; i < U; ++i) most[i] = max(most[i], (unsigned)__shfl_xor((int)most[i], d, 64));
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp;
+            if (gl == 0 && row < r1) tops.rows[(size_t)blockIdx.y * n + row] = most[i];
+        }
+    }
+    if (!tops.cols) return;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) across[threadIdx.x][v] = top[v];
+    __syncthreads();
+    if (grp == 0 && c < m)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            for (int k = 1; k < groups; ++k) top[v] = max(top[v], across[k * lanes + gl][v]);
+            tops.cols[(size_t)blockIdx.x * m + c + v] = top[v];
+        }
+}
+
+// 32-column tiles of a block
+int half_tiles(int64_t N) { return N <= 64 ? 2 : 4; }
+
+size_t half_parts_bytes(int64_t N, int64_t K) {
+    const int64_t w = half_tiles(N);
+    return align_up((size_t)(ceil_div(N, 32 * w) * w) * ceil_div(K, KB) * kTileBytes);
+}
+
+void set_product(HalfProduct &g, int64_t M, int64_t N, int64_t K, void *workspace) {
+    const int w = half_tiles(N);
+    g.M = (int)M; g.N = (int)N; g.K = (int)K;
+    g.steps = (int)ceil_div(K, KB);
+    g.tiles_m = (int)ceil_div(M, 128); g.tiles_n = (int)ceil_div(N, 32 * w);
+    g.parts = static_cast<char *>(workspace);
+    g.exps = reinterpret_cast<int *>(static_cast<char *>(workspace) + half_parts_bytes(N, K));
+}
+
+gnn_status_t split_weights(const HalfProduct &g, int halves, hipStream_t st) {
+    const dim3 grid((unsigned)(g.tiles_n * half_tiles(g.N)), (unsigned)ceil_div(g.steps, kPartSteps));
+    auto kernel = g.B.sk == 1 ? half_weights_kernel<true> : half_weights_kernel<false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(1024), 0, st, g.N, g.K, g.steps, g.B, halves, const_cast<char *>(g.parts),
+                       const_cast<int *>(g.exps));
+    return launch_status();
+}
+
+dim3 product_grid(const HalfProduct &g) { return dim3((unsigned)(8 * ceil_div((int64_t)g.tiles_m * g.tiles_n, 8))); }
+
+}  // namespace
+
+// a grid has less than 2^32 threads
+bool gemm_half_fits(int64_t M, int64_t N) {
+    return N <= INT32_MAX / 4 && M <= INT32_MAX - 256 && ceil_div(M, 128) * ceil_div(N, 32 * half_tiles(N)) < ((int64_t)1 << 24) - 8;
+}
+
+size_t gemm_half_workspace_bytes(int64_t N, int64_t K) {
+    return half_parts_bytes(N, K) + align_up((size_t)(ceil_div(N, 32) + 3) * 32 * sizeof(int));
+}
+
+size_t row_tops_bytes(int64_t n, int64_t parts) { return align_up((size_t)n * parts * sizeof(unsigned)); }
+size_t col_tops_bytes(int64_t n, int64_t columns) { return align_up((size_t)ceil_div(n, kTopRows) * columns * sizeof(unsigned)); }
+
+int top_parts(int64_t m, const float *X) { return (int)ceil_div(m, m % 4 == 0 && aligned16(X) ? 256 : 64); }
+
+gnn_status_t tops_launch(int64_t n, int m, const float *X, const Tops &tops, hipStream_t st) {
+    const bool vec = m % 4 == 0 && aligned16(X);
+    int lanes = 1;
+    while (lanes < 64 && lanes * (vec ? 4 : 1) < m) lanes <<= 1;
+    const int rows = tops.cols ? kTopRows : 8 * (256 / lanes);
+    const dim3 grid((unsigned)ceil_div(n, rows), (unsigned)top_parts(m, X));
+    hipLaunchKernelGGL(vec ? tops_kernel<4> : tops_kernel<1>, grid, dim3(256), 0, st, (long)n, m, lanes, rows, X, tops);
+    return launch_status();
+}
+
+gnn_status_t gemm_half_launch(int64_t M, int64_t N, int64_t K, const float *A, const unsigned *row_tops, int parts, const float *B,
+                              float *C, void *workspace, hipStream_t st) {
+    HalfProduct g{};
+    set_product(g, M, N, K, workspace);
+    g.A = A; g.row_tops = row_tops; g.top_parts = parts;
+    g.B = HalfOperand{B, 1, (long)K};
+    g.C = C;
+    g.stream = (size_t)M * N * sizeof(float) > kStreamBytes;
+    GNN_TRY(split_weights(g, 0, st));
+    const bool aligned = K % 4 == 0 && K < 1 << 24 && aligned16(A);
+    auto kernel = half_tiles(N) == 2 ? (aligned ? gemm_half_kernel<2, kPlain, true, 0> : gemm_half_kernel<2, kPlain, false, 0>)
+                                     : (aligned ? gemm_half_kernel<4, kPlain, true, 0> : gemm_half_kernel<4, kPlain, false, 0>);
+    hipLaunchKernelGGL(kernel, product_grid(g), dim3(256), 0, st, g);
+    return launch_status();
+}
+
+int gated_row_parts(int64_t half) { return (int)ceil_div(2 * half, 32 * half_tiles(2 * half)); }
+
+gnn_status_t gemm_half_gated_launch(int64_t M, int64_t K, const float *X, const unsigned *row_tops, const float *W,
+                                    const float *bias, const Gated &out, const Tops &tops, void *workspace, hipStream_t st) {
+    HalfProduct g{};
+    const int64_t N = 2 * (int64_t)out.half;
+    const int w = half_tiles(N);
+    set_product(g, M, N, K, workspace);
+    g.tiles_n = (int)ceil_div(out.half, 16 * w);
+    g.A = X; g.row_tops = row_tops; g.top_parts = top_parts(K, X);
+    g.B = HalfOperand{W, (long)N, 1};
+    g.bias = bias;
+    g.gated = out;
+    g.tops = tops;
+    g.stream = !out.D && (size_t)M * N * sizeof(float) > kStreamBytes;      // D is read next
+    GNN_TRY(split_weights(g, w, st));
+    const bool aligned = K % 4 == 0 && K < 1 << 24 && aligned16(X), back = out.D != nullptr;
+    const dim3 grid = product_grid(g);
+#define GATED_CASE(NT_, ALIGNED_, GATE_)                                                                                    \
+    if (w == NT_ && aligned == ALIGNED_ && out.gate == GATE_) {                                                             \
+        if (back) hipLaunchKernelGGL((gemm_half_kernel<NT_, kGateBackward, ALIGNED_, GATE_>), grid, dim3(256), 0, st, g);   \
+        else hipLaunchKernelGGL((gemm_half_kernel<NT_, kGateForward, ALIGNED_, GATE_>), grid, dim3(256), 0, st, g);         \
+    }
+#define GATED_CASES(NT_, ALIGNED_) \
+    GATED_CASE(NT_, ALIGNED_, GNN_GATE_SIGMOID) GATED_CASE(NT_, ALIGNED_, GNN_GATE_SILU) GATED_CASE(NT_, ALIGNED_, GNN_GATE_GELU)
+    GATED_CASES(2, false) GATED_CASES(2, true) GATED_CASES(4, false) GATED_CASES(4, true)
+#undef GATED_CASES
+#undef GATED_CASE
+    return launch_status();
+}
+
+}  // namespace gnn

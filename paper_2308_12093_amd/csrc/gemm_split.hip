@@ -14,17 +14,54 @@
 // are not finite (operands that are not, or that the rounding to bf16 or a partial sum carries over the edge), and a tile
 // with operands whose third part falls below the bf16 range (magnitudes below 2^-110: they lose up to 2^-134) where that
 // loss may show in a result.
-#include "gated.h"
-#include "split_parts.h"
+#include "common.h"
 
 namespace gnn {
 namespace {
 
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));   // 16 bytes at a 4-byte aligned address
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 
 constexpr int KB = 32;                 // reduction indices of a step: lane half h takes 16 h .. 16 h + 15
 constexpr unsigned kTinyCode = 2 * ((127u - 110) << 23) - 1;   // magnitude_code(2^-110)
+constexpr int kFragBytes = 64 * 16;    // eight bf16 per lane: one operand of one instruction
 constexpr int kStepBytes = 2 * 3 * kFragBytes;   // [instruction][part] for 32 columns and KB indices
+
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((floatx2){a, b}, bf16x2));
+}
+__device__ __forceinline__ float low(unsigned u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float high(unsigned u) { return __uint_as_float(u & 0xffff0000u); }
+
+// orders like the magnitude, except that zero comes last
+__device__ __forceinline__ unsigned magnitude_code(float a) { return 2 * __float_as_uint(a) - 1; }
+
+// three parts of eight floats; `least` collects the smallest magnitude code
+__device__ __forceinline__ void split8(const floatx4 &x, const floatx4 &y, bf16x8 (&part)[3], unsigned &least) {
+    uintx4 u[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = i < 2 ? x[2 * i] : y[2 * i - 4], b = i < 2 ? x[2 * i + 1] : y[2 * i - 3];
+        least = min(least, min(magnitude_code(a), magnitude_code(b)));
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            const unsigned h = pack_bf16(a, b);
+            u[p][i] = h;
+            if (p < 2) { a -= low(h); b -= high(h); }
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) part[p] = __builtin_bit_cast(bf16x8, u[p]);
+}
+
+// the kept products, smallest first; the last, of the leading parts, goes to the sum itself
+constexpr int kProducts = 6;
+__device__ constexpr int kPartA[kProducts] = {1, 0, 2, 1, 0, 0}, kPartB[kProducts] = {1, 2, 0, 0, 1, 0};
 
 // columns of B as the kernels read it: element (k, n) at k * sk + n * sn
 struct Operand {
@@ -36,8 +73,6 @@ struct Operand {
 // out: [32-column tile][KB step][instruction][part][lane][8]; lane (half, l): column 32 tile + l, indices
 // KB step + 16 half + 8 instruction + 0..7; zeros past N and K.  range[tile]: the tile's smallest magnitude code and its
 // largest magnitude.  One block per tile, 1024 threads: eight steps at a time.
-// halves: B is [B_gate | B_up], of N / 2 columns each, and `halves` consecutive tiles hold columns of the one and the same
-// columns of the other, so that a wavefront of the product has both.
 struct Range {
     unsigned least;
     float top;
@@ -45,17 +80,13 @@ struct Range {
 
 __global__ void __launch_bounds__(1024)
 split_weights_kernel(int N, int K, int steps, Operand b0, Operand b1, char *__restrict__ out0, char *__restrict__ out1,
-                     Range *__restrict__ range0, Range *__restrict__ range1, int halves) {
+                     Range *__restrict__ range0, Range *__restrict__ range1) {
     __shared__ unsigned s_least, s_top;
     const Operand b = blockIdx.y ? b1 : b0;
     char *out = (blockIdx.y ? out1 : out0) + (size_t)blockIdx.x * steps * kStepBytes;
     const int lane = threadIdx.x % 64, ins = (threadIdx.x / 64) % 2, sub = threadIdx.x / 128;
     const int l = lane % 32, half = lane / 32;
-    int n = blockIdx.x * 32 + l;
-    if (halves) {
-        const int c = blockIdx.x % halves, pair = halves / 2, j = ((int)blockIdx.x / halves * pair + c % pair) * 32 + l;
-        n = j < N / 2 ? j + (c < pair ? 0 : N / 2) : N;
-    }
+    const int n = blockIdx.x * 32 + l;
     if (threadIdx.x == 0) { s_least = ~0u; s_top = 0; }
     __syncthreads();
     unsigned least = ~0u, top = 0;                          // magnitudes order like their bits, NaN last
@@ -96,7 +127,6 @@ struct Product {
     int tiles_m, tiles_n;
     const uint16_t *a_bits;            // see GemmExtras
     int bit_words, bit_stride;         // of a row, in memory and in LDS (an odd number of banks)
-    Gated gated;
 };
 
 // logical tile of a block: each XCD (ids are dealt round-robin to eight) takes a contiguous range, the column tiles of
@@ -137,11 +167,7 @@ __host__ __device__ constexpr int kept_waves(int nt) { return nt == 1 ? 16 : 12;
 // kept_pays says where.
 // BITS: A is used where its bit is set; a lane's 16 floats have one word, from the block's copy in LDS (held in registers a
 // step ahead it spills).
-// GATE: C = [A | U] of a gated block is not written as such (kGateForward, kGateBackward: see Gated).  The first half of a
-// block's tiles are columns of A, the other half the same columns of U, so that a lane has both of an element: what a pass over
-// 4 n half floats behind the product took (2^16 x 1024 242 us of 985, forward) is done in registers.
-constexpr int kGateForward = 1, kGateBackward = 2;
-template <int NT, bool BITS, int KEPT, int GATE = 0>
+template <int NT, bool BITS, int KEPT>
 __global__ void __launch_bounds__(KEPT ? 64 * KEPT : 256, (NT == 4 || (KEPT && NT == 2) ? 3 : 4) - (BITS && NT > 1))
 gemm_split_kernel(Product g) {
     extern __shared__ __align__(16) char lds[];
@@ -165,11 +191,6 @@ gemm_split_kernel(Product g) {
         rt_by = 1;
     }
     int row0 = rt * 32;
-    auto column = [&](int c) __attribute__((always_inline)) {       // of this lane in tile c; N where there is none
-        if constexpr (GATE == 0) return (ct0 + c) * 32 + l;
-        const int j = (ct0 / 2 + c % (NT / 2)) * 32 + l;
-        return j < g.gated.half ? j + (c < NT / 2 ? 0 : g.gated.half) : g.N;
-    };
     // rows past the end re-read the last one
     auto row_offset = [&](int r) __attribute__((always_inline)) { return (size_t)min(r * 32 + l, g.M - 1) * g.K; };
     size_t ro = row_offset(rt);
@@ -391,7 +412,7 @@ gemm_split_kernel(Product g) {
             for (int v = 0; v < 16; ++v) {
                 const int row = 8 * (v / 4) + v % 4;         // of this register, behind the shift by 4 half
                 const float most = ((tiny >> row) & 1 ? of_b : 0.f) + ((zero >> row) & 1 ? 0.f : of_a);
-                bad |= column(c) < g.N && !(fabsf(acc[c][v]) >= most);
+                bad |= (ct0 + c) * 32 + l < g.N && !(fabsf(acc[c][v]) >= most);
             }
         }
     }
@@ -408,7 +429,7 @@ gemm_split_kernel(Product g) {
             for (int j = 0; j < 16; ++j)
 #pragma unroll
                 for (int c = 0; c < NT; ++c) {
-                    const int n = column(c);
+                    const int n = (ct0 + c) * 32 + l;
                     const float bv = k0 + j < g.K && n < g.N ? b.p[(k0 + j) * b.sk + n * b.sn] : 0.f;
                     acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(raw[j / 4][j % 4], bv, acc[c], 0, 0, 0);
                 }
@@ -428,42 +449,7 @@ gemm_split_kernel(Product g) {
             for (int c = 0; c < NT; ++c) acc[c][v] *= back;
         }
     }
-    if constexpr (GATE != 0) {
-        const int n = g.gated.half;
-#pragma unroll
-        for (int c = 0; c < NT / 2; ++c) {
-            const int j = (ct0 / 2 + c) * 32 + l;
-            if (j >= n) continue;
-            const float ba = g.bias ? g.bias[j] : 0.f, bu = g.bias ? g.bias[n + j] : 0.f;
-            float dh[16];                                    // a tile's worth of loads before the first store
-            if constexpr (GATE == kGateBackward)
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    dh[v] = g.gated.dH[(size_t)min(row0 + 4 * half + 8 * (v / 4) + v % 4, g.M - 1) * n + j];
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int row = row0 + 4 * half + 8 * (v / 4) + v % 4;
-                if (row >= g.M) continue;
-                const float a = acc[c][v] + ba, u = acc[c + NT / 2][v] + bu;
-                float act, slope = 0.f;
-                gate_of<GATE == kGateBackward>(g.gated.gate, a, act, slope);
-                auto out = [&](float *at, float o) __attribute__((always_inline)) {
-                    if (g.act & kActStream) __builtin_nontemporal_store(o, at);
-                    else *at = o;
-                };
-                if constexpr (GATE == kGateBackward) {
-                    out(g.gated.D + (size_t)row * 2 * n + j, dh[v] * u * slope);
-                    out(g.gated.D + (size_t)row * 2 * n + n + j, dh[v] * act);
-                } else {
-                    out(g.gated.H + (size_t)row * n + j, act * u);
-                    if (g.gated.Z) {
-                        out(g.gated.Z + (size_t)row * 2 * n + j, a);
-                        out(g.gated.Z + (size_t)row * 2 * n + n + j, u);
-                    }
-                }
-            }
-        }
-    } else if (row0 + 32 <= g.M && (ct0 + NT) * 32 <= g.N && !(g.act & kActAccumulate)) {
+    if (row0 + 32 <= g.M && (ct0 + NT) * 32 <= g.N && !(g.act & kActAccumulate)) {
         // whole tiles, the columns of a row one after the other
         float bias[NT];
 #pragma unroll
@@ -611,7 +597,7 @@ gnn_status_t gemm_split_launch(int tb, int64_t M, int64_t N, int64_t K, const fl
         return launched ? launch_status() : GNN_ERR_UNSUPPORTED;
     }
     hipLaunchKernelGGL(split_weights_kernel, dim3((unsigned)(g.tiles_n * w), A2 ? 2 : 1), dim3(1024), 0, st, (int)N,
-                       (int)K, g.steps, g.B, g.B2, ws, ws2, range, range2, 0);
+                       (int)K, g.steps, g.B, g.B2, ws, ws2, range, range2);
     GNN_TRY(launch_status());
     const dim3 grid((unsigned)split_blocks(M, N));
     const size_t lds = (size_t)2 * w * kStepBytes + (a_bits ? (size_t)128 * g.bit_stride * sizeof(uint16_t) : 0);
@@ -619,45 +605,6 @@ gnn_status_t gemm_split_launch(int tb, int64_t M, int64_t N, int64_t K, const fl
                   : w == 2 ? (a_bits ? gemm_split_kernel<2, true, 0> : gemm_split_kernel<2, false, 0>)
                            : (a_bits ? gemm_split_kernel<4, true, 0> : gemm_split_kernel<4, false, 0>);
     hipLaunchKernelGGL(kernel, grid, dim3(256), lds, st, g);
-    return launch_status();
-}
-
-// Tiles of a block of the gated product, half of them of the gate: a row of X is split once per block.
-static int gated_tiles(int64_t half) { return half <= 32 ? 2 : 4; }
-
-size_t gemm_gated_workspace_bytes(int64_t half, int64_t K) {
-    const int64_t w = gated_tiles(half), tiles = ceil_div(half, 16 * w) * w;
-    return align_up((size_t)tiles * ceil_div(K, KB) * kStepBytes) + align_up((size_t)tiles * sizeof(Range));
-}
-
-bool gemm_gated_fits(int64_t M, int64_t half) {
-    return ceil_div(M, 128) * ceil_div(half, 16 * gated_tiles(half)) < ((int64_t)1 << 24) - 8;
-}
-
-// [A | U] = X W + b, X [M][K], W [K][2 half], K >= 4 and gemm_gated_fits; `out` says what becomes of it.
-gnn_status_t gemm_gated_launch(int64_t M, int64_t K, const float *X, const float *W, const float *bias, const Gated &out,
-                               void *workspace, hipStream_t st) {
-    Product g{};
-    const int64_t N = 2 * (int64_t)out.half;
-    const int w = gated_tiles(out.half);
-    g.M = (int)M; g.N = (int)N; g.K = (int)K;
-    g.steps = (int)ceil_div(K, KB);
-    g.A = X;
-    g.B = Operand{W, (long)N, 1};
-    g.bias = bias;
-    g.gated = out;
-    if ((size_t)M * N * sizeof(float) > kStreamBytes) g.act = kActStream;
-    g.tiles_m = (int)ceil_div(M, 128); g.tiles_n = (int)ceil_div(out.half, 16 * w);
-    char *ws = static_cast<char *>(workspace);
-    Range *range = reinterpret_cast<Range *>(ws + align_up((size_t)g.tiles_n * w * g.steps * kStepBytes));
-    g.parts = ws; g.range = range;
-    hipLaunchKernelGGL(split_weights_kernel, dim3((unsigned)(g.tiles_n * w)), dim3(1024), 0, st, (int)N, (int)K, g.steps, g.B,
-                       g.B, ws, ws, range, range, w);
-    GNN_TRY(launch_status());
-    const dim3 grid((unsigned)(8 * ceil_div((int64_t)g.tiles_m * g.tiles_n, 8)));
-    auto kernel = w == 2 ? (out.D ? gemm_split_kernel<2, false, 0, kGateBackward> : gemm_split_kernel<2, false, 0, kGateForward>)
-                         : (out.D ? gemm_split_kernel<4, false, 0, kGateBackward> : gemm_split_kernel<4, false, 0, kGateForward>);
-    hipLaunchKernelGGL(kernel, grid, dim3(256), (size_t)2 * w * kStepBytes, st, g);
     return launch_status();
 }
 
