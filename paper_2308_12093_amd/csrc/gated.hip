@@ -102,14 +102,16 @@ gated_few_kernel(int M, int K, const float *__restrict__ X, const float *__restr
 }
 
 // D from the [A | U] that forward has kept, and the largest magnitudes of its rows and columns.  A block takes `rows` rows
-// (kTopRows where these are wanted) and 64 VEC columns of each half, `lanes` lanes a row.
+// (top_rows where these are wanted) and 64 VEC columns of each half, `lanes` lanes a row; the `parts`
+// blocks of the same rows stand side by side.
 template <int VEC, int GATE>
 __global__ void __launch_bounds__(256)
-gated_gradient_kernel(long n, int k, int lanes, int rows, const float *__restrict__ Z, const float *__restrict__ dH,
+gated_gradient_kernel(long n, int k, int lanes, int rows, int parts, const float *__restrict__ Z, const float *__restrict__ dH,
                       float *__restrict__ D, Tops tops) {
     __shared__ unsigned across[256][2 * VEC];
-    const int gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes, c = (blockIdx.y * 64 + gl) * VEC;
-    const long r0 = (long)blockIdx.x * rows, r1 = min(n, r0 + rows);
+    const int gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
+    const int part = blockIdx.x % parts, block = blockIdx.x / parts, c = (part * 64 + gl) * VEC;
+    const long r0 = (long)block * rows, r1 = min(n, r0 + rows);
     unsigned top[2 * VEC];
 #pragma unroll
     for (int v = 0; v < 2 * VEC; ++v) top[v] = 0;
@@ -163,7 +165,7 @@ gated_gradient_kernel(long n, int k, int lanes, int rows, const float *__restric
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const long row = first + i * groups + grp;
-            if (gl == 0 && row < r1) tops.rows[(size_t)blockIdx.y * n + row] = most[i];
+            if (gl == 0 && row < r1) tops.rows[(size_t)part * n + row] = most[i];
         }
     }
     if (!tops.cols) return;
@@ -177,8 +179,8 @@ gated_gradient_kernel(long n, int k, int lanes, int rows, const float *__restric
                 top[v] = max(top[v], across[q * lanes + gl][v]);
                 top[VEC + v] = max(top[VEC + v], across[q * lanes + gl][VEC + v]);
             }
-            tops.cols[(size_t)blockIdx.x * 2 * k + c + v] = top[v];
-            tops.cols[(size_t)blockIdx.x * 2 * k + k + c + v] = top[VEC + v];
+            tops.cols[(size_t)block * 2 * k + c + v] = top[v];
+            tops.cols[(size_t)block * 2 * k + k + c + v] = top[VEC + v];
         }
 }
 
@@ -202,11 +204,11 @@ gnn_status_t gradient(int64_t n, int k, int gate, const float *Z, const float *d
     const bool vec = k % 4 == 0 && aligned16(Z) && aligned16(dH);
     int lanes = 1;
     while (lanes < 64 && lanes * (vec ? 4 : 1) < k) lanes <<= 1;
-    const int rows = tops.cols ? kTopRows : 4 * (256 / lanes);
+    const int rows = tops.cols ? top_rows(n) : 4 * (256 / lanes);
     *parts = (int)ceil_div(k, vec ? 256 : 64);
     auto kernel = vec ? BY_GATE(gate, gated_gradient_kernel, 4) : BY_GATE(gate, gated_gradient_kernel, 1);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(n, rows), (unsigned)*parts), dim3(256), 0, st, (long)n, k, lanes, rows, Z,
-                       dH, D, tops);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(n, rows) * *parts)), dim3(256), 0, st, (long)n, k, lanes, rows, *parts,
+                       Z, dH, D, tops);
     return launch_status();
 }
 
@@ -218,11 +220,11 @@ struct Backward {
     Backward(char *at, int64_t n, int64_t m, int64_t k) {
         Carver carve(at);
         x_rows = carve.take<unsigned>(n * ceil_div(m, 64));
-        x_cols = carve.take<unsigned>(ceil_div(n, kTopRows) * m);
-        d_rows = carve.take<unsigned>(n * ceil_div(k, 32));      // gated_row_parts(k), or those of `gradient`
-        d_cols = carve.take<unsigned>(ceil_div(n, kTopRows) * 2 * k);
+        x_cols = carve.take<unsigned>(top_blocks(n) * m);
+        d_rows = carve.take<unsigned>(n * ceil_div(k, 32));      // gated_row_parts(n, k), or those of `gradient`
+        d_cols = carve.take<unsigned>(top_blocks(n) * 2 * k);
         rest = carve.take<char>(0);
-        size_t most = gemm_half_workspace_bytes(2 * k, m);
+        size_t most = gemm_half_gated_workspace_bytes(k, m);
         for (size_t b : {gemm_half_workspace_bytes(m, 2 * k), gemm_half_tn_workspace_bytes(m, 2 * k, n)})
             if (b > most) most = b;
         bytes = carve.off + most;
@@ -232,14 +234,15 @@ struct Backward {
 }  // namespace
 
 bool gated_fits(bool backward, int64_t n, int64_t m, int64_t k) {
-    if (m > 1 << 21 || k > 1 << 21) return false;          // 64 columns a block in y
+    if (m > 1 << 21 || k > 1 << 21) return false;
     if (gated_few(n, m, k)) return ceil_div(n, 32) * ceil_div(k, 32) < (int64_t)1 << 24 && (!backward || gemm_fits(n, m, 2 * k));
-    return n <= 1 << 28 && gemm_half_fits(n, 2 * k) && (!backward || (gemm_half_fits(n, m) && gemm_half_tn_fits(m, 2 * k, n)));
+    // blocks of the kernels that look for the largest magnitudes, or form D: 32 rows and 64 columns
+    return ceil_div(n, 32) * ceil_div(m > k ? m : k, 64) < (int64_t)1 << 24 && gemm_half_fits(n, 2 * k) && (!backward || (gemm_half_fits(n, m) && gemm_half_tn_fits(m, 2 * k, n)));
 }
 
 // What n rows take, or fewer: a product of few rows needs less.
 size_t gated_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k) {
-    if (!backward) return gated_few(n, m, k) ? kAlign : row_tops_bytes(n, ceil_div(m, 64)) + gemm_half_workspace_bytes(2 * k, m);
+    if (!backward) return gated_few(n, m, k) ? kAlign : align_up((size_t)n * ceil_div(m, 64) * sizeof(unsigned)) + gemm_half_gated_workspace_bytes(k, m);
     const size_t d = align_up((size_t)n * 2 * k * sizeof(float));
     size_t most = 0;
     // the rows up to which the kernels for few rows run
@@ -298,7 +301,7 @@ gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X
         GNN_TRY(gradient(n, k, gate, Z, dH, d, of_d, &parts, st));
     } else {
         GNN_TRY(gemm_half_gated_launch(n, m, X, w.x_rows, W, b, g, of_d, w.rest, st));
-        parts = gated_row_parts(k);
+        parts = gated_row_parts(n, k);
     }
     if (dX) GNN_TRY(gemm_half_launch(n, m, 2 * (int64_t)k, d, w.d_rows, parts, W, dX, w.rest, st));
     return gemm_half_tn_launch(m, 2 * (int64_t)k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);

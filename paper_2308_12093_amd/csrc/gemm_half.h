@@ -7,11 +7,13 @@ namespace gnn {
 
 // Largest magnitudes, as the bits of floats (which order like them, infinities and NaN last).
 //   rows: [part][n], of a part of each row (the whole row: of its parts' largest)
-//   cols: [block of kTopRows rows][columns]
+//   cols: [block of top_rows(n) rows][columns]
 struct Tops {
     unsigned *rows, *cols;             // either may be NULL: not wanted
 };
-constexpr int kTopRows = 128;
+// Few rows in smaller blocks, so that there are enough of them for the chip.
+__host__ __device__ constexpr int top_rows(int64_t n) { return n < 32768 ? 32 : 128; }
+static inline int64_t top_blocks(int64_t n) { return ceil_div(n, top_rows(n)); }
 
 // columns of B as a product reads it: element (k, n) at k * sk + n * sn
 struct HalfOperand {
@@ -20,10 +22,9 @@ struct HalfOperand {
 };
 
 bool gemm_half_fits(int64_t M, int64_t N);
-// scratch of a product: the parts of B and their exponents
+// scratch of a product: the parts of B and their exponents; parts of the reduction
 size_t gemm_half_workspace_bytes(int64_t N, int64_t K);
-size_t row_tops_bytes(int64_t n, int64_t parts);
-size_t col_tops_bytes(int64_t n, int64_t columns);
+size_t gemm_half_gated_workspace_bytes(int64_t half, int64_t K);
 // largest magnitudes of X [n][m], top_parts(m, X) parts a row
 int top_parts(int64_t m, const float *X);
 gnn_status_t tops_launch(int64_t n, int m, const float *X, const Tops &tops, hipStream_t st);
@@ -31,9 +32,9 @@ gnn_status_t tops_launch(int64_t n, int m, const float *X, const Tops &tops, hip
 // C [M][N] = A [M][K] B^T, B [N][K]; row_tops: of A, `parts` of them.  K >= 4 and gemm_half_fits.
 gnn_status_t gemm_half_launch(int64_t M, int64_t N, int64_t K, const float *A, const unsigned *row_tops, int parts, const float *B,
                               float *C, void *workspace, hipStream_t st);
-// [A | U] = X W + bias, X [M][K] with the row_tops of tops_launch, W [K][2 half]; `out` says what becomes of it.  Backward fills `tops` of D: gated_row_parts(half)
-// parts a row.
-int gated_row_parts(int64_t half);
+// [A | U] = X W + bias, X [M][K] with the row_tops of tops_launch, W [K][2 half]; `out` says what becomes of it.  Backward fills
+// `tops` of D: gated_row_parts(n, half) parts a row.
+int gated_row_parts(int64_t n, int64_t half);
 gnn_status_t gemm_half_gated_launch(int64_t M, int64_t K, const float *X, const unsigned *row_tops, const float *W,
                                     const float *bias, const Gated &out, const Tops &tops, void *workspace, hipStream_t st);
 // C [M][N] = A^T B, A [K][M], B [K][N]; sums [N] = the column sums of B unless it is NULL; a_tops, b_tops: their columns'.

@@ -38,15 +38,35 @@ half_weights_kernel(int N, int K, int steps, HalfOperand b, int halves, char *__
     };
     if (t < 32) top[t] = 0;
     __syncthreads();
-    unsigned most = 0;
     float x[8];
-    for (int s = sub; s < steps; s += 8) {
-        fetch(s, x);
+    if constexpr (TB) {                                    // a column is a row in memory: a wavefront reads two of the 32
+        const int c = t / 64 * 2;
+        unsigned both[2] = {0, 0};
+#pragma unroll 4
+        for (int k = 4 * lane; k < K; k += 256)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+            for (int i = 0; i < 2; ++i) {
+                // the last four where fewer are left; a column past the end is the last one again
+                const float4u v = *reinterpret_cast<const float4u *>(b.p + min(k, K - 4) + (long)min((int)blockIdx.x * 32 + c + i, N - 1) * b.sn);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) both[i] = max(both[i], __float_as_uint(v[j]) & 0x7fffffffu);
+            }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) both[i] = max(both[i], (unsigned)__shfl_xor((int)both[i], d, 64));
+            if (lane == 0) top[c + i] = both[i];
+        }
+    } else {
+        unsigned most = 0;
+        for (int s = sub; s < steps; s += 8) {
+            fetch(s, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+        }
+        most = max(most, (unsigned)__shfl_xor((int)most, 32, 64));
+        if (half == 0) atomicMax(&top[l], most);
     }
-    most = max(most, (unsigned)__shfl_xor((int)most, 32, 64));
-    if (half == 0) atomicMax(&top[l], most);
     __syncthreads();
     const int e = exponent_of(top[l]);
     if (blockIdx.y == 0 && t < 32) exps[blockIdx.x * 32 + t] = e;
@@ -73,6 +93,7 @@ struct HalfProduct {
     const char *parts;
     const int *exps;
     float *C;
+    int splits, split_steps;           // kPlain: the reduction's parts, C [split][M][N] then
     const float *bias;
     bool stream;                       // outputs beyond the caches: non-temporal stores
     int tiles_m, tiles_n;
@@ -102,8 +123,10 @@ gemm_half_kernel(HalfProduct g) {
     __shared__ __align__(16) char rows[ALIGNED ? 4 * 4096 : 16];
     __shared__ int s_exp[4][32];
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t / 64), lane = t % 64, l = lane % 32, half = lane / 32;
-    const long tile = xcd_tile((long)g.tiles_m * g.tiles_n);
-    if (tile >= (long)g.tiles_m * g.tiles_n) return;
+    const long tiles = (long)g.tiles_m * g.tiles_n, id = xcd_tile(tiles * g.splits);
+    if (id >= tiles * g.splits) return;
+    const long tile = id % tiles;
+    const int split = (int)(id / tiles), step0 = split * g.split_steps, step1 = min(g.steps, step0 + g.split_steps);
     const int ct0 = (int)(tile % g.tiles_n) * NT, row0 = ((int)(tile / g.tiles_n) * 4 + wave) * 32;
     auto column = [&](int c) __attribute__((always_inline)) {       // of this lane in tile c; N where there is none
         if constexpr (OUT == kPlain) return min((ct0 + c) * 32 + l, g.N);
@@ -116,7 +139,7 @@ gemm_half_kernel(HalfProduct g) {
     // its last four floats instead (K >= 4) and put in place by `settle`, so no load stands behind a branch.
     floatx4 raw[4];
     auto load = [&](int step) __attribute__((always_inline)) {
-        const int k = min(step, g.steps - 1) * KB + 16 * half;     // the last step again after the last: no branch, no use
+        const int k = min(step, step1 - 1) * KB + 16 * half;      // the last step again after the last: no branch, no use
 #pragma unroll
         for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const float4u *>(g.A + ro + min(k + 4 * i, g.K - 4));
     };
@@ -160,9 +183,9 @@ gemm_half_kernel(HalfProduct g) {
             copy(base + step * KB, 4 * (mine[i] + min(piece, g.K - 4 - step * KB)), rows + wave * 4096 + i * 1024);
         }
     };
-    stage(0, even);
-    if constexpr (ALIGNED) stage_rows(0);
-    else load(0);
+    stage(step0, even);
+    if constexpr (ALIGNED) stage_rows(step0);
+    else load(step0);
     float scale, scale2;
     {
         unsigned top = 0;
@@ -194,13 +217,13 @@ gemm_half_kernel(HalfProduct g) {
         // read in the step before, is free
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (step + 1 < g.steps) stage(step + 1, next);
+        if (step + 1 < step1) stage(step + 1, next);
         if constexpr (ALIGNED) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 raw[i] = *reinterpret_cast<const floatx4 *>(rows + wave * 4096 + l * 128 + ((4 * half + i) ^ (l / 2 % 8)) * 16);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // read before the next step's rows overwrite them
-            if (step + 1 < g.steps) stage_rows(step + 1);
+            if (step + 1 < step1) stage_rows(step + 1);
         }
         half8 a[2][2];
         settle(step);
@@ -219,9 +242,9 @@ gemm_half_kernel(HalfProduct g) {
             multiply(acc[c], a, b);
         }
     };
-    for (int step = 0; step < g.steps; step += 2) {
+    for (int step = step0; step < step1; step += 2) {
         turn(step, even, odd);
-        if (step + 1 < g.steps) turn(step + 1, odd, even);
+        if (step + 1 < step1) turn(step + 1, odd, even);
     }
     float finite = 0.f;
 #pragma unroll
@@ -231,7 +254,7 @@ gemm_half_kernel(HalfProduct g) {
     const bool again = __any(finite != 0.f);               // 0 x (inf or NaN) is NaN
     if (again) {
         clear();
-        for (int step = 0; step < g.steps; ++step) {
+        for (int step = step0; step < step1; ++step) {
             load(step);
             settle(step);
             const int k0 = step * KB + 16 * half;
@@ -258,13 +281,14 @@ gemm_half_kernel(HalfProduct g) {
         return ldexpf(acc[c][v], -(ea + eb[c]));
     };
     if constexpr (OUT == kPlain) {
+        float *C = g.C + (size_t)split * g.M * g.N;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int row = row0 + 8 * (v / 4) + 4 * half + v % 4;
 #pragma unroll
             for (int c = 0; c < NT; ++c) {                 // the columns of a row one after the other
                 const int n = (ct0 + c) * 32 + l;
-                if (row < g.M && n < g.N) out(g.C + (size_t)row * g.N + n, value(c, v));
+                if (row < g.M && n < g.N) out(C + (size_t)row * g.N + n, value(c, v));
             }
         }
     } else {
@@ -319,7 +343,7 @@ gemm_half_kernel(HalfProduct g) {
             row_top[0] = max(row_top[0], (unsigned)__shfl_xor((int)row_top[0], 1, 64));
             const int v = l / 2, row = row0 + 4 * half + 8 * (v / 4) + v % 4;
             if (l % 2 == 0 && row < g.M) g.tops.rows[(size_t)(ct0 / NT) * g.M + row] = row_top[0];
-            unsigned *s = reinterpret_cast<unsigned *>(even);      // the block's rows: kTopRows of them
+            unsigned *s = reinterpret_cast<unsigned *>(even);      // of the wavefronts, or of the block
             __syncthreads();
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
@@ -327,22 +351,28 @@ gemm_half_kernel(HalfProduct g) {
                 if (half == 0) s[(wave * NT + c) * 32 + l] = col_top[c];
             }
             __syncthreads();
-            const int c = t / 32, j = (ct0 / 2 + c % (NT / 2)) * 32 + t % 32;
-            if (t < NT * 32 && j < k)
-                g.tops.cols[(size_t)(tile / g.tiles_n) * 2 * k + (c < NT / 2 ? 0 : k) + j] =
-                    max(max(s[t], s[NT * 32 + t]), max(s[2 * NT * 32 + t], s[3 * NT * 32 + t]));
+            const int each = top_rows(g.M) / 32;           // wavefronts to one
+            for (int i = t; i < 4 / each * NT * 32; i += 256) {
+                const int w = i / (NT * 32) * each, at = i % (NT * 32), c = at / 32, j = (ct0 / 2 + c % (NT / 2)) * 32 + at % 32;
+                const long block = tile / g.tiles_n * (4 / each) + w / each;
+                unsigned top = 0;
+                for (int q = w; q < w + each; ++q) top = max(top, s[q * NT * 32 + at]);
+                if (j < k && block * 32 * each < g.M) g.tops.cols[(size_t)block * 2 * k + (c < NT / 2 ? 0 : k) + j] = top;
+            }
         }
     }
 }
 
 // ---- largest magnitudes -----------------------------------------------------------------------------------
-// A block reads `rows` rows (kTopRows where the columns' are wanted) and 64 VEC columns, `lanes` lanes a row.
+// A block reads `rows` rows (top_rows where the columns' are wanted) and 64 VEC columns, `lanes` lanes a row; the `parts` blocks of
+// the same rows stand side by side.
 template <int VEC>
 __global__ void __launch_bounds__(256)
-tops_kernel(long n, int m, int lanes, int rows, const float *__restrict__ X, Tops tops) {
+tops_kernel(long n, int m, int lanes, int rows, int parts, const float *__restrict__ X, Tops tops) {
     __shared__ unsigned across[256][VEC];
-    const int gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes, c = (blockIdx.y * 64 + gl) * VEC;
-    const long r0 = (long)blockIdx.x * rows, r1 = min(n, r0 + rows);
+    const int gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
+    const int part = blockIdx.x % parts, block = blockIdx.x / parts, c = (part * 64 + gl) * VEC;
+    const long r0 = (long)block * rows, r1 = min(n, r0 + rows);
     unsigned top[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) top[v] = 0;
@@ -379,7 +409,7 @@ tops_kernel(long n, int m, int lanes, int rows, const float *__restrict__ X, Top
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const long row = first + i * groups + grp;
-            if (gl == 0 && row < r1) tops.rows[(size_t)blockIdx.y * n + row] = most[i];
+            if (gl == 0 && row < r1) tops.rows[(size_t)part * n + row] = most[i];
         }
     }
     if (!tops.cols) return;
@@ -390,50 +420,71 @@ tops_kernel(long n, int m, int lanes, int rows, const float *__restrict__ X, Top
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
             for (int k = 1; k < groups; ++k) top[v] = max(top[v], across[k * lanes + gl][v]);
-            tops.cols[(size_t)blockIdx.x * m + c + v] = top[v];
+            tops.cols[(size_t)block * m + c + v] = top[v];
         }
 }
 
-// 32-column tiles of a block
-int half_tiles(int64_t N) { return N <= 64 ? 2 : 4; }
-
-size_t half_parts_bytes(int64_t N, int64_t K) {
-    const int64_t w = half_tiles(N);
-    return align_up((size_t)(ceil_div(N, 32 * w) * w) * ceil_div(K, KB) * kTileBytes);
+// sum of the parts of a split reduction
+__global__ void __launch_bounds__(256)
+sum_splits_kernel(long count, int splits, const float *__restrict__ part, float *__restrict__ C) {
+    const long i = (long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= count) return;
+    float a = 0.f, b = 0.f;
+    int s = 0;
+    for (; s + 1 < splits; s += 2) {
+        a += part[s * count + i];
+        b += part[(s + 1) * count + i];
+    }
+    if (s < splits) a += part[s * count + i];
+    C[i] = a + b;
 }
 
+// 32-column tiles of a block: four (a row is split once per block), or two where the columns are few or the blocks
+int half_tiles(int64_t M, int64_t N) { return N <= 64 || ceil_div(M, 128) * ceil_div(N, 128) < 256 ? 2 : 4; }
+
+// Parts of a long reduction where its tiles leave most of the chip idle, four steps of it at least: 1024 x 512 x 2048 65 -> 14 us.
+constexpr int64_t kSplitBlocks = 512;
+int plain_splits(int64_t tiles, int64_t steps) {
+    if (tiles >= kSplitBlocks / 2) return 1;
+    int64_t splits = kSplitBlocks / tiles;
+    if (splits > steps / 4) splits = steps / 4;
+    return splits < 1 ? 1 : (int)splits;
+}
+constexpr size_t kSplitBytes = kSplitBlocks * 128 * 64 * sizeof(float);    // their tiles have two column tiles
+
+size_t half_parts_bytes(int64_t N, int64_t K) { return align_up((size_t)ceil_div(N, 128) * 4 * ceil_div(K, KB) * kTileBytes); }
+size_t half_exps_bytes(int64_t N) { return align_up((size_t)ceil_div(N, 128) * 128 * sizeof(int)); }
+
 void set_product(HalfProduct &g, int64_t M, int64_t N, int64_t K, void *workspace) {
-    const int w = half_tiles(N);
+    const int w = half_tiles(M, N);
     g.M = (int)M; g.N = (int)N; g.K = (int)K;
     g.steps = (int)ceil_div(K, KB);
     g.tiles_m = (int)ceil_div(M, 128); g.tiles_n = (int)ceil_div(N, 32 * w);
+    g.splits = 1;
+    g.split_steps = g.steps;
     g.parts = static_cast<char *>(workspace);
     g.exps = reinterpret_cast<int *>(static_cast<char *>(workspace) + half_parts_bytes(N, K));
 }
 
-gnn_status_t split_weights(const HalfProduct &g, int halves, hipStream_t st) {
-    const dim3 grid((unsigned)(g.tiles_n * half_tiles(g.N)), (unsigned)ceil_div(g.steps, kPartSteps));
+gnn_status_t split_weights(const HalfProduct &g, int tiles, int halves, hipStream_t st) {
+    const dim3 grid((unsigned)(g.tiles_n * tiles), (unsigned)ceil_div(g.steps, kPartSteps));
     auto kernel = g.B.sk == 1 ? half_weights_kernel<true> : half_weights_kernel<false>;
     hipLaunchKernelGGL(kernel, grid, dim3(1024), 0, st, g.N, g.K, g.steps, g.B, halves, const_cast<char *>(g.parts),
                        const_cast<int *>(g.exps));
     return launch_status();
 }
 
-dim3 product_grid(const HalfProduct &g) { return dim3((unsigned)(8 * ceil_div((int64_t)g.tiles_m * g.tiles_n, 8))); }
+dim3 product_grid(const HalfProduct &g) { return dim3((unsigned)(8 * ceil_div((int64_t)g.tiles_m * g.tiles_n * g.splits, 8))); }
 
 }  // namespace
 
 // a grid has less than 2^32 threads
 bool gemm_half_fits(int64_t M, int64_t N) {
-    return N <= INT32_MAX / 4 && M <= INT32_MAX - 256 && ceil_div(M, 128) * ceil_div(N, 32 * half_tiles(N)) < ((int64_t)1 << 24) - 8;
+    return N <= INT32_MAX / 4 && M <= INT32_MAX - 256 && ceil_div(M, 128) * ceil_div(N, 64) < ((int64_t)1 << 24) - 8;
 }
 
-size_t gemm_half_workspace_bytes(int64_t N, int64_t K) {
-    return half_parts_bytes(N, K) + align_up((size_t)(ceil_div(N, 32) + 3) * 32 * sizeof(int));
-}
-
-size_t row_tops_bytes(int64_t n, int64_t parts) { return align_up((size_t)n * parts * sizeof(unsigned)); }
-size_t col_tops_bytes(int64_t n, int64_t columns) { return align_up((size_t)ceil_div(n, kTopRows) * columns * sizeof(unsigned)); }
+size_t gemm_half_workspace_bytes(int64_t N, int64_t K) { return half_parts_bytes(N, K) + half_exps_bytes(N) + kSplitBytes; }
+size_t gemm_half_gated_workspace_bytes(int64_t half, int64_t K) { return half_parts_bytes(2 * half, K) + half_exps_bytes(2 * half); }
 
 int top_parts(int64_t m, const float *X) { return (int)ceil_div(m, m % 4 == 0 && aligned16(X) ? 256 : 64); }
 
@@ -441,9 +492,10 @@ gnn_status_t tops_launch(int64_t n, int m, const float *X, const Tops &tops, hip
     const bool vec = m % 4 == 0 && aligned16(X);
     int lanes = 1;
     while (lanes < 64 && lanes * (vec ? 4 : 1) < m) lanes <<= 1;
-    const int rows = tops.cols ? kTopRows : 8 * (256 / lanes);
-    const dim3 grid((unsigned)ceil_div(n, rows), (unsigned)top_parts(m, X));
-    hipLaunchKernelGGL(vec ? tops_kernel<4> : tops_kernel<1>, grid, dim3(256), 0, st, (long)n, m, lanes, rows, X, tops);
+    const int rows = tops.cols ? top_rows(n) : 8 * (256 / lanes);
+    const int parts = top_parts(m, X);
+    hipLaunchKernelGGL(vec ? tops_kernel<4> : tops_kernel<1>, dim3((unsigned)(ceil_div(n, rows) * parts)), dim3(256), 0, st, (long)n,
+                       m, lanes, rows, parts, X, tops);
     return launch_status();
 }
 
@@ -455,21 +507,30 @@ gnn_status_t gemm_half_launch(int64_t M, int64_t N, int64_t K, const float *A, c
     g.B = HalfOperand{B, 1, (long)K};
     g.C = C;
     g.stream = (size_t)M * N * sizeof(float) > kStreamBytes;
-    GNN_TRY(split_weights(g, 0, st));
+    const int w = half_tiles(M, N), splits = plain_splits((int64_t)g.tiles_m * g.tiles_n, g.steps);
+    if (splits > 1) {
+        g.split_steps = (int)ceil_div(g.steps, splits);
+        g.splits = (int)ceil_div(g.steps, g.split_steps);
+        g.C = reinterpret_cast<float *>(static_cast<char *>(workspace) + half_parts_bytes(N, K) + half_exps_bytes(N));
+    }
+    GNN_TRY(split_weights(g, w, 0, st));
     const bool aligned = K % 4 == 0 && K < 1 << 24 && aligned16(A);
-    auto kernel = half_tiles(N) == 2 ? (aligned ? gemm_half_kernel<2, kPlain, true, 0> : gemm_half_kernel<2, kPlain, false, 0>)
+    auto kernel = w == 2 ? (aligned ? gemm_half_kernel<2, kPlain, true, 0> : gemm_half_kernel<2, kPlain, false, 0>)
                                      : (aligned ? gemm_half_kernel<4, kPlain, true, 0> : gemm_half_kernel<4, kPlain, false, 0>);
     hipLaunchKernelGGL(kernel, product_grid(g), dim3(256), 0, st, g);
+    GNN_TRY(launch_status());
+    if (g.splits == 1) return GNN_OK;
+    hipLaunchKernelGGL(sum_splits_kernel, dim3((unsigned)ceil_div(M * N, 256)), dim3(256), 0, st, (long)(M * N), g.splits, g.C, C);
     return launch_status();
 }
 
-int gated_row_parts(int64_t half) { return (int)ceil_div(2 * half, 32 * half_tiles(2 * half)); }
+int gated_row_parts(int64_t n, int64_t half) { return (int)ceil_div(half, 16 * half_tiles(n, 2 * half)); }
 
 gnn_status_t gemm_half_gated_launch(int64_t M, int64_t K, const float *X, const unsigned *row_tops, const float *W,
                                     const float *bias, const Gated &out, const Tops &tops, void *workspace, hipStream_t st) {
     HalfProduct g{};
     const int64_t N = 2 * (int64_t)out.half;
-    const int w = half_tiles(N);
+    const int w = half_tiles(M, N);
     set_product(g, M, N, K, workspace);
     g.tiles_n = (int)ceil_div(out.half, 16 * w);
     g.A = X; g.row_tops = row_tops; g.top_parts = top_parts(K, X);
@@ -478,7 +539,7 @@ gnn_status_t gemm_half_gated_launch(int64_t M, int64_t K, const float *X, const 
     g.gated = out;
     g.tops = tops;
     g.stream = !out.D && (size_t)M * N * sizeof(float) > kStreamBytes;      // D is read next
-    GNN_TRY(split_weights(g, w, st));
+    GNN_TRY(split_weights(g, w, w, st));
     const bool aligned = K % 4 == 0 && K < 1 << 24 && aligned16(X), back = out.D != nullptr;
     const dim3 grid = product_grid(g);
 #define GATED_CASE(NT_, ALIGNED_, GATE_)                                                                                    \

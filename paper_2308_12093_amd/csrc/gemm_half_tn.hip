@@ -6,11 +6,12 @@ namespace {
 
 using namespace half_parts;
 
+constexpr int64_t kChunkStep = 128;
 constexpr int64_t kMostRows = 4096;    // of a chunk, whose sums are in float; the chunks are added in double
 
 struct TnProduct {
     int M, N;
-    long K, chunk;                     // chunk: a multiple of kTopRows
+    long K, chunk;                     // chunk: a multiple of kChunkStep
     const float *A, *B;
     const unsigned *a_tops, *b_tops;
     int tiles_m, tiles_n, splits;
@@ -44,7 +45,8 @@ gemm_half_tn_kernel(TnProduct g) {
         const bool a = i < 64 * TM;
         const unsigned *tops = a ? g.a_tops + of_a(i) : g.b_tops + of_b(i - 64 * TM);
         unsigned top = 0;
-        for (long b = k0 / kTopRows; b * kTopRows < k1; ++b) top = max(top, tops[b * (a ? g.M : g.N)]);
+        const int each = top_rows(g.K);
+        for (long b = k0 / each; b * each < k1; ++b) top = max(top, tops[b * (a ? g.M : g.N)]);
         s_exp[i] = exponent_of(top);
     }
     // fragment i of the wavefront: instruction (wave & 1) of 32-column tile wave / 2 + 2 i; tiles of A first
@@ -235,33 +237,41 @@ gemm_half_tn_kernel(TnProduct g) {
     }
 }
 
-// out[i] = sum over the chunks, in double and in a fixed order; the outputs of C, then the column sums.  32 outputs a block, eight
-// lanes each.
+// out[i] = sum over the chunks, in double and in a fixed order; the outputs of C, then the column sums.  32 VEC outputs a block,
+// eight lanes each.
+template <int VEC>
 __global__ void __launch_bounds__(256)
 tn_reduce_kernel(long count, int splits, const float *__restrict__ part, float *__restrict__ C, long count2,
                  const float *__restrict__ part2, float *__restrict__ sums) {
-    __shared__ double red[8][33];
+    __shared__ double red[8][32][VEC];
     const int o = threadIdx.x % 32, sl = threadIdx.x / 32;
-    const long blocks = (count + 31) / 32;
+    const long blocks = (count + 32 * VEC - 1) / (32 * VEC);
     const bool second = blockIdx.x >= blocks;
-    const long i = (second ? blockIdx.x - blocks : blockIdx.x) * 32L + o, n = second ? count2 : count;
+    const long i = ((second ? blockIdx.x - blocks : blockIdx.x) * 32L + o) * VEC, n = second ? count2 : count;
     const float *p = second ? part2 : part;
-    double a0 = 0.0, a1 = 0.0;
-    if (i < n) {
-        int s = sl;
-        for (; s + 8 < splits; s += 16) {
-            a0 += p[s * n + i];
-            a1 += p[(s + 8) * n + i];
+    double a[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) a[v] = 0.0;
+    if (i < n)
+        for (int s = sl; s < splits; s += 8) {
+            if constexpr (VEC == 4) {
+                const floatx4 x = *reinterpret_cast<const floatx4 *>(p + s * n + i);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) a[v] += x[v];
+            } else {
+                a[0] += p[s * n + i];
+            }
         }
-        if (s < splits) a0 += p[s * n + i];
-    }
-    red[sl][o] = a0 + a1;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) red[sl][o][v] = a[v];
     __syncthreads();
-    if (sl == 0 && i < n) {
-        double t = 0.0;
-        for (int k = 0; k < 8; ++k) t += red[k][o];
-        (second ? sums : C)[i] = (float)t;
-    }
+    if (sl == 0 && i < n)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            double t = 0.0;
+            for (int k = 0; k < 8; ++k) t += red[k][o][v];
+            (second ? sums : C)[i + v] = (float)t;
+        }
 }
 
 int tn_tile(int64_t extent) { return extent <= 64 ? 1 : 2; }
@@ -269,8 +279,8 @@ int tn_tile(int64_t extent) { return extent <= 64 ? 1 : 2; }
 // Chunks: enough blocks for the chip, at least four steps each, at most kMostRows indices.
 int64_t tn_chunks(int64_t M, int64_t N, int64_t K) {
     const int64_t tiles = ceil_div(M, 64 * tn_tile(M)) * ceil_div(N, 64 * tn_tile(N));
-    int64_t chunks = ceil_div(768, tiles);
-    const int64_t most = ceil_div(K, kTopRows), least = ceil_div(K, kMostRows);
+    int64_t chunks = ceil_div(512, tiles);
+    const int64_t most = ceil_div(K, kChunkStep), least = ceil_div(K, kMostRows);
     if (chunks > most) chunks = most;
     if (chunks < least) chunks = least;
     return chunks < 1 ? 1 : chunks;
@@ -296,7 +306,7 @@ gnn_status_t gemm_half_tn_launch(int64_t M, int64_t N, int64_t K, const float *A
     const int tm = tn_tile(M), tn = tn_tile(N);
     const int64_t chunks = tn_chunks(M, N, K);
     g.M = (int)M; g.N = (int)N; g.K = K;
-    g.chunk = ceil_div(ceil_div(K, chunks), kTopRows) * kTopRows;
+    g.chunk = ceil_div(ceil_div(K, chunks), kChunkStep) * kChunkStep;
     g.splits = (int)ceil_div(K, g.chunk);
     g.A = A; g.B = B; g.a_tops = a_tops; g.b_tops = b_tops;
     g.tiles_m = (int)ceil_div(M, 64 * tm); g.tiles_n = (int)ceil_div(N, 64 * tn);
@@ -310,8 +320,10 @@ gnn_status_t gemm_half_tn_launch(int64_t M, int64_t N, int64_t K, const float *A
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, g);
     GNN_TRY(launch_status());
     const long count = (long)M * N, count2 = sums ? N : 0;
-    hipLaunchKernelGGL(tn_reduce_kernel, dim3((unsigned)(ceil_div(count, 32) + ceil_div(count2, 32))), dim3(256), 0, st, count,
-                       g.splits, g.part, C, count2, part2, sums);
+    const int vec = N % 4 == 0 ? 4 : 1;                    // the chunks lie N and M N floats apart in an aligned workspace
+    hipLaunchKernelGGL(vec == 4 ? tn_reduce_kernel<4> : tn_reduce_kernel<1>,
+                       dim3((unsigned)(ceil_div(count, 32 * vec) + ceil_div(count2, 32 * vec))), dim3(256), 0, st, count, g.splits,
+                       g.part, C, count2, part2, sums);
     return launch_status();
 }
 
