@@ -8,6 +8,7 @@ namespace {
 typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
 
 typedef float floatx2u __attribute__((ext_vector_type(2), aligned(4)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float4 load4(const float *row, int c, int f) {
     if (c + 4 <= f) {
@@ -33,15 +34,40 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-__device__ __forceinline__ float activation(float z, int act) {
-    if (act == kActRelu) return fmaxf(z, 0.f);
-    if (act == kActElu) return z > 0.f ? z : expm1f(z);
+// exp(x) for x <= 0: off by at most (1 + |x|) units in the last place, one instruction and a multiplication
+__device__ __forceinline__ float exp_down(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+
+// exp(x) - 1 for x <= 0: the series up to x^7 / 7! near zero (what it leaves out is below 2^-25 of the result), the difference
+// where it keeps its digits
+__device__ __forceinline__ float expm1_down(float x) {
+    const float p = fmaf(fmaf(fmaf(fmaf(fmaf(1.f / 5040, x, 1.f / 720), x, 1.f / 120), x, 1.f / 24), x, 1.f / 6), x, 0.5f);
+    return x > -0.35f ? fmaf(x * x, p, x) : exp_down(x) - 1.f;
+}
+
+template <int ACT>
+__device__ __forceinline__ float activation(float z) {
+    if constexpr (ACT == kActRelu) return fmaxf(z, 0.f);
+    if constexpr (ACT == kActElu) return z > 0.f ? z : expm1_down(z);
     return z;
 }
-__device__ __forceinline__ float slope(float z, int act) {
-    if (act == kActRelu) return z > 0.f ? 1.f : 0.f;
-    if (act == kActElu) return z > 0.f ? 1.f : expf(z);
+template <int ACT>
+__device__ __forceinline__ float slope(float z) {
+    if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : 0.f;
+    if constexpr (ACT == kActElu) return exp_down(fminf(z, 0.f));
     return 1.f;
+}
+__device__ __forceinline__ float activation(float z, int act) {
+    return act == kActRelu ? activation<kActRelu>(z) : act == kActElu ? activation<kActElu>(z) : z;
+}
+__device__ __forceinline__ float slope(float z, int act) {
+    return act == kActRelu ? slope<kActRelu>(z) : act == kActElu ? slope<kActElu>(z) : 1.f;
+}
+
+// 1 / sqrt(x): the instruction's, and a Newton step (an IEEE division and root take thirty instructions, for each lane of a row)
+__device__ __forceinline__ float inverse_root(float x) {
+    const float y = __builtin_amdgcn_rsqf(x);
+    const float r = fmaf(fmaf(-0.5f * x * y, y, 0.5f), y, y);
+    return x > 0x1p-100f && x < 0x1p100f ? r : y;          // x y y keeps its range there; infinities and NaN as they are
 }
 
 __global__ void __launch_bounds__(256)
@@ -96,31 +122,42 @@ __device__ __forceinline__ void row_sums(float (&v)[U], int lanes, float *red) {
     }
 }
 
-template <bool ALIGNED>
+// How rows are read and written.  kStreamed: aligned rows of arrays beyond the caches, past them (2^20 x 256 backward 645 -> 600
+// us, 2^18 x 512 around a residual connection 511 -> 488 and forward 398 -> 379; arrays that the caches hold would lose
+// what the next kernel finds there).
+enum { kAnyRow, kAlignedRow, kStreamed };
+
+template <int MEM>
 __device__ __forceinline__ float4 read4(const float *row, int c, int f, bool valid) {
     if (!valid || c >= f) return make_float4(0.f, 0.f, 0.f, 0.f);
-    if constexpr (ALIGNED) return *reinterpret_cast<const float4 *>(row + c);
-    else return load4(row, c, f);
+    if constexpr (MEM == kAnyRow) return load4(row, c, f);
+    else if constexpr (MEM == kAlignedRow) return *reinterpret_cast<const float4 *>(row + c);
+    else {
+        const floatx4 v = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(row + c));
+        return make_float4(v.x, v.y, v.z, v.w);
+    }
 }
-template <bool ALIGNED>
+template <int MEM>
 __device__ __forceinline__ void write4(float *row, int c, int f, float4 v) {
     if (c >= f) return;
-    if constexpr (ALIGNED) *reinterpret_cast<float4 *>(row + c) = v;
-    else store4(row, c, f, v);
+    if constexpr (MEM == kAnyRow) store4(row, c, f, v);
+    else if constexpr (MEM == kAlignedRow) *reinterpret_cast<float4 *>(row + c) = v;
+    else __builtin_nontemporal_store(floatx4{v.x, v.y, v.z, v.w}, reinterpret_cast<floatx4 *>(row + c));
 }
 
-template <int R, int U, bool ADD, bool ALIGNED, bool WIDE>
+template <int R, int U, int ACT, bool ADD, int MEM, bool WIDE>
 __global__ void __launch_bounds__(256)
 norm_forward_kernel(Norm a) {
     __shared__ float red[4 * U];
     const DropoutWords words(a.drop);
+    const float inv_f = 1.f / (float)a.f;
     const int f = a.f, lanes = a.lanes, gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
     float4 ga[R], be[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int c = 4 * (r * lanes + gl);
-        ga[r] = a.gamma ? read4<ALIGNED>(a.gamma, c, f, true) : make_float4(1.f, 1.f, 1.f, 1.f);
-        be[r] = a.beta ? read4<ALIGNED>(a.beta, c, f, true) : make_float4(0.f, 0.f, 0.f, 0.f);
+        ga[r] = a.gamma ? read4<MEM == kStreamed ? kAlignedRow : MEM>(a.gamma, c, f, true) : make_float4(1.f, 1.f, 1.f, 1.f);
+        be[r] = a.beta ? read4<MEM == kStreamed ? kAlignedRow : MEM>(a.beta, c, f, true) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     for (long base = (long)blockIdx.x * groups * U; base < a.n; base += (long)gridDim.x * groups * U) {
         float4 x[U][R];
@@ -130,7 +167,7 @@ norm_forward_kernel(Norm a) {
         for (int u = 0; u < U; ++u) {
             row[u] = base + u * groups + grp;
 #pragma unroll
-            for (int r = 0; r < R; ++r) x[u][r] = read4<ALIGNED>(a.X + row[u] * f, 4 * (r * lanes + gl), f, row[u] < a.n);
+            for (int r = 0; r < R; ++r) x[u][r] = read4<MEM>(a.X + row[u] * f, 4 * (r * lanes + gl), f, row[u] < a.n);
         }
         if constexpr (ADD) {
 #pragma unroll
@@ -138,11 +175,11 @@ norm_forward_kernel(Norm a) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const int g = r * lanes + gl;
-                    const float4 o = read4<ALIGNED>(a.R + row[u] * f, 4 * g, f, row[u] < a.n);
+                    const float4 o = read4<MEM>(a.R + row[u] * f, 4 * g, f, row[u] < a.n);
                     float4 v = words.apply(x[u][r], (uint32_t)row[u], g);
                     v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
                     x[u][r] = v;
-                    if (row[u] < a.n) write4<ALIGNED>(a.H + row[u] * f, 4 * g, f, v);
+                    if (row[u] < a.n) write4<MEM>(a.H + row[u] * f, 4 * g, f, v);
                 }
         }
 #pragma unroll
@@ -154,7 +191,7 @@ norm_forward_kernel(Norm a) {
         row_sums<U, WIDE>(mean, lanes, red);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            mean[u] /= (float)f;
+            mean[u] *= inv_f;
             rstd[u] = 0.f;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -169,7 +206,7 @@ norm_forward_kernel(Norm a) {
         row_sums<U, WIDE>(rstd, lanes, red);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            rstd[u] = 1.f / sqrtf(rstd[u] / (float)f + a.eps);
+            rstd[u] = inverse_root(fmaf(rstd[u], inv_f, a.eps));
             if (row[u] >= a.n) continue;
             if (gl == 0) *reinterpret_cast<floatx2u *>(a.stat + 2 * row[u]) = floatx2u{mean[u], rstd[u]};
 #pragma unroll
@@ -179,10 +216,10 @@ norm_forward_kernel(Norm a) {
                 float4 y = make_float4(fmaf(d.x * rstd[u], ga[r].x, be[r].x), fmaf(d.y * rstd[u], ga[r].y, be[r].y),
                                        fmaf(d.z * rstd[u], ga[r].z, be[r].z), fmaf(d.w * rstd[u], ga[r].w, be[r].w));
                 if constexpr (!ADD) {
-                    y = make_float4(activation(y.x, a.act), activation(y.y, a.act), activation(y.z, a.act), activation(y.w, a.act));
+                    y = make_float4(activation<ACT>(y.x), activation<ACT>(y.y), activation<ACT>(y.z), activation<ACT>(y.w));
                     y = words.apply(y, (uint32_t)row[u], g);
                 }
-                write4<ALIGNED>(a.Y + row[u] * f, 4 * g, f, y);
+                write4<MEM>(a.Y + row[u] * f, 4 * g, f, y);
             }
         }
     }
@@ -199,20 +236,21 @@ struct NormBack {
 };
 
 // ADD: dR = dH + the norm's gradient, dX = dropout(dR); without: dX = the norm's gradient of act'(dropout(dY)).
-template <int R, int U, bool ADD, bool ALIGNED, bool WIDE>
+template <int R, int U, int ACT, bool ADD, int MEM, bool WIDE>
 __global__ void __launch_bounds__(256)
 norm_backward_kernel(NormBack a) {
     __shared__ float red[8 * U];
     __shared__ float4 across[256];
     const DropoutWords words(a.drop);
+    const float inv_f = 1.f / (float)a.f;
     const int f = a.f, lanes = a.lanes, gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
     const bool write = ADD || a.dX;                        // uniform
     float4 ga[R], be[R], dg[R], db[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int c = 4 * (r * lanes + gl);
-        ga[r] = a.gamma ? read4<ALIGNED>(a.gamma, c, f, true) : make_float4(1.f, 1.f, 1.f, 1.f);
-        be[r] = a.beta ? read4<ALIGNED>(a.beta, c, f, true) : make_float4(0.f, 0.f, 0.f, 0.f);
+        ga[r] = a.gamma ? read4<MEM == kStreamed ? kAlignedRow : MEM>(a.gamma, c, f, true) : make_float4(1.f, 1.f, 1.f, 1.f);
+        be[r] = a.beta ? read4<MEM == kStreamed ? kAlignedRow : MEM>(a.beta, c, f, true) : make_float4(0.f, 0.f, 0.f, 0.f);
         dg[r] = db[r] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     for (long base = (long)blockIdx.x * groups * U; base < a.n; base += (long)gridDim.x * groups * U) {
@@ -226,8 +264,8 @@ norm_backward_kernel(NormBack a) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int c = 4 * (r * lanes + gl);
-                x[u][r] = read4<ALIGNED>(a.X + row[u] * f, c, f, valid);
-                d[u][r] = read4<ALIGNED>(a.dY + row[u] * f, c, f, valid);
+                x[u][r] = read4<MEM>(a.X + row[u] * f, c, f, valid);
+                d[u][r] = read4<MEM>(a.dY + row[u] * f, c, f, valid);
             }
         }
 #pragma unroll
@@ -245,9 +283,9 @@ norm_backward_kernel(NormBack a) {
                                 c + 2 < f ? (v.z - st.x) * st.y : 0.f, c + 3 < f ? (v.w - st.x) * st.y : 0.f);
                 if constexpr (!ADD) {
                     e = words.apply(e, (uint32_t)row[u], g);
-                    if (a.act != kActNone)
-                        e = make_float4(e.x * slope(fmaf(v.x, ga[r].x, be[r].x), a.act), e.y * slope(fmaf(v.y, ga[r].y, be[r].y), a.act),
-                                        e.z * slope(fmaf(v.z, ga[r].z, be[r].z), a.act), e.w * slope(fmaf(v.w, ga[r].w, be[r].w), a.act));
+                    if constexpr (ACT != kActNone)
+                        e = make_float4(e.x * slope<ACT>(fmaf(v.x, ga[r].x, be[r].x)), e.y * slope<ACT>(fmaf(v.y, ga[r].y, be[r].y)),
+                                        e.z * slope<ACT>(fmaf(v.z, ga[r].z, be[r].z)), e.w * slope<ACT>(fmaf(v.w, ga[r].w, be[r].w)));
                 }
                 dg[r] = make_float4(fmaf(e.x, v.x, dg[r].x), fmaf(e.y, v.y, dg[r].y), fmaf(e.z, v.z, dg[r].z), fmaf(e.w, v.w, dg[r].w));
                 db[r] = make_float4(db[r].x + e.x, db[r].y + e.y, db[r].z + e.z, db[r].w + e.w);
@@ -261,7 +299,7 @@ norm_backward_kernel(NormBack a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (row[u] >= a.n) continue;
-            const float s1 = s[2 * u] / (float)f, s2 = s[2 * u + 1] / (float)f;
+            const float s1 = s[2 * u] * inv_f, s2 = s[2 * u + 1] * inv_f;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int g = r * lanes + gl;
@@ -270,14 +308,14 @@ norm_backward_kernel(NormBack a) {
                                        rstd[u] * ((e.z - s1) - v.z * s2), rstd[u] * ((e.w - s1) - v.w * s2));
                 if constexpr (ADD) {
                     if (a.dH) {
-                        const float4 h = read4<ALIGNED>(a.dH + row[u] * f, 4 * g, f, true);
+                        const float4 h = read4<MEM>(a.dH + row[u] * f, 4 * g, f, true);
                         o = make_float4(o.x + h.x, o.y + h.y, o.z + h.z, o.w + h.w);
                     }
-                    write4<ALIGNED>(a.dR + row[u] * f, 4 * g, f, o);
+                    write4<MEM>(a.dR + row[u] * f, 4 * g, f, o);
                     if (!a.dX) continue;
                     o = words.apply(o, (uint32_t)row[u], g);
                 }
-                write4<ALIGNED>(a.dX + row[u] * f, 4 * g, f, o);
+                write4<MEM>(a.dX + row[u] * f, 4 * g, f, o);
             }
         }
     }
@@ -347,7 +385,7 @@ norm_forward_long_kernel(Norm a) {
     float square = 0.f;
     for (int c = 4 * threadIdx.x; c < f; c += 1024)        // a thread reads back what it has written itself
         for (int j = 0; j < 4 && c + j < f; ++j) square = fmaf(x[c + j] - mean, x[c + j] - mean, square);
-    const float rstd = 1.f / sqrtf(block_sum(square, red) / (float)f + a.eps);
+    const float rstd = inverse_root(block_sum(square, red) / (float)f + a.eps);
     if (threadIdx.x == 0) { a.stat[2 * row] = mean; a.stat[2 * row + 1] = rstd; }
     for (int c = 4 * threadIdx.x; c < f; c += 1024) {
         float z[4] = {0.f, 0.f, 0.f, 0.f};
@@ -478,7 +516,7 @@ int64_t norm_blocks(int64_t n, int f) {
     }
     const Shape s = norm_shape(f);
     const int64_t groups = 256 / s.lanes;
-    const int64_t most = ceil_div(n, groups * 4);          // four rows a group at least
+    const int64_t most = ceil_div(n, groups * 2);          // two rows a group at least
     int64_t blocks = ceil_div(n, groups * kNormChain);
     if (blocks < 1024) blocks = most < 1024 ? most : 1024;
     return blocks;
@@ -501,11 +539,26 @@ gnn_status_t dropout_launch(int n, int f, const float *X, const float *R, const 
     return launch_status();
 }
 
-#define NORM_CASE(KERNEL_, ADD_, PER_, U_, WIDE_)                                                            \
-    if (shape.per == PER_ && shape.wide == WIDE_ && add == ADD_) {                                               \
-        if (aligned) hipLaunchKernelGGL((KERNEL_<PER_, U_, ADD_, true, WIDE_>), grid, dim3(256), 0, st, a);      \
-        else hipLaunchKernelGGL((KERNEL_<PER_, U_, ADD_, false, WIDE_>), grid, dim3(256), 0, st, a);             \
+// U_: rows at a time, and of streamed arrays, which take more loads under way
+#define NORM_CASE(KERNEL_, PER_, U_, STREAM_U_, WIDE_)                                                       \
+    if (shape.per == PER_ && shape.wide == WIDE_) {                                                              \
+        if (mem == kStreamed) NORM_ACT(KERNEL_, PER_, STREAM_U_, kStreamed, WIDE_)                               \
+        else if (mem == kAlignedRow) NORM_ACT(KERNEL_, PER_, U_, kAlignedRow, WIDE_)                             \
+        else NORM_ACT(KERNEL_, PER_, U_, kAnyRow, WIDE_)                                                         \
     }
+#define NORM_ACT(KERNEL_, PER_, U_, MEM_, WIDE_)                                                                 \
+    {                                                                                                            \
+        if (add) NORM_LAUNCH(KERNEL_, PER_, U_, kActNone, true, MEM_, WIDE_);                                    \
+        else if (act == kActRelu) NORM_LAUNCH(KERNEL_, PER_, U_, kActRelu, false, MEM_, WIDE_);                  \
+        else if (act == kActElu) NORM_LAUNCH(KERNEL_, PER_, U_, kActElu, false, MEM_, WIDE_);                    \
+        else NORM_LAUNCH(KERNEL_, PER_, U_, kActNone, false, MEM_, WIDE_);                                       \
+    }
+#define NORM_LAUNCH(KERNEL_, PER_, U_, ACT_, ADD_, MEM_, WIDE_) \
+    hipLaunchKernelGGL((KERNEL_<PER_, U_, ACT_, ADD_, MEM_, WIDE_>), grid, dim3(256), 0, st, a)
+
+static int norm_memory(int64_t n, int f, bool aligned) {
+    return !aligned ? kAnyRow : (size_t)n * f * sizeof(float) > kStreamBytes ? kStreamed : kAlignedRow;
+}
 
 gnn_status_t norm_forward_launch(int n, int f, const float *X, const float *R, const float *gamma, const float *beta,
                                  float eps, int act, const Dropout &drop, float *H, float *Y, float *stat, hipStream_t st) {
@@ -520,14 +573,14 @@ gnn_status_t norm_forward_launch(int n, int f, const float *X, const float *R, c
     const bool add = R != nullptr;
     const bool aligned = f % 4 == 0 && aligned16(X) && aligned16(Y) && aligned16(gamma) && aligned16(beta) &&
                          (!add || (aligned16(R) && aligned16(H)));
-    const int u = shape.wide || shape.per == 4 ? 1 : shape.per == 2 ? 2 : 4;
+    const int u = shape.wide || shape.per == 4 ? 1 : shape.per == 2 ? 2 : 4, mem = norm_memory(n, f, aligned);
     int64_t blocks = ceil_div(n, 256 / shape.lanes * u);
     if (blocks > 2048) blocks = 2048;
     const dim3 grid((unsigned)blocks);
-    NORM_CASE(norm_forward_kernel, false, 1, 4, false) NORM_CASE(norm_forward_kernel, false, 2, 2, false)
-    NORM_CASE(norm_forward_kernel, false, 4, 1, false) NORM_CASE(norm_forward_kernel, false, 4, 1, true)
-    NORM_CASE(norm_forward_kernel, true, 1, 4, false) NORM_CASE(norm_forward_kernel, true, 2, 2, false)
-    NORM_CASE(norm_forward_kernel, true, 4, 1, false) NORM_CASE(norm_forward_kernel, true, 4, 1, true)
+    NORM_CASE(norm_forward_kernel, 1, 4, 4, false)
+    NORM_CASE(norm_forward_kernel, 2, 2, 2, false)
+    NORM_CASE(norm_forward_kernel, 4, 1, 1, false)
+    NORM_CASE(norm_forward_kernel, 4, 1, 1, true)
     return launch_status();
 }
 
@@ -555,11 +608,12 @@ gnn_status_t norm_backward_launch(int n, int f, const float *X, const float *sta
         a.lanes = shape.lanes;
         const bool aligned = f % 4 == 0 && aligned16(X) && aligned16(dY) && aligned16(gamma) && aligned16(beta) &&
                              aligned16(dX) && aligned16(dR) && aligned16(dH);
+        const int mem = norm_memory(n, f, aligned);
         const dim3 grid((unsigned)blocks);
-        NORM_CASE(norm_backward_kernel, false, 1, 2, false) NORM_CASE(norm_backward_kernel, false, 2, 1, false)
-        NORM_CASE(norm_backward_kernel, false, 4, 1, false) NORM_CASE(norm_backward_kernel, false, 4, 1, true)
-        NORM_CASE(norm_backward_kernel, true, 1, 2, false) NORM_CASE(norm_backward_kernel, true, 2, 1, false)
-        NORM_CASE(norm_backward_kernel, true, 4, 1, false) NORM_CASE(norm_backward_kernel, true, 4, 1, true)
+        NORM_CASE(norm_backward_kernel, 1, 2, 4, false)
+        NORM_CASE(norm_backward_kernel, 2, 1, 2, false)
+        NORM_CASE(norm_backward_kernel, 4, 1, 1, false)
+        NORM_CASE(norm_backward_kernel, 4, 1, 1, true)
     }
     GNN_TRY(launch_status());
     if (!sums) return GNN_OK;
@@ -568,5 +622,7 @@ gnn_status_t norm_backward_launch(int n, int f, const float *X, const float *sta
     return launch_status();
 }
 #undef NORM_CASE
+#undef NORM_ACT
+#undef NORM_LAUNCH
 
 }  // namespace gnn
