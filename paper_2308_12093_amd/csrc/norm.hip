@@ -4,18 +4,28 @@
 namespace gnn {
 namespace {
 
-// Four consecutive floats of a row of f, at any 4-byte aligned address; zeros past the row's end.
 typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
 
 typedef float floatx2u __attribute__((ext_vector_type(2), aligned(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
+typedef float floatx3u __attribute__((ext_vector_type(3), aligned(4)));
+
+// Columns c .. c + 3 < f + 3 of a row of f, at any 4-byte aligned address; zeros past the row's end.  The one to three of the last
+// lane are one access, too: f % 4 is the same for all.
 __device__ __forceinline__ float4 load4(const float *row, int c, int f) {
     if (c + 4 <= f) {
         const float4u v = *reinterpret_cast<const float4u *>(row + c);
         return make_float4(v.x, v.y, v.z, v.w);
     }
-    return make_float4(row[c], c + 1 < f ? row[c + 1] : 0.f, c + 2 < f ? row[c + 2] : 0.f, 0.f);
+    const int left = f & 3;
+    if (left == 1) return make_float4(row[c], 0.f, 0.f, 0.f);
+    if (left == 2) {
+        const floatx2u v = *reinterpret_cast<const floatx2u *>(row + c);
+        return make_float4(v.x, v.y, 0.f, 0.f);
+    }
+    const floatx3u v = *reinterpret_cast<const floatx3u *>(row + c);
+    return make_float4(v.x, v.y, v.z, 0.f);
 }
 
 __device__ __forceinline__ void store4(float *row, int c, int f, float4 v) {
@@ -23,9 +33,10 @@ __device__ __forceinline__ void store4(float *row, int c, int f, float4 v) {
         *reinterpret_cast<float4u *>(row + c) = float4u{v.x, v.y, v.z, v.w};
         return;
     }
-    row[c] = v.x;
-    if (c + 1 < f) row[c + 1] = v.y;
-    if (c + 2 < f) row[c + 2] = v.z;
+    const int left = f & 3;
+    if (left == 1) row[c] = v.x;
+    else if (left == 2) *reinterpret_cast<floatx2u *>(row + c) = floatx2u{v.x, v.y};
+    else *reinterpret_cast<floatx3u *>(row + c) = floatx3u{v.x, v.y, v.z};
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
