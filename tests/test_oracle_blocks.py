@@ -86,3 +86,33 @@ def test_layer_norm_gradient_against_differences():
     e, vx, vg = 1e-5, rng.normal(size=X.shape), rng.normal(size=11)
     slope = (value(X + e * vx, gamma + e * vg) - value(X - e * vx, gamma - e * vg)) / (2 * e)
     assert slope == pytest.approx(float((dX * vx).sum() + (dgamma * vg).sum()), rel=1e-7)
+
+
+def test_the_composed_block_against_autograd():
+    """tests/block_case.py: attention written densely, everything else by torch, gradients by autograd."""
+    import oracle
+    from tests import block_case as BC
+    n, heads, k, q = 60, 2, 4, 10
+    rowptr, col, t = BC.inputs(n, 3, heads, k, q, seed=1)
+    rp, c, _ = oracle.add_self_loops_degree(rowptr, col)
+    r = BC.define(rp, c, t, heads, step=5)
+    v = {name: torch.tensor(a.astype(np.float64), requires_grad=name != "T") for name, a in t.items()}
+    f = heads * k
+    m1, m2 = (torch.tensor(blocks.dropout_factor(n, f, BC.P_DROP, BC.SEED, 5, s)) for s in (0, 1))
+    y1 = torch.nn.functional.layer_norm(v["X"], (f,), v["g1"], v["b1"], BC.EPS)
+    M = (y1 @ v["Wa"]).view(n, heads, k)
+    logits = torch.einsum("nhk,hk->nh", M, v["a_src"])[:, None] + torch.einsum("nhk,hk->nh", M, v["a_dst"])[None]
+    stored = torch.zeros(n, n, dtype=torch.bool)
+    stored[np.repeat(np.arange(n), np.diff(rp)), c] = True
+    alpha = torch.nn.functional.leaky_relu(logits, BC.SLOPE).masked_fill(~stored[..., None], -np.inf).softmax(dim=1)
+    A = torch.einsum("ijh,jhk->ihk", alpha, M).reshape(n, f) + v["ba"]
+    H = v["X"] + m1 * A
+    z = torch.nn.functional.layer_norm(H, (f,), v["g2"], v["b2"], BC.EPS) @ v["W"] + v["b"]
+    O = H + m2 * ((torch.nn.functional.silu(z[:, :q]) * z[:, q:]) @ v["Wd"])
+    loss = 0.5 * ((O - v["T"]) ** 2).sum()
+    loss.backward()
+    assert r["loss"] == pytest.approx(loss.item(), rel=1e-12)
+    np.testing.assert_allclose(r["O"], O.detach().numpy(), rtol=1e-10, atol=1e-11)
+    names = dict(X="dX", g1="dg1", b1="db1", g2="dg2", b2="db2", Wa="dWa", a_src="da_src", a_dst="da_dst", ba="dba", W="dW", b="db", Wd="dWd")
+    for name, grad in names.items():
+        np.testing.assert_allclose(np.reshape(r[grad], v[name].shape), v[name].grad.numpy(), rtol=1e-8, atol=1e-9, err_msg=name)
