@@ -186,7 +186,15 @@ gated_gradient_kernel(long n, int k, int lanes, int rows, int parts, const float
 
 // the other kernels read four indices at a time, of f_in and of 2 f_out
 bool too_narrow(int64_t m, int64_t k) { return m < 4 || k < 2; }
-bool gated_few(int64_t n, int64_t m, int64_t k) { return too_narrow(m, k) || ceil_div(n, 32) * ceil_div(k, 32) <= 512; }
+// Tiles of 32 x 32 of H up to which the kernels for few rows are the faster; their time goes with tiles and f_in, where the others
+// begin at five launches and 15 us, eight and 60 us backward.  Few rows / others in us, forward, with backward from Z: 24000 x 64 -> 64, 1500
+// tiles, 10.9 / 17.8, 48 / 69; 12000 x 128 -> 128, 1500, 17.0 / 20.2, 78 / 82; 16000, 2000, 21.5 / 21.0, 89 / 90; 4000 x 256 -> 256,
+// 1000, 21.1 / 21.7, 86 / 86; 2976 x 256 -> 512, 1500, 26.6 / 25.1, 111 / 97; 672 x 512 -> 1024, 700, 26.4 / 28.8, 122 / 100.
+int64_t few_tiles(int64_t m) { return 320000 / (m + 64); }
+// Weights whose gradient is better off in float than through partial products of doubles and the pass over those, however few
+// the rows: 1 x 512 -> 1024 forward and back 57 -> 45 us, 256 rows 75 -> 63; half as many weights, 1 x 256 -> 512, 29 / 33.
+bool wide_weights(int64_t m, int64_t k) { return !too_narrow(m, k) && m * 2 * k >= 1 << 19; }
+bool gated_few(int64_t n, int64_t m, int64_t k) { return too_narrow(m, k) || ceil_div(n, 32) * ceil_div(k, 32) <= few_tiles(m); }
 
 #define BY_GATE(GATE_, KERNEL_, ARG_)                                        \
     ((GATE_) == GNN_GATE_SIGMOID ? KERNEL_<ARG_, GNN_GATE_SIGMOID>           \
@@ -225,7 +233,7 @@ struct Backward {
         d_cols = carve.take<unsigned>(top_blocks(n) * 2 * k);
         rest = carve.take<char>(0);
         size_t most = gemm_half_gated_workspace_bytes(k, m);
-        for (size_t b : {gemm_half_workspace_bytes(m, 2 * k), gemm_half_tn_workspace_bytes(m, 2 * k, n)})
+        for (size_t b : {gemm_half_workspace_bytes(m, 2 * k), gemm_half_tn_workspace_bytes(m, 2 * k, n), gemm_workspace_bytes(0, 1, n, m, 2 * k)})
             if (b > most) most = b;
         bytes = carve.off + most;
     }
@@ -235,7 +243,7 @@ struct Backward {
 
 bool gated_fits(bool backward, int64_t n, int64_t m, int64_t k) {
     if (m > 1 << 21 || k > 1 << 21) return false;
-    if (gated_few(n, m, k)) return ceil_div(n, 32) * ceil_div(k, 32) < (int64_t)1 << 24 && (!backward || gemm_fits(n, m, 2 * k));
+    if (gated_few(n, m, k)) return ceil_div(n, 32) * ceil_div(k, 32) < (int64_t)1 << 24 && (!backward || (gemm_fits(n, m, 2 * k) && gemm_half_tn_fits(m, 2 * k, n)));
     // blocks of the kernels that look for the largest magnitudes, or form D: 32 rows and 64 columns
     return ceil_div(n, 32) * ceil_div(m > k ? m : k, 64) < (int64_t)1 << 24 && gemm_half_fits(n, 2 * k) && (!backward || (gemm_half_fits(n, m) && gemm_half_tn_fits(m, 2 * k, n)));
 }
@@ -246,14 +254,14 @@ size_t gated_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k) {
     const size_t d = align_up((size_t)n * 2 * k * sizeof(float));
     size_t most = 0;
     // the rows up to which the kernels for few rows run
-    const int64_t rows = too_narrow(m, k) ? n : 32 * (512 / ceil_div(k, 32)), small = n < rows ? n : rows;
-    if (small > 0) {
+    const int64_t rows = too_narrow(m, k) ? n : 32 * (few_tiles(m) / ceil_div(k, 32)), small = n < rows ? n : rows;
+    if (small > 0 && !wide_weights(m, k)) {
         const size_t tn = gemm_workspace_bytes(1, 0, m, 2 * k, small);     // a row of sums per chunk is an m-th of it
         most = tn + align_up(tn / m);
         const size_t x = gemm_workspace_bytes(0, 1, small, m, 2 * k);
         if (x > most) most = x;
     }
-    if (!gated_few(n, m, k)) {
+    if (!gated_few(n, m, k) || wide_weights(m, k)) {
         const Backward w(nullptr, n, m, k);
         if (w.bytes > most) most = w.bytes;
     }
@@ -284,9 +292,20 @@ gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X
     int parts = 0;
     if (gated_few(n, m, k)) {
         void *rest = carve.take<char>(0);
-        if (Z) GNN_TRY(gradient(n, k, gate, Z, dH, d, Tops{nullptr, nullptr}, &parts, st));
-        else GNN_TRY(few(n, m, X, W, b, g, st));
-        if (dX) GNN_TRY(gemm_launch(0, 1, n, m, 2 * (int64_t)k, d, W, dX, nullptr, 0, rest, st));
+        const bool wide = wide_weights(m, k);
+        const Backward w(static_cast<char *>(rest), n, m, k);
+        const Tops of_d{nullptr, wide ? w.d_cols : nullptr};
+        if (Z) {
+            GNN_TRY(gradient(n, k, gate, Z, dH, d, of_d, &parts, st));
+        } else {
+            GNN_TRY(few(n, m, X, W, b, g, st));
+            if (wide) GNN_TRY(tops_launch(n, 2 * k, d, of_d, st));
+        }
+        if (dX) GNN_TRY(gemm_launch(0, 1, n, m, 2 * (int64_t)k, d, W, dX, nullptr, 0, wide ? w.rest : rest, st));
+        if (wide) {
+            GNN_TRY(tops_launch(n, m, X, Tops{nullptr, w.x_cols}, st));
+            return gemm_half_tn_launch(m, 2 * (int64_t)k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
+        }
         const TnPlans tn = gemm_tn_plans(m, 2 * (int64_t)k, n);
         GemmExtras extras{};
         extras.sums = db;

@@ -13,7 +13,7 @@ from tests._util import assert_close, dev, host
 pytestmark = pytest.mark.gpu
 
 # (nodes, degree, heads, features a head, hidden of the feed-forward block, seed): small products, and those on fp16 parts
-CASES = [(300, 4, 3, 16, 40, 0), (257, 3, 2, 6, 33, 0), (5000, 2, 2, 16, 256, 3)]
+CASES = [(300, 4, 3, 16, 40, 0), (257, 3, 2, 6, 33, 0), (5000, 2, 2, 16, 1024, 3)]
 
 
 class Block:
