@@ -498,8 +498,8 @@ typedef enum { GNN_ACT_NONE = 0, GNN_ACT_RELU = 1, GNN_ACT_ELU = 2 } gnn_act_t;
  *   likewise: act, drop, gamma and beta as in forward.  dX may be dY.  The sums over the rows have a fixed order.
  *   workspace: gnn_layer_norm_workspace_bytes(n, f), which does not fall as n grows; not used where dgamma and dbeta are NULL
  *   (then it may be NULL).
- * Errors: INVALID_ARG (NULL X / Y / stat / dY, negative n, f < 1, eps not positive and finite, act no gnn_act_t, drop as in
- *   gnn_dropout, workspace NULL or not 256-byte aligned), BUFFER_TOO_SMALL.
+ * Errors: INVALID_ARG (NULL X / Y / stat / dY, negative n, f < 1, eps below the least normal float or not finite, act no
+ *   gnn_act_t, drop as in gnn_dropout, workspace NULL or not 256-byte aligned), BUFFER_TOO_SMALL.
  */
 gnn_status_t gnn_layer_norm_fwd(int32_t n, int32_t f, const float *X, const float *gamma, const float *beta, float eps,
                                 gnn_act_t act, const gnn_dropout_t *drop, float *Y, float *stat_out, void *hip_stream);
@@ -533,10 +533,13 @@ typedef enum { GNN_GATE_SIGMOID = 0, GNN_GATE_SILU = 1, GNN_GATE_GELU = 2 } gnn_
  *   Z [n, 2 f_out] or NULL: receives [A | U], which backward may read instead of forming it again.
  * gnn_gated_bwd - with D = [dH .* U .* act'(A) | dH .* act(A)]:  dW = X^T D [f_in, 2 f_out], db = D^T 1 [2 f_out] (NULL: not
  *   wanted), dX = D W^T [n, f_in] (NULL: not wanted).  Z as forward left it, or NULL: [A | U] is formed again from X, W and b.
- *   dX must not overlap X or dH.
+ *   The products take three fp16 products of two parts per float (or fp32 products where rows are few): rounding errors are
+ *   those of fp32 sums, for elements down to 2^-29 of the largest of their row or column; smaller ones are held to 2^-51 of it.
+ *   Outputs must not overlap inputs or each other.
  *   workspace: gnn_gated_workspace_bytes(backward, n, f_in, f_out), backward 0 or 1; what it returns does not fall as n grows.
  * Errors: INVALID_ARG (NULL X / W / H / dH / dW, negative n, f_in < 1 or f_out < 1, gate no gnn_gate_t, workspace NULL or not
- *   256-byte aligned), BUFFER_TOO_SMALL, UNSUPPORTED (2 f_out or the number of tiles beyond 2^31).
+ *   256-byte aligned), BUFFER_TOO_SMALL, UNSUPPORTED (f_in or f_out beyond 2^21, f_in f_out or
+ *   n ceil(max(f_in, f_out) / 64) from 2^28 on, and backward 64 x 64 tiles of dW times n / 4096 from 2^24 on).
  */
 gnn_status_t gnn_gated_fwd(gnn_gate_t gate, int32_t n, int32_t f_in, int32_t f_out, const float *X, const float *W,
                            const float *b, float *H, float *Z, void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -1,5 +1,6 @@
 // extern "C" entry points: argument checks, then the internal launchers.
 // Every check runs before the first launch, so a failing call has no side effect.
+#include <float.h>
 #include <math.h>
 
 #include "dropout.h"
@@ -46,6 +47,9 @@ gnn_status_t take_dropout(const gnn_dropout_t *d, Dropout *out) {
     *out = Dropout{d->state, d->site, (uint32_t)llrint((double)d->p * 4294967296.0), (float)(1.0 / (1.0 - (double)d->p))};
     return GNN_OK;
 }
+
+// a rounding of the variance to zero must not meet an infinite root
+bool bad_eps(float eps) { return !(eps >= FLT_MIN && eps < INFINITY); }
 
 gnn_status_t check_norm_sums(int32_t n, int32_t f, const float *dgamma, const float *dbeta, const void *workspace,
                              size_t workspace_bytes) {
@@ -442,7 +446,7 @@ size_t gnn_layer_norm_workspace_bytes(int32_t n, int32_t f) { return norm_worksp
 gnn_status_t gnn_layer_norm_fwd(int32_t n, int32_t f, const float *X, const float *gamma, const float *beta, float eps,
                                 gnn_act_t act, const gnn_dropout_t *drop, float *Y, float *stat_out, void *hip_stream) {
     Dropout d;
-    if (n < 0 || f <= 0 || !(eps > 0.f && eps < INFINITY)) return GNN_ERR_INVALID_ARG;
+    if (n < 0 || f <= 0 || bad_eps(eps)) return GNN_ERR_INVALID_ARG;
     if (act != GNN_ACT_NONE && act != GNN_ACT_RELU && act != GNN_ACT_ELU) return GNN_ERR_INVALID_ARG;
     GNN_TRY(take_dropout(drop, &d));
     if (n == 0) return GNN_OK;
@@ -467,7 +471,7 @@ gnn_status_t gnn_add_layer_norm_fwd(int32_t n, int32_t f, const float *X, const 
                                     const float *gamma, const float *beta, float eps, float *H, float *Y, float *stat_out,
                                     void *hip_stream) {
     Dropout d;
-    if (n < 0 || f <= 0 || !(eps > 0.f && eps < INFINITY)) return GNN_ERR_INVALID_ARG;
+    if (n < 0 || f <= 0 || bad_eps(eps)) return GNN_ERR_INVALID_ARG;
     GNN_TRY(take_dropout(drop, &d));
     if (n == 0) return GNN_OK;
     if (!X || !R || !H || !Y || !stat_out || H == Y) return GNN_ERR_INVALID_ARG;

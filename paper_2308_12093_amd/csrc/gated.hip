@@ -1,5 +1,6 @@
 // The gated feed-forward block H = act(X W_gate + b_gate) .* (X W_up + b_up), forward and backward.  Its large products are
-// those of gemm_split.hip (forward, and backward where [A | U] was not kept, with the block's own epilogue) and gemm.hip.
+// those of gemm_half.hip (forward, and backward where [A | U] was not kept, with the block's own epilogue) and of
+// gemm_half_tn.hip; those of few rows are here and in gemm.hip.
 #include "gemm_half.h"
 
 namespace gnn {
@@ -243,9 +244,13 @@ struct Backward {
 
 bool gated_fits(bool backward, int64_t n, int64_t m, int64_t k) {
     if (m > 1 << 21 || k > 1 << 21) return false;
-    if (gated_few(n, m, k)) return ceil_div(n, 32) * ceil_div(k, 32) < (int64_t)1 << 24 && (!backward || (gemm_fits(n, m, 2 * k) && gemm_half_tn_fits(m, 2 * k, n)));
-    // blocks of the kernels that look for the largest magnitudes, or form D: 32 rows and 64 columns
-    return ceil_div(n, 32) * ceil_div(m > k ? m : k, 64) < (int64_t)1 << 24 && gemm_half_fits(n, 2 * k) && (!backward || (gemm_half_fits(n, m) && gemm_half_tn_fits(m, 2 * k, n)));
+    const int64_t most = (int64_t)1 << 24;                 // a grid has less than 2^32 threads
+    if (gated_few(n, m, k))                                // D in blocks of 16 rows and 64 columns
+        return ceil_div(n, 16) * ceil_div(k, 64) < most &&
+               (!backward || (gemm_fits(n, m, 2 * k) && gemm_half_tn_fits(m, 2 * k, n)));
+    // largest magnitudes in blocks of 32 rows and 64 columns
+    return ceil_div(n, 32) * ceil_div(m > k ? m : k, 64) < most && gemm_half_fits(n, 2 * k) &&
+           (!backward || (gemm_half_fits(n, m) && gemm_half_tn_fits(m, 2 * k, n)));
 }
 
 // What n rows take, or fewer: a product of few rows needs less.
@@ -306,11 +311,9 @@ gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X
             GNN_TRY(tops_launch(n, m, X, Tops{nullptr, w.x_cols}, st));
             return gemm_half_tn_launch(m, 2 * (int64_t)k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
         }
-        const TnPlans tn = gemm_tn_plans(m, 2 * (int64_t)k, n);
         GemmExtras extras{};
         extras.sums = db;
-        extras.tn = &tn;
-        extras.workspace = static_cast<char *>(rest) + gemm_tn_workspace_bytes(tn, m, 2 * (int64_t)k);
+        extras.workspace = static_cast<char *>(rest) + gemm_workspace_bytes(1, 0, m, 2 * (int64_t)k, n);
         return gemm_launch(1, 0, m, 2 * (int64_t)k, n, X, d, dW, nullptr, 0, rest, st, nullptr, 0, 0, nullptr, nullptr, &extras);
     }
     const Backward w(static_cast<char *>(workspace) + carve.off, n, m, k);

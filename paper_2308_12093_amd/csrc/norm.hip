@@ -57,7 +57,7 @@ __device__ __forceinline__ float expm1_down(float x) {
 
 template <int ACT>
 __device__ __forceinline__ float activation(float z) {
-    if constexpr (ACT == kActRelu) return fmaxf(z, 0.f);
+    if constexpr (ACT == kActRelu) return z < 0.f ? 0.f : z;                // NaN stays
     if constexpr (ACT == kActElu) return z > 0.f ? z : expm1_down(z);
     return z;
 }

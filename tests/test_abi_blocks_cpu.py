@@ -56,7 +56,7 @@ def test_missing_arrays_are_refused(call, needed):
 
 @pytest.mark.parametrize("call", [forward, add_forward])
 def test_epsilons_that_are_refused(call):
-    for eps in (0.0, -1e-5, float("nan"), float("inf")):
+    for eps in (0.0, -1e-5, 1e-40, float("nan"), float("inf")):
         assert call(eps=eps) == BAD, eps
 
 

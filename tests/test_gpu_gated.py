@@ -221,3 +221,33 @@ def test_a_captured_step_replays(n, m, k):
         torch.cuda.synchronize()
         assert all(torch.equal(out[name], want[name]) for name in out)
         step(torch.empty_like(out["dW"]))                  # eager, on the same workspace
+
+
+def test_arrays_of_more_than_two_to_the_32_bytes():
+    """[A | U] and D of 5 GB: the last rows of H and dX, and the weights' gradient, which every row is in."""
+    n, m, k = (1 << 20) + 5, 16, 600
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    X, W, dH = (torch.randn(*s, generator=gen, device="cuda") for s in ((n, m), (m, 2 * k), (n, k)))
+    W /= 4.0
+    H, Z, dX = torch.empty(n, k, device="cuda"), torch.empty(n, 2 * k, device="cuda"), torch.empty(n, m, device="cuda")
+    dW, ws = torch.empty(m, 2 * k, device="cuda"), B.alloc(max(B.gnn_gated_workspace_bytes(back, n, m, k) for back in (0, 1)))
+    for keep in (True, False):
+        B.gnn_gated_fwd(GATES["sigmoid"], n, m, k, X, W, None, H, Z if keep else None, ws)
+        B.gnn_gated_bwd(GATES["sigmoid"], n, m, k, X, W, None, Z if keep else None, dH, dW, None, dX, ws)
+        tail = slice(n - 37, n)
+        Wh, Xh, dHh = host(W), host(X[tail]), host(dH[tail])
+        want, z = blocks.gated_forward(Xh, Wh, None, "sigmoid")
+        _, _, want_dX, _ = blocks.gated_backward(Xh, Wh, z, dHh, "sigmoid")
+        assert np.abs(host(H[tail]) - want).max() < 1e-5 and np.abs(host(dX[tail]) - want_dX).max() < 1e-3
+        ref = torch.zeros(m, 2 * k, dtype=torch.float64, device="cuda")
+        mag = torch.zeros_like(ref)
+        for first in range(0, n, 1 << 17):
+            x = X[first:first + (1 << 17)].double()
+            zz = x @ W.double()
+            s = torch.sigmoid(zz[:, :k])
+            d = dH[first:first + (1 << 17)].double()
+            D = torch.cat([d * zz[:, k:] * s * (1 - s), d * s], 1)
+            ref += x.t() @ D
+            mag += x.abs().t() @ D.abs()
+        # of each term: the bound of the products (16 indices) and the gate's, and the sums of 4096 rows in float
+        assert bool(((dW.double() - ref).abs() <= (2112 + 64) * U * mag).all())

@@ -397,3 +397,14 @@ def test_calls_go_to_the_current_stream():
     s.synchronize()
     want = host(X) + blocks.dropout(host(Y), blocks.dropout_factor(n, f, 0.5, 0, 0))
     assert np.abs(host(Z) - want).max() < 1e-5 and bool(torch.isfinite(got).all())
+
+
+@pytest.mark.parametrize("f", [33, 96, 4100])
+def test_relu_passes_nan_on(f):
+    """A row that holds an infinity has no mean: its outputs are NaN under ReLU as well, but for those that are dropped."""
+    c = Case(9, f, "relu", 0.25)
+    c.X[4, f // 2] = np.inf
+    Y, stat = torch.empty(9, f, device="cuda"), torch.empty(9, 2, device="cuda")
+    B.gnn_layer_norm_fwd(9, f, dev(c.X), dev(c.gamma), dev(c.beta), EPS, ACTS["relu"], c.drop, Y, stat)
+    got = host(Y)
+    assert np.array_equal(np.isnan(got[4]), c.factor[4] != 0) and np.isfinite(np.delete(got, 4, 0)).all()
