@@ -10,39 +10,41 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
 
-constexpr int KB = 32;                 // reduction indices of a step: lane half h takes 16 h .. 16 h + 15
 
 // Few rows: four wavefronts per 32 rows and 32 columns of H share the reduction, operands straight from memory into
-// registers two steps ahead (the two lane halves of v_mfma_f32_32x32x2_f32 take 16 consecutive indices each), one launch, no
-// scratch.  A wavefront has the sums of the gate and of the other projection for the same elements.
+// registers two steps ahead (the two lane halves of v_mfma_f32_32x32x2_f32 take P consecutive indices each), one launch, no
+// scratch.  A wavefront has the sums of the gate and of the other projection for the same elements.  Bound by the launch and two
+// waits for memory while tiles are few (1 x 256 -> 512 4.9 us), then by the L1's accesses, 64 an instruction for rows that lanes
+// read 16 bytes each of: 3001 x 256 -> 256 13.7 us, 57 TFLOP/s.  Steps of 16 indices leave room for a fourth wavefront per SIMD
+// where 32 take 158 registers (15.8 us; 3001 x 203 -> 259 20.8 -> 18.2); steps of 8, four ahead, 17.4, but 1 x 256 -> 512 5.3.
 template <bool BACK, int GATE>
 __global__ void __launch_bounds__(256)
 gated_few_kernel(int M, int K, const float *__restrict__ X, const float *__restrict__ W, const float *__restrict__ bias, Gated g,
                  int tiles_n) {
-    constexpr int AHEAD = 2;
+    constexpr int AHEAD = 2, P = 8;            // steps ahead; indices of a step for each lane half
     __shared__ floatx4 sums[4][2][4][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, l = lane % 32, half = lane / 32;
     const int m0 = (int)(blockIdx.x / tiles_n) * 32, j = (int)(blockIdx.x % tiles_n) * 32 + l, jj = min(j, g.half - 1);
-    const int all = (K + KB - 1) / KB, first = all * wave / 4, total = all * (wave + 1) / 4;
+    const int all = (K + 2 * P - 1) / (2 * P), first = all * wave / 4, total = all * (wave + 1) / 4;
     const float *x = X + (size_t)min(m0 + l, M - 1) * K, *w = W + jj;       // what is past the end re-reads the last
     const size_t ld = 2 * (size_t)g.half;
-    float xs[AHEAD][16], ga[AHEAD][16], up[AHEAD][16];
+    float xs[AHEAD][P], ga[AHEAD][P], up[AHEAD][P];
     auto load = [&](int step, int s) __attribute__((always_inline)) {
-        const int k0 = step * KB + 16 * half;
-        if (k0 + 16 <= K) {
+        const int k0 = (2 * step + half) * P;
+        if (k0 + P <= K) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < P / 4; ++i) {
                 const floatx4u v = *reinterpret_cast<const floatx4u *>(x + k0 + 4 * i);
                 xs[s][4 * i] = v.x; xs[s][4 * i + 1] = v.y; xs[s][4 * i + 2] = v.z; xs[s][4 * i + 3] = v.w;
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < P; ++i) {
                 ga[s][i] = w[(k0 + i) * ld];
                 up[s][i] = w[(k0 + i) * ld + g.half];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < P; ++i) {
                 xs[s][i] = k0 + i < K ? x[k0 + i] : 0.f;
                 ga[s][i] = k0 + i < K ? w[(k0 + i) * ld] : 0.f;
                 up[s][i] = k0 + i < K ? w[(k0 + i) * ld + g.half] : 0.f;
@@ -60,7 +62,7 @@ gated_few_kernel(int M, int K, const float *__restrict__ X, const float *__restr
         for (int s = 0; s < AHEAD; ++s) {
             if (step + s < total) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
+                for (int i = 0; i < P; ++i) {
                     a = __builtin_amdgcn_mfma_f32_32x32x2f32(xs[s][i], ga[s][i], a, 0, 0, 0);
                     u = __builtin_amdgcn_mfma_f32_32x32x2f32(xs[s][i], up[s][i], u, 0, 0, 0);
                 }
@@ -187,11 +189,12 @@ gated_gradient_kernel(long n, int k, int lanes, int rows, int parts, const float
 
 // the other kernels read four indices at a time, of f_in and of 2 f_out
 bool too_narrow(int64_t m, int64_t k) { return m < 4 || k < 2; }
-// Tiles of 32 x 32 of H up to which the kernels for few rows are the faster; their time goes with tiles and f_in, where the others
-// begin at five launches and 15 us, eight and 60 us backward.  Few rows / others in us, forward, with backward from Z: 24000 x 64 -> 64, 1500
-// tiles, 10.9 / 17.8, 48 / 69; 12000 x 128 -> 128, 1500, 17.0 / 20.2, 78 / 82; 16000, 2000, 21.5 / 21.0, 89 / 90; 4000 x 256 -> 256,
-// 1000, 21.1 / 21.7, 86 / 86; 2976 x 256 -> 512, 1500, 26.6 / 25.1, 111 / 97; 672 x 512 -> 1024, 700, 26.4 / 28.8, 122 / 100.
-int64_t few_tiles(int64_t m) { return 320000 / (m + 64); }
+// Tiles of 32 x 32 of H up to which the kernels for few rows are the faster; their time goes with tiles times f_in, where the others
+// begin at five launches and 15 us, eight and 60 us backward.  Few rows / others in us, forward, with backward from Z:
+// 128000 x 8 -> 64, 8000 tiles, 26.9 / 30.8, 123 / 136; 176000, 11000, 35.3 / 33.8, 173 / 167; 16000 x 64 -> 256, 4000, 20.0 / 24.4,
+// 94 / 96; 24000, 6000, 27.6 / 26.5, 132 / 112; 32000 x 96 -> 96, 3000, 22.9 / 26.2, 99 / 96; 16000 x 128 -> 128, 2000, 19.3 / 20.6,
+// 87 / 85; 4000 x 256 -> 256, 1000, 19.8 / 21.7, 85 / 84; 1500, 26.6 / 23.8, 122 / 92; 1984 x 512 -> 512, 1000, 33.0 / 29.2, 123 / 100.
+int64_t few_tiles(int64_t m) { return m < 32 ? 8000 : 260000 / m; }
 // Weights whose gradient is better off in float than through partial products of doubles and the pass over those, however few
 // the rows: 1 x 512 -> 1024 forward and back 57 -> 45 us, 256 rows 75 -> 63; half as many weights, 1 x 256 -> 512, 29 / 33.
 bool wide_weights(int64_t m, int64_t k) { return !too_narrow(m, k) && m * 2 * k >= 1 << 19; }

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import oracle
+from oracle import blocks
 from paper_2308_12093_amd import binding as B
 from paper_2308_12093_amd import graphs
 from tests import block_case as BC
@@ -12,7 +13,7 @@ from tests._util import assert_close, dev, host
 
 pytestmark = pytest.mark.gpu
 
-# (nodes, degree, heads, features a head, hidden of the feed-forward block, seed): small products, and those on fp16 parts
+# (nodes, degree, heads, features a head, hidden of the feed-forward block, seed): few rows of the feed-forward block
 CASES = [(300, 4, 3, 16, 40, 0), (257, 3, 2, 6, 33, 0), (5000, 2, 2, 16, 1024, 3)]
 
 
@@ -89,3 +90,40 @@ def test_block(n, deg, heads, k, q, seed, keep):
         torch.cuda.synchronize()
         for name in COMPARED:
             assert torch.equal(block.o[name], want[name]), name
+
+
+@pytest.mark.parametrize("keep", [True, False])
+def test_block_of_many_rows(keep):
+    """The feed-forward block's products on fp16 parts.  What is a row's own is compared with the whole block's definition.  A sum
+    over 9000 rows adds up the roundings of all that stand before it (of magnitudes, sum |G| |dP|, of some thousands: 10^-4 each unit
+    in the last place), so it is compared with its definition at the arrays that its kernel was given, within c u times the sum
+    of magnitudes, u = 2^-24: c = 1 for the product of doubles' rounding to float, 2112 + 64 for the chunks of 4096 rows in float
+    and the gate, 300 + 64 for the norm's and its statistics (off by 13 u of the row's mean magnitude: |xhat| + 1)."""
+    n, deg, heads, k, q, seed = 9000, 2, 2, 16, 1024, 3
+    rowptr, col, t = BC.inputs(n, deg, heads, k, q, seed)
+    rp, c, _ = oracle.add_self_loops_degree(rowptr, col)
+    block, u = Block(graphs.gat_graph(rowptr, col), heads, k, q, t, keep), 2.0 ** -24
+    r = BC.define(rp, c, t, heads, 0)
+    assert r["nearest"] > 1e-5
+    block.step()
+    o = {name: host(a).astype(np.float64) for name, a in block.o.items()}
+    for name in ("Y1", "A", "H", "Y2", "G", "O", "dX"):
+        assert_close(o[name], r[name], name)
+
+    def within(name, ref, most):
+        over = np.abs(o[name] - ref) - most
+        assert over.max() <= 0, (name, over.max(), np.abs(o[name] - ref).max())
+
+    ref = o["G"].T @ o["dP"]
+    within("dWd", ref, u * (np.abs(ref) + 1e-6 * (np.abs(o["G"]).T @ np.abs(o["dP"]))))
+    _, Z = blocks.gated_forward(o["Y2"], t["W"], t["b"], BC.GATE)
+    dW, db, _, D = blocks.gated_backward(o["Y2"], t["W"], Z, o["dG"], BC.GATE)
+    mag = np.abs(o["dG"]) * (1 + np.abs(Z[:, :q]) + np.abs(Z[:, q:])) * 2      # |D| and the gate's part in its error
+    mag = np.concatenate([mag, mag], axis=1)
+    within("dW", dW, (2112 + 64) * u * (np.abs(o["Y2"]).T @ mag))
+    within("db", db, (2112 + 64) * u * mag.sum(axis=0))
+    for X, dY, gamma, beta, dg, dbeta in ((o["H"], o["dY2"], "g2", "b2", "dg2", "db2"), (t["X"], o["dY1"], "g1", "b1", "dg1", "db1")):
+        _, ref_g, ref_b = blocks.layer_norm_backward(X, t[gamma], t[beta], BC.EPS, dY)
+        xhat = np.abs(blocks.normalise(X, BC.EPS)[0])
+        within(dg, ref_g, 364 * u * (np.abs(dY) * (xhat + 1)).sum(axis=0))
+        within(dbeta, ref_b, 364 * u * np.abs(dY).sum(axis=0))

@@ -79,7 +79,9 @@ SHAPES = [(1, 1, 1), (1, 256, 512), (2, 3, 5), (5, 16, 16), (7, 64, 33), (31, 10
           (9000, 300, 515), (5000, 700, 33), (1, 2050, 7), (17, 1030, 1026),
           (3000, 40, 1200), (3000, 41, 1201), (40000, 20, 1), (40000, 3, 40), (30000, 300, 30), (40000, 301, 30), (33000, 50, 30), (40001, 33, 65),
           (2000, 512, 1000), (32767, 20, 40), (32768, 36, 130), (32767, 36, 130), (1, 520, 600), (33, 513, 514),
-          (200, 260, 1025)]
+          (200, 260, 1025),
+          (32767, 68, 130), (32768, 68, 130), (32769, 67, 129), (20011, 104, 129), (66001, 52, 68), (3000, 40, 2304), (3000, 41, 2401),
+          (100000, 24, 65), (300000, 4, 20), (260000, 5, 30)]
 
 
 @pytest.mark.parametrize("gate", ["sigmoid", "silu", "gelu"])
@@ -118,7 +120,7 @@ def test_without_an_input_gradient(n, m, k):
     assert all(torch.equal(a, b) for a, b in zip(got[:4], again[:4])) and bool(torch.isnan(again[4]).all())
 
 
-@pytest.mark.parametrize("n,m,k", [(3, 24, 20), (500, 64, 96), (5000, 64, 64), (20000, 64, 160), (3000, 40, 1200)])
+@pytest.mark.parametrize("n,m,k", [(3, 24, 20), (500, 64, 96), (5000, 64, 64), (20000, 64, 160), (3000, 40, 1200), (24000, 64, 200), (3000, 41, 2401)])
 def test_what_is_not_finite_stays_where_it_belongs(n, m, k):
     """An infinite or NaN input spoils its row of H and dX, a NaN gradient the weights that it meets; every other row is exact."""
     c = Case(n, m, k, "silu")
@@ -143,7 +145,7 @@ def test_what_is_not_finite_stays_where_it_belongs(n, m, k):
 
 def test_an_infinite_product_is_infinite():
     """As with the fp32 instruction: parts of an infinity would make NaN of it."""
-    for n, k in ((2, 32), (4000, 32), (40000, 160)):
+    for n, k in ((2, 32), (4000, 32), (40000, 160), (60000, 160)):
         c = Case(n, 32, k, "sigmoid", bias=False)
         W = np.abs(c.W)
         X = np.abs(c.X)
@@ -155,13 +157,13 @@ def test_an_infinite_product_is_infinite():
 
 @pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** 60])
 def test_magnitudes_far_from_one(scale):
-    for n, k in ((20, 40), (3000, 40), (20000, 160)):
+    for n, k in ((20, 40), (3000, 40), (20000, 160), (45000, 160)):
         c = Case(n, 40, k, "sigmoid", bias=False, scale=scale)
         H, _, dW, _, _ = run(c, False)
         within(H, c.H, c.H_most, "H")
 
 
-@pytest.mark.parametrize("n,k", [(50, 48), (20000, 160)])
+@pytest.mark.parametrize("n,k", [(50, 48), (20000, 160), (45000, 160)])
 def test_one_large_feature_beside_others(n, k):
     """A column of 1e8 whose weights are zero: the others keep their digits, in the products with the rows and with the columns."""
     c = Case(n, 40, k, "sigmoid", bias=False)
@@ -173,7 +175,7 @@ def test_one_large_feature_beside_others(n, k):
     within(dW, c.dW, c.dW_most, "dW")
 
 
-@pytest.mark.parametrize("n,k", [(50, 48), (20000, 160)])
+@pytest.mark.parametrize("n,k", [(50, 48), (20000, 160), (45000, 160)])
 def test_rows_of_gradients_of_all_magnitudes(n, k):
     """dH of 1 down to 2^-60, and rows of zeros: every row of dX keeps its digits."""
     c = Case(n, 40, k, "silu")
@@ -195,7 +197,8 @@ def test_no_rows():
     assert not dW.any() and not db.any()
 
 
-@pytest.mark.parametrize("n,m,k", [(300, 64, 96), (5000, 64, 64), (1, 100, 60), (20000, 64, 160), (3000, 40, 1200)])
+@pytest.mark.parametrize("n,m,k", [(300, 64, 96), (5000, 64, 64), (1, 100, 60), (20000, 64, 160), (3000, 40, 1200), (24000, 64, 200),
+                                   (3000, 40, 2304)])
 def test_a_captured_step_replays(n, m, k):
     c = Case(n, m, k, "silu")
     X, W, b, dH = dev(c.X), dev(c.W), dev(c.b), dev(c.dH)
