@@ -108,7 +108,7 @@ gemm_half_tn_kernel(TnProduct g) {
     // The products of the step in `buf`, and between them the parts of the next (`raw`, into `next`), whose floats are then loaded
     // for the one after it.  A matrix instruction takes 32 cycles, in which its wavefront can issue eight others: they are
     // written, and kept (sched_barrier), in that order: left to itself the compiler issues all matrix instructions, then
-    // all others (65536 x 512 x 2048: 616 us).
+    // all others (512 x 2048 over 65536 rows: 616 us; in this order 600, 229 TFLOP/s, 0.69 PFLOP/s on the instruction).
     auto turn = [&](long k, const char *buf, char *next, float (&raw)[FRAGS][8], bool more) __attribute__((always_inline)) {
         __syncthreads();
         half8 a[TM][2][2], b[TN][2][2];
