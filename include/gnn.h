@@ -481,7 +481,8 @@ gnn_status_t gnn_rng_advance(uint64_t *state, uint64_t by, void *hip_stream);
 /*
  * gnn_dropout - Y = R + dropout(X), all [n, f]; R NULL: Y = dropout(X).  drop NULL (or p = 0): nothing is dropped.
  *   The gradient with respect to X is the same call on dY without R, that with respect to R is dY.
- *   Y may be X or R.  Errors: INVALID_ARG (NULL X / Y, negative n, f < 1, p outside [0, 1), state NULL or misaligned).
+ *   Y may be X or R.  Errors: INVALID_ARG (NULL X / Y, negative n, f < 1, p outside [0, 1), state NULL or misaligned),
+ *   UNSUPPORTED (f beyond 2^30).
  */
 gnn_status_t gnn_dropout(int32_t n, int32_t f, const float *X, const float *R, const gnn_dropout_t *drop, float *Y,
                          void *hip_stream);
@@ -499,7 +500,8 @@ typedef enum { GNN_ACT_NONE = 0, GNN_ACT_RELU = 1, GNN_ACT_ELU = 2 } gnn_act_t;
  *   workspace: gnn_layer_norm_workspace_bytes(n, f), which does not fall as n grows; not used where dgamma and dbeta are NULL
  *   (then it may be NULL).
  * Errors: INVALID_ARG (NULL X / Y / stat / dY, negative n, f < 1, eps below the least normal float or not finite, act no
- *   gnn_act_t, drop as in gnn_dropout, workspace NULL or not 256-byte aligned), BUFFER_TOO_SMALL.
+ *   gnn_act_t, drop as in gnn_dropout, workspace NULL or not 256-byte aligned), BUFFER_TOO_SMALL, UNSUPPORTED (f beyond 2^24, or
+ *   2^24 rows and more of f beyond 4096).
  */
 gnn_status_t gnn_layer_norm_fwd(int32_t n, int32_t f, const float *X, const float *gamma, const float *beta, float eps,
                                 gnn_act_t act, const gnn_dropout_t *drop, float *Y, float *stat_out, void *hip_stream);

@@ -58,6 +58,9 @@ gnn_status_t check_norm_sums(int32_t n, int32_t f, const float *dgamma, const fl
     return workspace_bytes < norm_workspace_bytes(n, f) ? GNN_ERR_BUFFER_TOO_SMALL : GNN_OK;
 }
 
+// blocks of the kernels for long rows, a row each, and of the last sums, 16 columns each
+bool norm_fits(int32_t n, int32_t f) { return f <= 1 << 24 && (f <= 4096 || n < 1 << 24); }
+
 bool bad_gated(int gate, int32_t n, int32_t f_in, int32_t f_out) {
     return (gate != GNN_GATE_SIGMOID && gate != GNN_GATE_SILU && gate != GNN_GATE_GELU) || n < 0 || f_in <= 0 || f_out <= 0;
 }
@@ -438,6 +441,7 @@ gnn_status_t gnn_dropout(int32_t n, int32_t f, const float *X, const float *R, c
     GNN_TRY(take_dropout(drop, &d));
     if (n == 0) return GNN_OK;
     if (!X || !Y) return GNN_ERR_INVALID_ARG;
+    if (f > 1 << 30) return GNN_ERR_UNSUPPORTED;
     return dropout_launch(n, f, X, R, d, Y, as_stream(hip_stream));
 }
 
@@ -451,6 +455,7 @@ gnn_status_t gnn_layer_norm_fwd(int32_t n, int32_t f, const float *X, const floa
     GNN_TRY(take_dropout(drop, &d));
     if (n == 0) return GNN_OK;
     if (!X || !Y || !stat_out) return GNN_ERR_INVALID_ARG;
+    if (!norm_fits(n, f)) return GNN_ERR_UNSUPPORTED;
     return norm_forward_launch(n, f, X, nullptr, gamma, beta, eps, act, d, nullptr, Y, stat_out, as_stream(hip_stream));
 }
 
@@ -462,6 +467,7 @@ gnn_status_t gnn_layer_norm_bwd(int32_t n, int32_t f, const float *X, const floa
     if (act != GNN_ACT_NONE && act != GNN_ACT_RELU && act != GNN_ACT_ELU) return GNN_ERR_INVALID_ARG;
     GNN_TRY(take_dropout(drop, &d));
     if (n > 0 && (!X || !stat || !dY)) return GNN_ERR_INVALID_ARG;
+    if (!norm_fits(n, f)) return GNN_ERR_UNSUPPORTED;
     GNN_TRY(check_norm_sums(n, f, dgamma, dbeta, workspace, workspace_bytes));
     return norm_backward_launch(n, f, X, stat, gamma, beta, act, d, false, dY, nullptr, nullptr, dX, dgamma, dbeta, workspace,
                                 as_stream(hip_stream));
@@ -475,6 +481,7 @@ gnn_status_t gnn_add_layer_norm_fwd(int32_t n, int32_t f, const float *X, const 
     GNN_TRY(take_dropout(drop, &d));
     if (n == 0) return GNN_OK;
     if (!X || !R || !H || !Y || !stat_out || H == Y) return GNN_ERR_INVALID_ARG;
+    if (!norm_fits(n, f)) return GNN_ERR_UNSUPPORTED;
     return norm_forward_launch(n, f, X, R, gamma, beta, eps, kActNone, d, H, Y, stat_out, as_stream(hip_stream));
 }
 
@@ -485,6 +492,7 @@ gnn_status_t gnn_add_layer_norm_bwd(int32_t n, int32_t f, const float *H, const 
     if (n < 0 || f <= 0) return GNN_ERR_INVALID_ARG;
     GNN_TRY(take_dropout(drop, &d));
     if (n > 0 && (!H || !stat || !dY || !dR || dX == dR)) return GNN_ERR_INVALID_ARG;
+    if (!norm_fits(n, f)) return GNN_ERR_UNSUPPORTED;
     GNN_TRY(check_norm_sums(n, f, dgamma, dbeta, workspace, workspace_bytes));
     return norm_backward_launch(n, f, H, stat, gamma, nullptr, kActNone, d, true, dY, dH, dR, dX, dgamma, dbeta, workspace,
                                 as_stream(hip_stream));

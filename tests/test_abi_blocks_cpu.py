@@ -46,6 +46,14 @@ def test_sizes_and_dropouts_that_are_refused(call):
         assert call(d=drop(**wrong)) == BAD, wrong
 
 
+@pytest.mark.parametrize("call", [forward, backward, add_forward, add_backward])
+def test_rows_that_no_grid_covers_are_refused(call):
+    more = dict(nbytes=1 << 62) if call in (backward, add_backward) else {}
+    for n, f in ((1, (1 << 24) + 1), (1, (1 << 31) - 1), (1 << 24, 4097)):
+        assert call(n=n, f=f, **more) == B.GNN_ERR_UNSUPPORTED, (n, f)
+    assert dropout(n=1, f=(1 << 30) + 1) == B.GNN_ERR_UNSUPPORTED
+
+
 @pytest.mark.parametrize("call,needed", [(dropout, "XY"), (forward, ["X", "Y", "stat"]), (backward, ["X", "stat", "dY", "ws"]),
                                          (add_forward, ["X", "R", "H", "Y", "stat"]),
                                          (add_backward, ["H", "stat", "dY", "dR", "ws"])])
