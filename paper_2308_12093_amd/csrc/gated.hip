@@ -13,10 +13,11 @@ typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
 
 // Few rows: four wavefronts per 32 rows and 32 columns of H share the reduction, operands straight from memory into
 // registers two steps ahead (the two lane halves of v_mfma_f32_32x32x2_f32 take P consecutive indices each), one launch, no
-// scratch.  A wavefront has the sums of the gate and of the other projection for the same elements.  Bound by the launch and two
-// waits for memory while tiles are few (1 x 256 -> 512 4.9 us), then by the L1's accesses, 64 an instruction for rows that lanes
-// read 16 bytes each of: 3001 x 256 -> 256 13.7 us, 57 TFLOP/s.  Steps of 16 indices leave room for a fourth wavefront per SIMD
-// where 32 take 158 registers (15.8 us; 3001 x 203 -> 259 20.8 -> 18.2); steps of 8, four ahead, 17.4, but 1 x 256 -> 512 5.3.
+// scratch.  A wavefront has the sums of the gate and of the other projection for the same elements.  While tiles are few, bound by
+// the launch and two waits for memory (1 x 256 -> 512 4.9 us); then by no one thing: 3001 x 203 -> 259, 18.2 us, four blocks on the
+// fullest CU, takes 15.9 with no loads of X, 13.4 with none of W, and its matrix instructions alone 5.5; X in whole lines, which
+// would have to pass through LDS, 17.5.  Steps of 16 indices leave room for a fourth wavefront per SIMD where 32 take 158
+// registers (20.8 us); steps of 8, four ahead, 17.4, but 1 x 256 -> 512 5.3.
 template <bool BACK, int GATE>
 __global__ void __launch_bounds__(256)
 gated_few_kernel(int M, int K, const float *__restrict__ X, const float *__restrict__ W, const float *__restrict__ bias, Gated g,
