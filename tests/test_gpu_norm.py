@@ -189,26 +189,27 @@ def test_a_row_that_is_not_finite_spoils_itself_alone():
         assert (np.abs(t[rest] - want[rest]) <= most[rest]).all()
 
 
-def test_layer_norm_in_place_and_with_parts_of_its_gradients():
-    c = Case(77, 200, "elu", 0.4)
+@pytest.mark.parametrize("f", [200, 5003])
+def test_layer_norm_in_place_and_with_parts_of_its_gradients(f):
+    c = Case(77, f, "elu", 0.4)
     c.define()
     want = run_norm(c)
     X, dY, ga, be = dev(c.X), dev(c.dY), dev(c.gamma), dev(c.beta)
     stat = torch.empty(77, 2, device="cuda")
     Y = X.clone()
-    B.gnn_layer_norm_fwd(77, 200, Y, ga, be, EPS, ACTS["elu"], c.drop, Y, stat)
+    B.gnn_layer_norm_fwd(77, f, Y, ga, be, EPS, ACTS["elu"], c.drop, Y, stat)
     assert torch.equal(Y, want[0])
-    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(77, 200))
-    dg, db = torch.empty(200, device="cuda"), torch.empty(200, device="cuda")
+    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(77, f))
+    dg, db = torch.empty(f, device="cuda"), torch.empty(f, device="cuda")
     both = dY.clone()
-    B.gnn_layer_norm_bwd(77, 200, X, stat, ga, be, ACTS["elu"], c.drop, both, both, dg, db, ws)
+    B.gnn_layer_norm_bwd(77, f, X, stat, ga, be, ACTS["elu"], c.drop, both, both, dg, db, ws)
     assert torch.equal(both, want[1]) and torch.equal(dg, want[2]) and torch.equal(db, want[3])
-    alone = torch.empty(77, 200, device="cuda")
-    B.gnn_layer_norm_bwd(77, 200, X, stat, ga, be, ACTS["elu"], c.drop, dY, alone, None, None, None)
+    alone = torch.empty(77, f, device="cuda")
+    B.gnn_layer_norm_bwd(77, f, X, stat, ga, be, ACTS["elu"], c.drop, dY, alone, None, None, None)
     assert torch.equal(alone, want[1])
     for which in range(2):
-        one = torch.empty(200, device="cuda")
-        B.gnn_layer_norm_bwd(77, 200, X, stat, ga, be, ACTS["elu"], c.drop, dY, None, *((one, None) if which == 0 else (None, one)), ws)
+        one = torch.empty(f, device="cuda")
+        B.gnn_layer_norm_bwd(77, f, X, stat, ga, be, ACTS["elu"], c.drop, dY, None, *((one, None) if which == 0 else (None, one)), ws)
         assert torch.equal(one, want[2 + which])
 
 
@@ -251,25 +252,26 @@ def test_add_layer_norm(n, f, p):
             within(got, getattr(c, name), getattr(c, name + "_most"), name)
 
 
-def test_add_layer_norm_over_its_own_inputs():
-    c = Case(100, 72, p=0.3, residual=True)
+@pytest.mark.parametrize("f", [72, 4108])
+def test_add_layer_norm_over_its_own_inputs(f):
+    c = Case(100, f, p=0.3, residual=True)
     H, Y, dR, dX, dg, db = run_add(c)
-    ga, be, stat, y = dev(c.gamma), dev(c.beta), torch.empty(100, 2, device="cuda"), torch.empty(100, 72, device="cuda")
+    ga, be, stat, y = dev(c.gamma), dev(c.beta), torch.empty(100, 2, device="cuda"), torch.empty(100, f, device="cuda")
     for over in (0, 1):
         X, R = dev(c.X), dev(c.R)
-        B.gnn_add_layer_norm_fwd(100, 72, X, R, c.drop, ga, be, EPS, (X, R)[over], y, stat)
+        B.gnn_add_layer_norm_fwd(100, f, X, R, c.drop, ga, be, EPS, (X, R)[over], y, stat)
         assert torch.equal((X, R)[over], H) and torch.equal(y, Y)
-    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(100, 72))
-    g, b = torch.empty(72, device="cuda"), torch.empty(72, device="cuda")
+    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(100, f))
+    g, b = torch.empty(f, device="cuda"), torch.empty(f, device="cuda")
     for over in (0, 1):
         dY, dH = dev(c.dY), dev(c.dH)
-        B.gnn_add_layer_norm_bwd(100, 72, H, stat, ga, c.drop, dY, dH, (dY, dH)[over], (dH, dY)[over], g, b, ws)
+        B.gnn_add_layer_norm_bwd(100, f, H, stat, ga, c.drop, dY, dH, (dY, dH)[over], (dH, dY)[over], g, b, ws)
         assert torch.equal((dY, dH)[over], dR) and torch.equal((dH, dY)[over], dX) and torch.equal(g, dg) and torch.equal(b, db)
     # nothing flows back into H from elsewhere; the masked gradient is not asked for
-    zero, alone = torch.zeros(100, 72, device="cuda"), torch.empty(100, 72, device="cuda")
-    want = torch.empty(100, 72, device="cuda")
-    B.gnn_add_layer_norm_bwd(100, 72, H, stat, ga, c.drop, dev(c.dY), zero, want, None, g, b, ws)
-    B.gnn_add_layer_norm_bwd(100, 72, H, stat, ga, c.drop, dev(c.dY), None, alone, None, None, None, None)
+    zero, alone = torch.zeros(100, f, device="cuda"), torch.empty(100, f, device="cuda")
+    want = torch.empty(100, f, device="cuda")
+    B.gnn_add_layer_norm_bwd(100, f, H, stat, ga, c.drop, dev(c.dY), zero, want, None, g, b, ws)
+    B.gnn_add_layer_norm_bwd(100, f, H, stat, ga, c.drop, dev(c.dY), None, alone, None, None, None, None)
     assert torch.equal(alone, want)
 
 
