@@ -233,9 +233,9 @@ struct Backward {
     Backward(char *at, int64_t n, int64_t m, int64_t k) {
         Carver carve(at);
         x_rows = carve.take<unsigned>(n * ceil_div(m, 64));
-        x_cols = carve.take<unsigned>(top_blocks(n) * m);
+        x_cols = carve.take<unsigned>(most_top_blocks(n) * m);
         d_rows = carve.take<unsigned>(n * ceil_div(k, 32));      // gated_row_parts(n, k), or those of `gradient`
-        d_cols = carve.take<unsigned>(top_blocks(n) * 2 * k);
+        d_cols = carve.take<unsigned>(most_top_blocks(n) * 2 * k);
         rest = carve.take<char>(0);
         size_t most = gemm_half_gated_workspace_bytes(k, m);
         for (size_t b : {gemm_half_workspace_bytes(m, 2 * k), gemm_half_tn_workspace_bytes(m, 2 * k, n), gemm_workspace_bytes(0, 1, n, m, 2 * k)})

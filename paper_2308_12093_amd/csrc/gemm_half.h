@@ -12,8 +12,14 @@ struct Tops {
     unsigned *rows, *cols;             // either may be NULL: not wanted
 };
 // Few rows in smaller blocks, so that there are enough of them for the chip.
-__host__ __device__ constexpr int top_rows(int64_t n) { return n < 32768 ? 32 : 128; }
+constexpr int64_t kTopRowsLine = 32768;
+__host__ __device__ constexpr int top_rows(int64_t n) { return n < kTopRowsLine ? 32 : 128; }
 static inline int64_t top_blocks(int64_t n) { return ceil_div(n, top_rows(n)); }
+// of n rows or fewer: just below the line there are more blocks than from it on
+static inline int64_t most_top_blocks(int64_t n) {
+    const int64_t below = top_blocks(n < kTopRowsLine ? n : kTopRowsLine - 1), all = top_blocks(n);
+    return all > below ? all : below;
+}
 
 // columns of B as a product reads it: element (k, n) at k * sk + n * sn
 struct HalfOperand {

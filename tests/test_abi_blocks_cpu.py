@@ -128,3 +128,13 @@ def test_a_workspace_for_the_most_rows_serves_fewer(f):
         for back in (0, 1):
             sizes = [B.gnn_gated_workspace_bytes(back, n, m, f) for n in rows]
             assert sizes == sorted(sizes), (m, back)
+
+
+@pytest.mark.parametrize("m,k", [(512, 1024), (1024, 512), (512, 512), (300, 30), (128, 1024), (512, 7), (16, 512), (2048, 129)])
+def test_a_workspace_serves_fewer_rows_on_both_sides_of_every_line(m, k):
+    """Row by row where blocks of rows change their size (32768) and around powers of two."""
+    rows = sorted({n for p in range(23) for n in range(max(1, (1 << p) - 40), (1 << p) + 450)} | set(range(32700, 33300)))
+    for back in (0, 1):
+        sizes = [B.gnn_gated_workspace_bytes(back, n, m, k) for n in rows]
+        fall = [(n, a, b) for n, a, b in zip(rows[1:], sizes, sizes[1:]) if b < a]
+        assert not fall, fall[:3]
