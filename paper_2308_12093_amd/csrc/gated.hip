@@ -246,14 +246,15 @@ struct Backward {
 
 }  // namespace
 
+// A grid has less than 2^32 threads, 2^24 blocks of 256: the kernels for few rows take 32 x 32 elements of H a block, D and the
+// largest magnitudes are formed in blocks of 16 rows and 64 columns at least.  Both stay below it while there are less than 2^23
+// pieces of 32 x 64.
 bool gated_fits(bool backward, int64_t n, int64_t m, int64_t k) {
     if (m > 1 << 21 || k > 1 << 21) return false;
-    const int64_t most = (int64_t)1 << 24;                 // a grid has less than 2^32 threads
-    if (gated_few(n, m, k))                                // D in blocks of 16 rows and 64 columns
-        return ceil_div(n, 16) * ceil_div(k, 64) < most &&
-               (!backward || (gemm_fits(n, m, 2 * k) && gemm_half_tn_fits(m, 2 * k, n)));
-    // largest magnitudes in blocks of 32 rows and 64 columns
-    return ceil_div(n, 32) * ceil_div(m > k ? m : k, 64) < most && gemm_half_fits(n, 2 * k) &&
+    const int64_t rows = ceil_div(n, 32), most = (int64_t)1 << 23;
+    if (gated_few(n, m, k))
+        return rows * ceil_div(k, 64) < most && (!backward || (gemm_fits(n, m, 2 * k) && gemm_half_tn_fits(m, 2 * k, n)));
+    return rows * ceil_div(m > k ? m : k, 64) < most && gemm_half_fits(n, 2 * k) &&
            (!backward || (gemm_half_fits(n, m) && gemm_half_tn_fits(m, 2 * k, n)));
 }
 

@@ -288,10 +288,12 @@ int64_t tn_chunks(int64_t M, int64_t N, int64_t K) {
 
 }  // namespace
 
+// A grid has less than 2^32 threads: 2^24 blocks, of the product rounded up to a multiple of eight; of the last sums both those of
+// C and those of the column sums.
 bool gemm_half_tn_fits(int64_t M, int64_t N, int64_t K) {
     if (M > INT32_MAX / 4 || N > INT32_MAX / 4) return false;
-    const int64_t blocks = ceil_div(M, 64) * ceil_div(N, 64);
-    return blocks < 1 << 24 && blocks * tn_chunks(M, N, K) < (int64_t)1 << 24 && ceil_div(M * N, 32) < (int64_t)1 << 24;
+    const int64_t blocks = ceil_div(M, 64) * ceil_div(N, 64), most = (int64_t)1 << 24;
+    return blocks < most && blocks * tn_chunks(M, N, K) < most - 8 && ceil_div(M * N, 32) + ceil_div(N, 32) < most;
 }
 
 // no less for a larger K

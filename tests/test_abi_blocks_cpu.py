@@ -138,3 +138,15 @@ def test_a_workspace_serves_fewer_rows_on_both_sides_of_every_line(m, k):
         sizes = [B.gnn_gated_workspace_bytes(back, n, m, k) for n in rows]
         fall = [(n, a, b) for n, a, b in zip(rows[1:], sizes, sizes[1:]) if b < a]
         assert not fall, fall[:3]
+
+
+def test_gated_blocks_that_no_grid_covers_are_refused():
+    """2^24 blocks of 256 threads and more: each of these is the sum or product of what one launch of the call would need."""
+    no = B.GNN_ERR_UNSUPPORTED
+    # the last sums of dW and of db together: 16384 x 32766 / 32 + 32766 / 32
+    assert gated_backward(n=10, m=16384, k=16383, nbytes=1 << 60) == no
+    # 32 x 32 elements of H a block: 256 x 65536
+    for call in (gated, gated_backward):
+        assert call(n=8176, m=3, k=1 << 21, nbytes=1 << 60) == no
+    # 16 rows and 64 columns of X a block, 65 columns are two: 8388608 x 2
+    assert gated(n=(1 << 27) - 1, m=65, k=64, nbytes=1 << 60) == no
