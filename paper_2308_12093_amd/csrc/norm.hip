@@ -101,7 +101,7 @@ dropout_kernel(int n, int f, const float *X, const float *R, Dropout drop, float
 
 // ---- layer norm -------------------------------------------------------------------------------------------
 // A row is the work of `lanes` lanes (a power of two up to a block's 256), R times four columns each, and stays in their
-// registers: mean and variance are two sums over the same registers, so that the variance is one of differences.  Every array
+// registers: mean and variance are sums over the same registers, so that the variance is one of differences.  Every array
 // passes through memory once.  U rows at a time keep loads under way where a row is short; weights are loaded once per block.
 struct Norm {
     int n, f, lanes;
@@ -113,26 +113,70 @@ struct Norm {
     float *H, *Y, *stat;
 };
 
+// v: the sums of a wavefront's lanes of a row; then those of the row's wavefronts, two or four
+template <int U>
+__device__ __forceinline__ void wide_sums(float (&v)[U], int lanes, float *red) {
+    const int wave = threadIdx.x / 64, first = threadIdx.x / lanes * (lanes / 64);
+    __syncthreads();
+    if (threadIdx.x % 64 == 0)
+#pragma unroll
+        for (int u = 0; u < U; ++u) red[4 * u + wave] = v[u];
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float s = red[4 * u + first] + red[4 * u + first + 1];
+        if (lanes == 256) s += red[4 * u + 2] + red[4 * u + 3];
+        v[u] = s;
+    }
+}
+
 // the sums of each of U values over the lanes of a row, in all of them
 template <int U, bool WIDE>
 __device__ __forceinline__ void row_sums(float (&v)[U], int lanes, float *red) {
     for (int d = (WIDE ? 64 : lanes) >> 1; d > 0; d >>= 1)
 #pragma unroll
         for (int u = 0; u < U; ++u) v[u] += __shfl_xor(v[u], d, 64);
-    if constexpr (WIDE) {                                  // the row's wavefronts: two or four
-        const int wave = threadIdx.x / 64, first = threadIdx.x / lanes * (lanes / 64);
-        __syncthreads();
-        if (threadIdx.x % 64 == 0)
+    if constexpr (WIDE) wide_sums(v, lanes, red);
+}
+// The same of U pairs: each half of the lanes goes on with one value of a pair and hands it to the other in the end, two
+// exchanges more than for one value.
+template <int U, bool WIDE>
+__device__ __forceinline__ void row_sums_of_pairs(float (&v)[2 * U], int lanes, float *red) {
+    const int half = (WIDE ? 64 : lanes) >> 1;
+    if (half > 0) {
+        const bool upper = threadIdx.x & half;
+        float s[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) red[4 * u + wave] = v[u];
-        __syncthreads();
+        for (int u = 0; u < U; ++u) s[u] = (upper ? v[2 * u + 1] : v[2 * u]) + __shfl_xor(upper ? v[2 * u] : v[2 * u + 1], half, 64);
+        for (int d = half >> 1; d > 0; d >>= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) s[u] += __shfl_xor(s[u], d, 64);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float s = red[4 * u + first] + red[4 * u + first + 1];
-            if (lanes == 256) s += red[4 * u + 2] + red[4 * u + 3];
-            v[u] = s;
+            const float other = __shfl_xor(s[u], half, 64);
+            v[2 * u] = upper ? other : s[u];
+            v[2 * u + 1] = upper ? s[u] : other;
         }
     }
+    if constexpr (WIDE) wide_sums(v, lanes, red);
+}
+
+// What the mean m of a row is off by, from the sum of the differences d to it, and its variance + eps, from the sum of their squares as
+// well.  Far from zero one unit in the last place of m is as large as what rows of nearly equal values are normalised by, and
+// a sum over lanes divided by f misses the value of a row of f equal ones in a third of all cases.  Such a row's d are a few
+// units each, so the sums are exact; so is their quotient after the step behind the product with 1 / f: d - off and the variance
+// are zero, and m + off is the value.
+__device__ __forceinline__ float rounded_mean(float sum, float inv_f) {
+#pragma clang fp contract(off)
+    return sum * inv_f;                                    // not one with the subtraction that follows: d is exact so
+}
+__device__ __forceinline__ float mean_off_by(float sum, float f, float inv_f) {
+    const float off = sum * inv_f;
+    return fmaf(fmaf(-off, f, sum), inv_f, off);
+}
+__device__ __forceinline__ float variance_and(float eps, float sum, float square, float off, float inv_f) {
+    const float left = fmaf(-off, sum, square);
+    return fmaf(left < 0.f ? 0.f : left, inv_f, eps);      // NaN stays
 }
 
 // How rows are read and written.  kStreamed: aligned rows of arrays beyond the caches, past them (2^20 x 256 backward 645 -> 600
@@ -163,7 +207,7 @@ __device__ __forceinline__ void write4(float *row, int c, int f, float4 v) {
 template <int R, int U, int ACT, bool ADD, int MEM, bool WIDE>
 __global__ void __launch_bounds__(256)
 norm_forward_kernel(Norm a) {
-    __shared__ float red[4 * U];
+    __shared__ float red[8 * U];
     const DropoutWords words(a.drop);
     const float inv_f = 1.f / (float)a.f;
     const int f = a.f, lanes = a.lanes, gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
@@ -176,13 +220,13 @@ norm_forward_kernel(Norm a) {
     }
     for (long base = (long)blockIdx.x * groups * U; base < a.n; base += (long)gridDim.x * groups * U) {
         float4 x[U][R];
-        long row[U];
-        float mean[U], rstd[U];
+        unsigned row[U];                                   // below 2^31 + 2^12
+        float mean[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            row[u] = base + u * groups + grp;
+            row[u] = (unsigned)base + u * groups + grp;
 #pragma unroll
-            for (int r = 0; r < R; ++r) x[u][r] = read4<MEM>(a.X + row[u] * f, 4 * (r * lanes + gl), f, row[u] < a.n);
+            for (int r = 0; r < R; ++r) x[u][r] = read4<MEM>(a.X + (size_t)row[u] * f, 4 * (r * lanes + gl), f, row[u] < (unsigned)a.n);
         }
         if constexpr (ADD) {
 #pragma unroll
@@ -190,11 +234,11 @@ norm_forward_kernel(Norm a) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const int g = r * lanes + gl;
-                    const float4 o = read4<MEM>(a.R + row[u] * f, 4 * g, f, row[u] < a.n);
-                    float4 v = words.apply(x[u][r], (uint32_t)row[u], g);
+                    const float4 o = read4<MEM>(a.R + (size_t)row[u] * f, 4 * g, f, row[u] < (unsigned)a.n);
+                    float4 v = words.apply(x[u][r], row[u], g);
                     v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
                     x[u][r] = v;
-                    if (row[u] < a.n) write4<MEM>(a.H + row[u] * f, 4 * g, f, v);
+                    if (row[u] < (unsigned)a.n) write4<MEM>(a.H + (size_t)row[u] * f, 4 * g, f, v);
                 }
         }
 #pragma unroll
@@ -204,10 +248,11 @@ norm_forward_kernel(Norm a) {
             for (int r = 0; r < R; ++r) mean[u] += (x[u][r].x + x[u][r].y) + (x[u][r].z + x[u][r].w);
         }
         row_sums<U, WIDE>(mean, lanes, red);
+        float s[2 * U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            mean[u] *= inv_f;
-            rstd[u] = 0.f;
+            mean[u] = rounded_mean(mean[u], inv_f);
+            s[2 * u] = s[2 * u + 1] = 0.f;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int c = 4 * (r * lanes + gl);
@@ -215,26 +260,28 @@ norm_forward_kernel(Norm a) {
                 const float d0 = c < f ? v.x - mean[u] : 0.f, d1 = c + 1 < f ? v.y - mean[u] : 0.f;
                 const float d2 = c + 2 < f ? v.z - mean[u] : 0.f, d3 = c + 3 < f ? v.w - mean[u] : 0.f;
                 x[u][r] = make_float4(d0, d1, d2, d3);
-                rstd[u] += fmaf(d0, d0, d1 * d1) + fmaf(d2, d2, d3 * d3);
+                s[2 * u] += (d0 + d1) + (d2 + d3);
+                s[2 * u + 1] += fmaf(d0, d0, d1 * d1) + fmaf(d2, d2, d3 * d3);
             }
         }
-        row_sums<U, WIDE>(rstd, lanes, red);
+        row_sums_of_pairs<U, WIDE>(s, lanes, red);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            rstd[u] = inverse_root(fmaf(rstd[u], inv_f, a.eps));
-            if (row[u] >= a.n) continue;
-            if (gl == 0) *reinterpret_cast<floatx2u *>(a.stat + 2 * row[u]) = floatx2u{mean[u], rstd[u]};
+            const float off = mean_off_by(s[2 * u], (float)f, inv_f);
+            const float rstd = inverse_root(variance_and(a.eps, s[2 * u], s[2 * u + 1], off, inv_f));
+            if (row[u] >= (unsigned)a.n) continue;
+            if (gl == 0) *reinterpret_cast<floatx2u *>(a.stat + 2 * (size_t)row[u]) = floatx2u{mean[u] + off, rstd};
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int g = r * lanes + gl;
-                const float4 d = x[u][r];
-                float4 y = make_float4(fmaf(d.x * rstd[u], ga[r].x, be[r].x), fmaf(d.y * rstd[u], ga[r].y, be[r].y),
-                                       fmaf(d.z * rstd[u], ga[r].z, be[r].z), fmaf(d.w * rstd[u], ga[r].w, be[r].w));
+                const float4 d = make_float4(x[u][r].x - off, x[u][r].y - off, x[u][r].z - off, x[u][r].w - off);
+                float4 y = make_float4(fmaf(d.x * rstd, ga[r].x, be[r].x), fmaf(d.y * rstd, ga[r].y, be[r].y),
+                                       fmaf(d.z * rstd, ga[r].z, be[r].z), fmaf(d.w * rstd, ga[r].w, be[r].w));
                 if constexpr (!ADD) {
                     y = make_float4(activation<ACT>(y.x), activation<ACT>(y.y), activation<ACT>(y.z), activation<ACT>(y.w));
-                    y = words.apply(y, (uint32_t)row[u], g);
+                    y = words.apply(y, row[u], g);
                 }
-                write4<MEM>(a.Y + row[u] * f, 4 * g, f, y);
+                write4<MEM>(a.Y + (size_t)row[u] * f, 4 * g, f, y);
             }
         }
     }
@@ -312,7 +359,7 @@ norm_backward_kernel(NormBack a) {
             }
         }
         if (!write) continue;
-        row_sums<2 * U, WIDE>(s, lanes, red);
+        row_sums_of_pairs<U, WIDE>(s, lanes, red);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (row[u] >= a.n) continue;
@@ -404,8 +451,8 @@ norm_forward_long_kernel(Norm a) {
         }
         sum += (v.x + v.y) + (v.z + v.w);
     }
-    const float mean = block_sum(sum, red) / (float)f;
-    float square = 0.f;
+    const float inv_f = 1.f / (float)f, mean = rounded_mean(block_sum(sum, red), inv_f);
+    float differences = 0.f, square = 0.f;
 #pragma unroll 4
     for (int c = 4 * threadIdx.x; c < f; c += 1024) {      // a thread reads back what it has written itself
         float d[4];
@@ -413,11 +460,15 @@ norm_forward_long_kernel(Norm a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             d[j] = c + j < f ? d[j] - mean : 0.f;
+            differences += d[j];
             square = fmaf(d[j], d[j], square);
         }
     }
-    const float rstd = inverse_root(block_sum(square, red) / (float)f + a.eps);
-    if (threadIdx.x == 0) { a.stat[2 * row] = mean; a.stat[2 * row + 1] = rstd; }
+    differences = block_sum(differences, red);
+    square = block_sum(square, red);
+    const float off = mean_off_by(differences, (float)f, inv_f);
+    const float rstd = inverse_root(variance_and(a.eps, differences, square, off, inv_f));
+    if (threadIdx.x == 0) { a.stat[2 * row] = mean + off; a.stat[2 * row + 1] = rstd; }
 #pragma unroll 2
     for (int c = 4 * threadIdx.x; c < f; c += 1024) {
         float z[4], ga[4], be[4];
@@ -425,7 +476,7 @@ norm_forward_long_kernel(Norm a) {
         weights4(a.gamma, c, f, 1.f, ga);
         weights4(a.beta, c, f, 0.f, be);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] = activation(fmaf((z[j] - mean) * rstd, ga[j], be[j]), a.act);
+        for (int j = 0; j < 4; ++j) z[j] = activation(fmaf(((z[j] - mean) - off) * rstd, ga[j], be[j]), a.act);
         float4 y = make_float4(z[0], z[1], z[2], z[3]);
         if (!a.R) y = words.apply(y, (uint32_t)row, c / 4);
         store4(a.Y + row * f, c, f, y);

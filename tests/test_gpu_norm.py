@@ -410,3 +410,50 @@ def test_relu_passes_nan_on(f):
     B.gnn_layer_norm_fwd(9, f, dev(c.X), dev(c.gamma), dev(c.beta), EPS, ACTS["relu"], c.drop, Y, stat)
     got = host(Y)
     assert np.array_equal(np.isnan(got[4]), c.factor[4] != 0) and np.isfinite(np.delete(got, 4, 0)).all()
+
+
+@pytest.mark.parametrize("f", [1, 3, 7, 15, 47, 65, 100, 203, 255, 256, 257, 1000, 1024, 2050, 4095, 4097, 5003, 8192])
+@pytest.mark.parametrize("residual", [False, True])
+def test_rows_of_equal_values_have_no_deviation(f, residual):
+    """Every row one value, any magnitude: its mean is that value and xhat is 0, so Y is beta, the variance 0 and dgamma 0.  A mean that
+    is off by a unit in its last place gives xhat = 0.295 for 12345.678 instead."""
+    n = 64
+    rng = np.random.default_rng(f)
+    value = (np.exp(rng.uniform(-8.0, 12.0, n)) * rng.choice([-1.0, 1.0], n)).astype(np.float32)
+    value[0] = 12345.678
+    X = np.repeat(value[:, None], f, axis=1)
+    beta, gamma = rng.standard_normal(f).astype(np.float32), (1 + rng.standard_normal(f) / 4).astype(np.float32)
+    dY = dev(rng.standard_normal((n, f)).astype(np.float32))
+    x, ga, be = dev(X), dev(gamma), dev(beta)
+    Y, stat, out = (torch.full(s, NAN, device="cuda") for s in ((n, f), (n, 2), (n, f)))
+    dg, ws = torch.full((f,), NAN, device="cuda"), B.alloc(B.gnn_layer_norm_workspace_bytes(n, f))
+    if residual:
+        H = torch.full((n, f), NAN, device="cuda")
+        B.gnn_add_layer_norm_fwd(n, f, x, torch.zeros_like(x), None, ga, be, EPS, H, Y, stat)
+        B.gnn_add_layer_norm_bwd(n, f, H, stat, ga, None, dY, None, out, None, dg, None, ws)
+        assert torch.equal(H, x)
+    else:
+        B.gnn_layer_norm_fwd(n, f, x, ga, be, EPS, ACTS["none"], None, Y, stat)
+        B.gnn_layer_norm_bwd(n, f, x, stat, ga, be, ACTS["none"], None, dY, out, dg, None, ws)
+    assert torch.equal(Y, be.expand(n, f)) and not dg.any()
+    assert torch.equal(stat[:, 0], dev(value))
+    within(stat[:, 1], np.full(n, 1.0 / np.sqrt(np.float64(np.float32(EPS)))), np.full(n, 4 * U / np.sqrt(EPS)), "rstd")
+
+
+@pytest.mark.parametrize("n,f", [(300, 47), (300, 130), (64, 1030), (64, 4100)])
+def test_rows_far_from_zero_keep_the_digits_that_their_values_have(n, f):
+    """Values of 30000 + N(0, 4), exact in float: the mean is rounded once (u of it) and is otherwise off by the roundings of the
+    differences' sum, L u mean|d|, instead of those of the values'; the rest by the rules above."""
+    c = Case(n, f, offset=30000.0)
+    c.define()
+    got = host(run_norm(c)[0]).astype(np.float64)
+    x = c.X.astype(np.float64)
+    xhat, mean, rstd = blocks.normalise(x, EPS)
+    L, d = f / 64 + 12, np.abs(x - mean)
+    em = U * np.abs(mean) + 2 * L * U * d.mean(1, keepdims=True)
+    # the differences were taken to a mean that is off by L u |mean|: their squares' sum is corrected by a term of that size squared
+    r = (L / 2 + 6) * U * (1 + (L * U * mean * rstd) ** 2) + rstd ** 2 * em ** 2
+    g = np.abs(c.gamma.astype(np.float64))
+    ez = g * (em * rstd + np.abs(xhat) * (r + 2 * U)) + 3 * U * (g * np.abs(xhat) + np.abs(c.beta))
+    over = np.abs(got - c.Y) - (ez + 4 * U * np.abs(c.Y))
+    assert over.max() <= 0, (over.max(), np.abs(got - c.Y).max())
