@@ -457,3 +457,15 @@ def test_rows_far_from_zero_keep_the_digits_that_their_values_have(n, f):
     ez = g * (em * rstd + np.abs(xhat) * (r + 2 * U)) + 3 * U * (g * np.abs(xhat) + np.abs(c.beta))
     over = np.abs(got - c.Y) - (ez + 4 * U * np.abs(c.Y))
     assert over.max() <= 0, (over.max(), np.abs(got - c.Y).max())
+
+
+@pytest.mark.parametrize("f", [6, 33, 96, 4100])
+def test_elu_backward_passes_nan_on(f):
+    """A row that is not finite has no derivative: it is NaN in the sums of every column, as in the definition."""
+    c = Case(9, f, "elu", 0.25)
+    c.X[4, f // 2] = np.nan
+    _, dX, dg, db = (host(t) for t in run_norm(c))
+    want = blocks.layer_norm_backward(c.X, c.gamma, c.beta, EPS, c.dY, "elu", c.factor)
+    for got, ref in zip((dX, dg, db), want):
+        assert np.array_equal(np.isnan(got), np.isnan(ref))
+    assert np.isnan(db).all() and np.isnan(dX).any(1).sum() == 1
