@@ -199,6 +199,8 @@ int64_t few_tiles(int64_t m) { return m < 32 ? 8000 : 260000 / m; }
 // Weights whose gradient is better off in float than through partial products of doubles and the pass over those, however few
 // the rows: 1 x 512 -> 1024 forward and back 57 -> 45 us, 256 rows 75 -> 63; half as many weights, 1 x 256 -> 512, 29 / 33.
 bool wide_weights(int64_t m, int64_t k) { return !too_narrow(m, k) && m * 2 * k >= 1 << 19; }
+// D W^T is a product of the layers
+bool short_columns(int64_t k) { return 2 * k < kShortReduction; }
 bool gated_few(int64_t n, int64_t m, int64_t k) { return too_narrow(m, k) || ceil_div(n, 32) * ceil_div(k, 32) <= few_tiles(m); }
 
 #define BY_GATE(GATE_, KERNEL_, ARG_)                                        \
@@ -255,7 +257,7 @@ bool gated_fits(bool backward, int64_t n, int64_t m, int64_t k) {
     if (gated_few(n, m, k))
         return rows * ceil_div(k, 64) < most && (!backward || (gemm_fits(n, m, 2 * k) && gemm_half_tn_fits(m, 2 * k, n)));
     return rows * ceil_div(m > k ? m : k, 64) < most && gemm_half_fits(n, 2 * k) &&
-           (!backward || (gemm_half_fits(n, m) && gemm_half_tn_fits(m, 2 * k, n)));
+           (!backward || ((short_columns(k) ? gemm_fits(n, m, 2 * k) : gemm_half_fits(n, m)) && gemm_half_tn_fits(m, 2 * k, n)));
 }
 
 // What n rows take, or fewer: a product of few rows needs less.
@@ -285,7 +287,7 @@ gnn_status_t gated_forward_launch(int gate, int n, int m, int k, const float *X,
     if (gated_few(n, m, k)) return few(n, m, X, W, b, g, st);
     Carver carve(workspace);
     const Tops tops{carve.take<unsigned>((size_t)n * ceil_div(m, 64)), nullptr};
-    GNN_TRY(tops_launch(n, m, X, tops, st));
+    if (m >= kShortReduction) GNN_TRY(tops_launch(n, m, X, tops, st));
     return gemm_half_gated_launch(n, m, X, tops.rows, W, b, g, Tops{nullptr, nullptr}, carve.take<char>(0), st);
 }
 
@@ -323,14 +325,15 @@ gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X
     }
     const Backward w(static_cast<char *>(workspace) + carve.off, n, m, k);
     const Tops of_d{w.d_rows, w.d_cols};
-    GNN_TRY(tops_launch(n, m, X, Tops{Z ? nullptr : w.x_rows, w.x_cols}, st));
+    GNN_TRY(tops_launch(n, m, X, Tops{Z || m < kShortReduction ? nullptr : w.x_rows, w.x_cols}, st));
     if (Z) {
         GNN_TRY(gradient(n, k, gate, Z, dH, d, of_d, &parts, st));
     } else {
         GNN_TRY(gemm_half_gated_launch(n, m, X, w.x_rows, W, b, g, of_d, w.rest, st));
         parts = gated_row_parts(n, k);
     }
-    if (dX) GNN_TRY(gemm_half_launch(n, m, 2 * (int64_t)k, d, w.d_rows, parts, W, dX, w.rest, st));
+    if (dX && short_columns(k)) GNN_TRY(gemm_launch(0, 1, n, m, 2 * (int64_t)k, d, W, dX, nullptr, 0, w.rest, st));
+    else if (dX) GNN_TRY(gemm_half_launch(n, m, 2 * (int64_t)k, d, w.d_rows, parts, W, dX, w.rest, st));
     return gemm_half_tn_launch(m, 2 * (int64_t)k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
 }
 

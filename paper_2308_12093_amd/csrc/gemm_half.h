@@ -27,6 +27,12 @@ struct HalfOperand {
     long sk, sn;
 };
 
+// A product of two parts each is off by up to 7.4 u (u = 2^-24) where one of floats is by u at most, but is rounded less often on its way
+// into the sum.  Root mean square of the errors of sums of K products of normal numbers, in u sqrt(K): parts 1.4 for K = 4 to 32, 1.5
+// for 64, 1.7 for 128; a chain of float multiplications and additions 0.7 for 4, 1.2 for 16, 1.5 for 24, 1.7 for 32, 3.4 for
+// 128.  So shorter reductions than this, one step of the kernels, take the fp32 instruction: [A | U] of the gated block
+// here, D W^T in gemm_launch.
+constexpr int64_t kShortReduction = 32;
 bool gemm_half_fits(int64_t M, int64_t N);
 // scratch of a product: the parts of B and their exponents; parts of the reduction
 size_t gemm_half_workspace_bytes(int64_t N, int64_t K);
@@ -38,7 +44,8 @@ gnn_status_t tops_launch(int64_t n, int m, const float *X, const Tops &tops, hip
 // C [M][N] = A [M][K] B^T, B [N][K]; row_tops: of A, `parts` of them.  K >= 4 and gemm_half_fits.
 gnn_status_t gemm_half_launch(int64_t M, int64_t N, int64_t K, const float *A, const unsigned *row_tops, int parts, const float *B,
                               float *C, void *workspace, hipStream_t st);
-// [A | U] = X W + bias, X [M][K] with the row_tops of tops_launch, W [K][2 half]; `out` says what becomes of it.  Backward fills
+// [A | U] = X W + bias, X [M][K] with the row_tops of tops_launch (not read where K < kShortReduction), W [K][2 half]; `out` says
+// what becomes of it.  Backward fills
 // `tops` of D: gated_row_parts(n, half) parts a row.
 int gated_row_parts(int64_t n, int64_t half);
 gnn_status_t gemm_half_gated_launch(int64_t M, int64_t K, const float *X, const unsigned *row_tops, const float *W,

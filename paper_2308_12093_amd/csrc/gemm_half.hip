@@ -1,5 +1,7 @@
 // Products of fp32 matrices on the fp16 matrix instruction (half_parts.h), for the gated block: X W with the gate behind it, and
 // D W^T.
+#include <type_traits>
+
 #include "half_parts.h"
 
 namespace gnn {
@@ -90,7 +92,7 @@ struct HalfProduct {
     const unsigned *row_tops;          // [top_parts][M]
     int top_parts;
     HalfOperand B;
-    const char *parts;
+    const char *parts;                 // of B; neither they nor row_tops are read where the reduction is short
     const int *exps;
     float *C;
     int splits, split_steps;           // kPlain: the reduction's parts, C [split][M][N] then
@@ -115,10 +117,15 @@ enum { kPlain, kGateForward, kGateBackward };
 // Each buffer is an array of its own: the compiler then knows which copies a read has to wait for.
 // GATE (gnn_gate_t) is known to the compiler: with all three in it the epilogue of 32 elements a lane outgrew the instruction cache
 // (2^17 x 128 -> 256 backward 213 us).
-// ALIGNED: K is a multiple of 4, below 2^24, and A 16-byte aligned; otherwise lanes read their rows themselves.
-template <int NT, int OUT, bool ALIGNED, int GATE>
+// ROWS: kCopied where K is a multiple of 4, below 2^24, and A 16-byte aligned; otherwise lanes read their rows themselves, kLoaded.
+// kShort, of a gated block with K < kShortReduction: on the fp32 instruction, W's columns of the block through LDS.  A lane half takes
+// 16 of the indices, 12 or 8.
+enum { kLoaded, kCopied, kShort };
+
+template <int NT, int OUT, int ROWS, int GATE>
 __global__ void __launch_bounds__(256, OUT == kGateBackward ? 2 : 3)
 gemm_half_kernel(HalfProduct g) {
+    constexpr bool ALIGNED = ROWS == kCopied;
     constexpr int STAGE = NT * kTileBytes;
     __shared__ __align__(16) char even[STAGE];
     __shared__ __align__(16) char odd[STAGE];
@@ -145,19 +152,20 @@ gemm_half_kernel(HalfProduct g) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const float4u *>(g.A + ro + min(k + 4 * i, g.K - 4));
     };
-    auto settle = [&](int step) __attribute__((always_inline)) {
-        const int k0 = step * KB;
-        if (k0 + KB <= g.K) return;
+    auto settle_from = [&](int k0) __attribute__((always_inline)) {        // raw[i]: indices k0 + 4 i .. of this lane
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             // floats past the end: 0 none .. 4 all; a shift by one, by two and by four places
-            const int over = min(max(k0 + 16 * half + 4 * i + 4 - g.K, 0), 4);
+            const int over = min(max(k0 + 4 * i + 4 - g.K, 0), 4);
             const bool one = over & 1, two = over & 2, all = over & 4;
             floatx4 v = raw[i];
             v = floatx4{one ? v.y : v.x, one ? v.z : v.y, one ? v.w : v.z, one ? 0.f : v.w};
             v = floatx4{two ? v.z : v.x, two ? v.w : v.y, two ? 0.f : v.z, two ? 0.f : v.w};
             raw[i] = floatx4{all ? 0.f : v.x, all ? 0.f : v.y, all ? 0.f : v.z, all ? 0.f : v.w};
         }
+    };
+    auto settle = [&](int step) __attribute__((always_inline)) {
+        if ((step + 1) * KB > g.K) settle_from(step * KB + 16 * half);
     };
     // global -> LDS, 1 KB per wavefront and instruction, from a uniform base and a 32-bit offset
     auto copy = [](const void *base, unsigned offset, char *to) __attribute__((always_inline)) {
@@ -185,11 +193,11 @@ gemm_half_kernel(HalfProduct g) {
             copy(base + step * KB, 4 * (mine[i] + min(piece, g.K - 4 - step * KB)), rows + wave * 4096 + i * 1024);
         }
     };
-    stage(step0, even);
-    if constexpr (ALIGNED) stage_rows(step0);
-    else load(step0);
-    float scale, scale2;
-    {
+    float scale = 1.f, scale2 = 1.f;
+    if constexpr (ROWS != kShort) {
+        stage(step0, even);
+        if constexpr (ALIGNED) stage_rows(step0);
+        else load(step0);
         unsigned top = 0;
         for (int p = 0; p < g.top_parts; ++p) top = max(top, g.row_tops[(size_t)p * g.M + min(row0 + l, g.M - 1)]);
         const int e = exponent_of(top);
@@ -244,30 +252,56 @@ gemm_half_kernel(HalfProduct g) {
             multiply(acc[c], a, b);
         }
     };
-    for (int step = step0; step < step1; step += 2) {
-        turn(step, even, odd);
-        if (step + 1 < step1) turn(step + 1, odd, even);
-    }
-    float finite = 0.f;
+    bool again = ROWS == kShort;
+    if constexpr (ROWS == kShort) {
+        auto product = [&](auto each) __attribute__((always_inline)) {
+            constexpr int P = decltype(each)::value;
+            float *w = reinterpret_cast<float *>(even);            // [2 P indices][32 NT columns], zeros past the end
+            for (int i = t; i < 2 * P * NT * 32; i += 256) {
+                const int k = i / (NT * 32), c = i / 32 % NT, j = (ct0 / 2 + c % (NT / 2)) * 32 + i % 32;
+                w[i] = k < g.K && j < g.gated.half ? g.B.p[k * g.B.sk + j + (c < NT / 2 ? 0 : g.gated.half)] : 0.f;
+            }
 #pragma unroll
-    for (int c = 0; c < NT; ++c)
+            for (int i = 0; i < P / 4; ++i) raw[i] = *reinterpret_cast<const float4u *>(g.A + ro + min(P * half + 4 * i, g.K - 4));
 #pragma unroll
-        for (int v = 0; v < 16; ++v) finite = fmaf(acc[c][v], 0.f, finite);
-    const bool again = __any(finite != 0.f);               // 0 x (inf or NaN) is NaN
-    if (again) {
-        clear();
-        for (int step = step0; step < step1; ++step) {
-            load(step);
-            settle(step);
-            const int k0 = step * KB + 16 * half;
+            for (int i = P / 4; i < 4; ++i) raw[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+            settle_from(P * half);
+            __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
+            for (int j = 0; j < P; ++j)
 #pragma unroll
-                for (int c = 0; c < NT; ++c) {
-                    const int n = column(c);
-                    const float bv = k0 + j < g.K && n < g.N ? g.B.p[(k0 + j) * g.B.sk + n * g.B.sn] : 0.f;
-                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(raw[j / 4][j % 4], bv, acc[c], 0, 0, 0);
-                }
+                for (int c = 0; c < NT; ++c)
+                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(raw[j / 4][j % 4], w[((P * half + j) * NT + c) * 32 + l], acc[c], 0, 0, 0);
+        };
+        if (g.K > 24) product(std::integral_constant<int, 16>());
+        else if (g.K > 16) product(std::integral_constant<int, 12>());
+        else product(std::integral_constant<int, 8>());
+    } else {
+        for (int step = step0; step < step1; step += 2) {
+            turn(step, even, odd);
+            if (step + 1 < step1) turn(step + 1, odd, even);
+        }
+        float finite = 0.f;
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) finite = fmaf(acc[c][v], 0.f, finite);
+        again = __any(finite != 0.f);                      // 0 x (inf or NaN) is NaN
+        if (again) {
+            clear();
+            for (int step = step0; step < step1; ++step) {
+                load(step);
+                settle(step);
+                const int k0 = step * KB + 16 * half;
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) {
+                        const int n = column(c);
+                        const float bv = k0 + j < g.K && n < g.N ? g.B.p[(k0 + j) * g.B.sk + n * g.B.sn] : 0.f;
+                        acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(raw[j / 4][j % 4], bv, acc[c], 0, 0, 0);
+                    }
+            }
         }
     }
     int eb[NT];
@@ -519,8 +553,8 @@ gnn_status_t gemm_half_launch(int64_t M, int64_t N, int64_t K, const float *A, c
     }
     GNN_TRY(split_weights(g, w, 0, st));
     const bool aligned = K % 4 == 0 && K < 1 << 24 && aligned16(A);
-    auto kernel = w == 2 ? (aligned ? gemm_half_kernel<2, kPlain, true, 0> : gemm_half_kernel<2, kPlain, false, 0>)
-                                     : (aligned ? gemm_half_kernel<4, kPlain, true, 0> : gemm_half_kernel<4, kPlain, false, 0>);
+    auto kernel = w == 2 ? (aligned ? gemm_half_kernel<2, kPlain, kCopied, 0> : gemm_half_kernel<2, kPlain, kLoaded, 0>)
+                                     : (aligned ? gemm_half_kernel<4, kPlain, kCopied, 0> : gemm_half_kernel<4, kPlain, kLoaded, 0>);
     hipLaunchKernelGGL(kernel, product_grid(g), dim3(256), 0, st, g);
     GNN_TRY(launch_status());
     if (g.splits == 1) return GNN_OK;
@@ -543,17 +577,19 @@ gnn_status_t gemm_half_gated_launch(int64_t M, int64_t K, const float *X, const 
     g.gated = out;
     g.tops = tops;
     g.stream = !out.D && (size_t)M * N * sizeof(float) > kStreamBytes;      // D is read next
-    GNN_TRY(split_weights(g, w, w, st));
-    const bool aligned = K % 4 == 0 && K < 1 << 24 && aligned16(X), back = out.D != nullptr;
+    const bool back = out.D != nullptr;
+    const int rows = K < kShortReduction ? kShort : K % 4 == 0 && K < 1 << 24 && aligned16(X) ? kCopied : kLoaded;
+    if (rows != kShort) GNN_TRY(split_weights(g, w, w, st));
     const dim3 grid = product_grid(g);
-#define GATED_CASE(NT_, ALIGNED_, GATE_)                                                                                    \
-    if (w == NT_ && aligned == ALIGNED_ && out.gate == GATE_) {                                                             \
-        if (back) hipLaunchKernelGGL((gemm_half_kernel<NT_, kGateBackward, ALIGNED_, GATE_>), grid, dim3(256), 0, st, g);   \
-        else hipLaunchKernelGGL((gemm_half_kernel<NT_, kGateForward, ALIGNED_, GATE_>), grid, dim3(256), 0, st, g);         \
+#define GATED_CASE(NT_, ROWS_, GATE_)                                                                                       \
+    if (w == NT_ && rows == ROWS_ && out.gate == GATE_) {                                                                   \
+        if (back) hipLaunchKernelGGL((gemm_half_kernel<NT_, kGateBackward, ROWS_, GATE_>), grid, dim3(256), 0, st, g);      \
+        else hipLaunchKernelGGL((gemm_half_kernel<NT_, kGateForward, ROWS_, GATE_>), grid, dim3(256), 0, st, g);            \
     }
-#define GATED_CASES(NT_, ALIGNED_) \
-    GATED_CASE(NT_, ALIGNED_, GNN_GATE_SIGMOID) GATED_CASE(NT_, ALIGNED_, GNN_GATE_SILU) GATED_CASE(NT_, ALIGNED_, GNN_GATE_GELU)
-    GATED_CASES(2, false) GATED_CASES(2, true) GATED_CASES(4, false) GATED_CASES(4, true)
+#define GATED_CASES(NT_, ROWS_) \
+    GATED_CASE(NT_, ROWS_, GNN_GATE_SIGMOID) GATED_CASE(NT_, ROWS_, GNN_GATE_SILU) GATED_CASE(NT_, ROWS_, GNN_GATE_GELU)
+    GATED_CASES(2, kLoaded) GATED_CASES(2, kCopied) GATED_CASES(2, kShort)
+    GATED_CASES(4, kLoaded) GATED_CASES(4, kCopied) GATED_CASES(4, kShort)
 #undef GATED_CASES
 #undef GATED_CASE
     return launch_status();

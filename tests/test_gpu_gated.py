@@ -254,3 +254,42 @@ def test_arrays_of_more_than_two_to_the_32_bytes():
             mag += x.abs().t() @ D.abs()
         # of each term: the bound of the products (16 indices) and the gate's, and the sums of 4096 rows in float
         assert bool(((dW.double() - ref).abs() <= (2112 + 64) * U * mag).all())
+
+
+@pytest.mark.parametrize("m", [4, 5, 7, 8, 16, 24, 31])
+def test_short_reductions_are_those_of_floats(m):
+    """One-hot rows, the commonest input of a layer on a graph: below 32 features a row of [A | U] is a row of W, bit for bit, few rows
+    and many, kept or formed again (D, and with it dX, is the same then)."""
+    for n, k in ((300, 40), (70000, 160), (33000, 515)):
+        c = Case(n, m, k, "sigmoid", bias=False)
+        which = np.arange(n) % m
+        c.X[:] = 0.0
+        c.X[np.arange(n), which] = 1.0
+        c.define()
+        kept = run(c, True)
+        assert np.array_equal(host(kept[1]), c.W[which])
+        check(c, kept, True)
+        formed = run(c, False)
+        check(c, formed, False)
+        assert torch.equal(kept[0], formed[0])
+
+
+@pytest.mark.parametrize("k", [2, 3, 5, 8, 12, 15])
+def test_short_reductions_of_the_input_gradient(k):
+    """D = [dH / 4 | dH / 2] exactly (a = 0, U = 1, sigmoid), so dX is one product of 2 k indices: its root mean square error is at most
+    that of a chain of float multiplications and additions, within the scatter of 10^7 results (below 1 %, taken as 5)."""
+    n, m = 40000, 260
+    rng = np.random.default_rng(k)
+    f32 = lambda *s: rng.standard_normal(s).astype(np.float32)  # noqa: E731
+    X, W, dH = f32(n, m), f32(m, 2 * k), f32(n, k)
+    Z = np.concatenate([np.zeros((n, k), np.float32), np.ones((n, k), np.float32)], 1)
+    D = np.concatenate([dH / 4, dH / 2], 1)
+    dX, dW = torch.empty(n, m, device="cuda"), torch.empty(m, 2 * k, device="cuda")
+    ws = B.alloc(B.gnn_gated_workspace_bytes(True, n, m, k))
+    B.gnn_gated_bwd(GATES["sigmoid"], n, m, k, dev(X), dev(W), None, dev(Z), dev(dH), dW, None, dX, ws)
+    exact = D.astype(np.float64) @ W.astype(np.float64).T
+    chain = np.zeros((n, m), np.float32)
+    for j in range(2 * k):
+        chain = (chain + np.outer(D[:, j].astype(np.float64), W[:, j])).astype(np.float32)
+    rms = lambda a: np.sqrt(np.mean((a - exact) ** 2))  # noqa: E731
+    assert rms(host(dX).astype(np.float64)) <= 1.05 * rms(chain)
