@@ -197,7 +197,8 @@ bool too_narrow(int64_t m, int64_t k) { return m < 4 || k < 2; }
 // 87 / 85; 4000 x 256 -> 256, 1000, 19.8 / 21.7, 85 / 84; 1500, 26.6 / 23.8, 122 / 92; 1984 x 512 -> 512, 1000, 33.0 / 29.2, 123 / 100.
 int64_t few_tiles(int64_t m) { return m < 32 ? 8000 : 260000 / m; }
 // Weights whose gradient is better off in float than through partial products of doubles and the pass over those, however few
-// the rows: 1 x 512 -> 1024 forward and back 57 -> 45 us, 256 rows 75 -> 63; half as many weights, 1 x 256 -> 512, 29 / 33.
+// the rows, forward and back, doubles / float: 1 x 512 -> 1024 57 / 27 us, 256 rows 75 / 63; half as many weights, 1 x 256 -> 512, 28
+// through doubles and 33 through parts of floats.
 bool wide_weights(int64_t m, int64_t k) { return !too_narrow(m, k) && m * 2 * k >= 1 << 19; }
 // D W^T is a product of the layers
 bool short_columns(int64_t k) { return 2 * k < kShortReduction; }
@@ -301,21 +302,22 @@ gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X
     Carver carve(workspace);
     float *d = carve.take<float>((size_t)n * 2 * k);
     const Gated g{k, gate, nullptr, nullptr, dH, d};
+    const bool one_step = n < kShortReduction;             // X^T D does without largest magnitudes
     int parts = 0;
     if (gated_few(n, m, k)) {
         void *rest = carve.take<char>(0);
         const bool wide = wide_weights(m, k);
         const Backward w(static_cast<char *>(rest), n, m, k);
-        const Tops of_d{nullptr, wide ? w.d_cols : nullptr};
+        const Tops of_d{nullptr, wide && !one_step ? w.d_cols : nullptr};
         if (Z) {
             GNN_TRY(gradient(n, k, gate, Z, dH, d, of_d, &parts, st));
         } else {
             GNN_TRY(few(n, m, X, W, b, g, st));
-            if (wide) GNN_TRY(tops_launch(n, 2 * k, d, of_d, st));
+            if (of_d.cols) GNN_TRY(tops_launch(n, 2 * k, d, of_d, st));
         }
         if (dX) GNN_TRY(gemm_launch(0, 1, n, m, 2 * (int64_t)k, d, W, dX, nullptr, 0, wide ? w.rest : rest, st));
         if (wide) {
-            GNN_TRY(tops_launch(n, m, X, Tops{nullptr, w.x_cols}, st));
+            if (!one_step) GNN_TRY(tops_launch(n, m, X, Tops{nullptr, w.x_cols}, st));
             return gemm_half_tn_launch(m, 2 * (int64_t)k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
         }
         GemmExtras extras{};
@@ -324,8 +326,8 @@ gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X
         return gemm_launch(1, 0, m, 2 * (int64_t)k, n, X, d, dW, nullptr, 0, rest, st, nullptr, 0, 0, nullptr, nullptr, &extras);
     }
     const Backward w(static_cast<char *>(workspace) + carve.off, n, m, k);
-    const Tops of_d{w.d_rows, w.d_cols};
-    GNN_TRY(tops_launch(n, m, X, Tops{Z || m < kShortReduction ? nullptr : w.x_rows, w.x_cols}, st));
+    const Tops of_x{Z || m < kShortReduction ? nullptr : w.x_rows, one_step ? nullptr : w.x_cols}, of_d{w.d_rows, w.d_cols};
+    if (of_x.rows || of_x.cols) GNN_TRY(tops_launch(n, m, X, of_x, st));
     if (Z) {
         GNN_TRY(gradient(n, k, gate, Z, dH, d, of_d, &parts, st));
     } else {

@@ -30,8 +30,8 @@ struct HalfOperand {
 // A product of two parts each is off by up to 7.4 u (u = 2^-24) where one of floats is by u at most, but is rounded less often on its way
 // into the sum.  Root mean square of the errors of sums of K products of normal numbers, in u sqrt(K): parts 1.4 for K = 4 to 32, 1.5
 // for 64, 1.7 for 128; a chain of float multiplications and additions 0.7 for 4, 1.2 for 16, 1.5 for 24, 1.7 for 32, 3.4 for
-// 128.  So shorter reductions than this, one step of the kernels, take the fp32 instruction: [A | U] of the gated block
-// here, D W^T in gemm_launch.
+// 128.  So shorter reductions than this, one step of the kernels, are formed in float: [A | U] of the gated block on the
+// fp32 instruction, A^T B in plain code, D W^T in gemm_launch.
 constexpr int64_t kShortReduction = 32;
 bool gemm_half_fits(int64_t M, int64_t N);
 // scratch of a product: the parts of B and their exponents; parts of the reduction
@@ -50,7 +50,8 @@ gnn_status_t gemm_half_launch(int64_t M, int64_t N, int64_t K, const float *A, c
 int gated_row_parts(int64_t n, int64_t half);
 gnn_status_t gemm_half_gated_launch(int64_t M, int64_t K, const float *X, const unsigned *row_tops, const float *W,
                                     const float *bias, const Gated &out, const Tops &tops, void *workspace, hipStream_t st);
-// C [M][N] = A^T B, A [K][M], B [K][N]; sums [N] = the column sums of B unless it is NULL; a_tops, b_tops: their columns'.
+// C [M][N] = A^T B, A [K][M], B [K][N]; sums [N] = the column sums of B unless it is NULL; a_tops, b_tops: their columns', not read
+// where K < kShortReduction.
 bool gemm_half_tn_fits(int64_t M, int64_t N, int64_t K);
 size_t gemm_half_tn_workspace_bytes(int64_t M, int64_t N, int64_t K);
 gnn_status_t gemm_half_tn_launch(int64_t M, int64_t N, int64_t K, const float *A, const unsigned *a_tops, const float *B,

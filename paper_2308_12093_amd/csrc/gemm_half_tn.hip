@@ -274,6 +274,54 @@ tn_reduce_kernel(long count, int splits, const float *__restrict__ part, float *
         }
 }
 
+// The same of fewer indices than kShortReduction, in float: a thread adds VEC columns of kShortRows rows of C.  B comes through the
+// caches once per kShortRows rows, what bounds it is C.
+constexpr int kShortRows = 4;
+
+template <int VEC>
+__global__ void __launch_bounds__(256)
+tn_short_kernel(int M, int N, int K, int blocks_n, const float *__restrict__ A, const float *__restrict__ B, float *__restrict__ C,
+                float *__restrict__ sums) {
+    const int m0 = (int)(blockIdx.x / blocks_n) * kShortRows, n = ((int)(blockIdx.x % blocks_n) * 256 + threadIdx.x) * VEC;
+    if (n >= N) return;
+    float acc[kShortRows][VEC], sum[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+        sum[v] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kShortRows; ++i) acc[i][v] = 0.f;
+    }
+#pragma unroll 4
+    for (int k = 0; k < K; ++k) {
+        float b[VEC];
+        if constexpr (VEC == 4) {
+            const floatx4 x = *reinterpret_cast<const floatx4 *>(B + (size_t)k * N + n);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) b[v] = x[v];
+        } else {
+            b[0] = B[(size_t)k * N + n];
+        }
+#pragma unroll
+        for (int i = 0; i < kShortRows; ++i) {
+            const float a = A[(size_t)k * M + min(m0 + i, M - 1)];
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) acc[i][v] = fmaf(a, b[v], acc[i][v]);
+        }
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) sum[v] += b[v];
+    }
+#pragma unroll
+    for (int i = 0; i < kShortRows; ++i) {
+        if (m0 + i >= M) break;
+        float *to = C + (size_t)(m0 + i) * N + n;
+        if constexpr (VEC == 4) *reinterpret_cast<float4u *>(to) = float4u{acc[i][0], acc[i][1], acc[i][2], acc[i][3]};
+        else *to = acc[i][0];
+    }
+    if (sums && m0 == 0)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) sums[n + v] = sum[v];
+}
+
 int tn_tile(int64_t extent) { return extent <= 64 ? 1 : 2; }
 
 // Chunks: enough blocks for the chip, at least four steps each, at most kMostRows indices.
@@ -304,6 +352,13 @@ size_t gemm_half_tn_workspace_bytes(int64_t M, int64_t N, int64_t K) {
 
 gnn_status_t gemm_half_tn_launch(int64_t M, int64_t N, int64_t K, const float *A, const unsigned *a_tops, const float *B,
                                  const unsigned *b_tops, float *C, float *sums, void *workspace, hipStream_t st) {
+    if (K < kShortReduction) {
+        const int vec = N % 4 == 0 && aligned16(B) ? 4 : 1;
+        const int64_t blocks_n = ceil_div(N, 256 * vec);
+        hipLaunchKernelGGL(vec == 4 ? tn_short_kernel<4> : tn_short_kernel<1>, dim3((unsigned)(ceil_div(M, kShortRows) * blocks_n)),
+                           dim3(256), 0, st, (int)M, (int)N, (int)K, (int)blocks_n, A, B, C, sums);
+        return launch_status();
+    }
     TnProduct g{};
     const int tm = tn_tile(M), tn = tn_tile(N);
     const int64_t chunks = tn_chunks(M, N, K);

@@ -293,3 +293,38 @@ def test_short_reductions_of_the_input_gradient(k):
         chain = (chain + np.outer(D[:, j].astype(np.float64), W[:, j])).astype(np.float32)
     rms = lambda a: np.sqrt(np.mean((a - exact) ** 2))  # noqa: E731
     assert rms(host(dX).astype(np.float64)) <= 1.05 * rms(chain)
+
+
+@pytest.mark.parametrize("m,k", [(520, 600), (513, 514), (256, 1030), (700, 377), (16384, 500)])
+def test_weights_of_one_row_have_the_products_of_floats(m, k):
+    """One row: dW is x_i d_j, rounded once, with D as db has it (a sum of one)."""
+    c = Case(1, m, k, "silu")
+    for keep, by in ((True, 0), (False, 1)):
+        got = run(c, keep, by)
+        check(c, got, keep)
+        assert torch.equal(got[2], dev(c.X).t() * got[3])
+
+
+@pytest.mark.parametrize("n", [1, 2, 7, 15, 16, 31, 32, 33])
+def test_weights_of_few_rows(n):
+    """Wide weights, and [A | U] and D by the products of many rows as well (16384 x 500): dW within the error of a chain of n float
+    multiplications and additions below 32 rows."""
+    for m, k in ((512, 600), (513, 515), (16384, 500)):
+        rng = np.random.default_rng(n)
+        f32 = lambda *s: rng.standard_normal(s).astype(np.float32)  # noqa: E731
+        X, W, dH = f32(n, m), f32(m, 2 * k), f32(n, k)
+        Z = np.concatenate([np.zeros((n, k), np.float32), np.ones((n, k), np.float32)], 1)
+        D = np.concatenate([dH / 4, dH / 2], 1)             # exactly: a = 0, U = 1, sigmoid
+        dW, end = space(m, 2 * k)
+        db, end2 = space(1, 2 * k)
+        dX = torch.empty(n, m, device="cuda")
+        ws = B.alloc(B.gnn_gated_workspace_bytes(True, n, m, k))
+        ws.fill_(255)
+        B.gnn_gated_bwd(GATES["sigmoid"], n, m, k, dev(X), dev(W), None, dev(Z), dev(dH), dW, db[0], dX, ws)
+        assert bool((end == 7.0).all()) and bool((end2 == 7.0).all())
+        terms = n if n < 32 else 8 * ((n + 15) // 16) + 8   # as above from there on
+        mag = np.abs(X).astype(np.float64).T @ np.abs(D)
+        within(dW, X.astype(np.float64).T @ D, terms * U * mag, "dW")
+        within(db[0], D.astype(np.float64).sum(0), terms * U * np.abs(D).sum(0), "db")
+        within(dX, D.astype(np.float64) @ W.astype(np.float64).T,
+               (8 * ((2 * k + 15) // 16) + 8) * U * (np.abs(D) @ np.abs(W).astype(np.float64).T), "dX")
