@@ -328,3 +328,100 @@ def test_weights_of_few_rows(n):
         within(db[0], D.astype(np.float64).sum(0), terms * U * np.abs(D).sum(0), "db")
         within(dX, D.astype(np.float64) @ W.astype(np.float64).T,
                (8 * ((2 * k + 15) // 16) + 8) * U * (np.abs(D) @ np.abs(W).astype(np.float64).T), "dX")
+
+
+def signs(rng, *shape):
+    return rng.choice(np.array([-1.0, 1.0], np.float32), shape)
+
+
+def twelve_bits(rng, *shape):
+    """Odd whole numbers of 2049 .. 4095 and either sign: twelve bits, of which one fp16 number holds eleven, so that each has a second
+    part.  Sums of 4096 of them times +-1 stay below 2^24, exact in float in any order."""
+    return (2 * rng.integers(1024, 2048, shape) + 1).astype(np.float32) * signs(rng, *shape)
+
+
+@pytest.mark.parametrize("n,m,k", [(33, 512, 600), (5000, 64, 64), (9000, 300, 515), (40000, 128, 256), (33000, 50, 30), (40001, 33, 65),
+                                   (2000, 512, 1000), (66001, 52, 68), (3000, 41, 1201), (100000, 40, 30), (32769, 67, 129)])
+def test_second_parts_of_the_rows_reach_every_sum(n, m, k):
+    """[A | U] = X W of whole numbers, gate columns zero: bit for bit as kept, and as formed again by what D sums up to: sixteen rows
+    to a column, other ones for each, so that the sums stay exact (below 2^22, in steps of 1 / 4)."""
+    rng = np.random.default_rng(n + m)
+    c = Case(n, m, k, "sigmoid", bias=False)
+    c.X = twelve_bits(rng, n, m)
+    c.W = np.concatenate([np.zeros((m, k), np.float32), signs(rng, m, k)], 1)
+    c.dH = np.zeros((n, k), np.float32)
+    c.dH[rng.integers(0, n, (16, k)), np.arange(k)] = 1.0
+    c.dH *= signs(rng, n, k)
+    U = c.X.astype(np.float64) @ c.W[:, k:].astype(np.float64)
+    kept, formed = run(c, True), run(c, False)
+    assert np.array_equal(host(kept[1]), np.concatenate([np.zeros((n, k)), U], 1))
+    for got in (kept, formed):
+        assert np.array_equal(host(got[0]), U / 2)
+        D = np.concatenate([c.dH * U / 4, c.dH / 2.0], 1)
+        assert np.abs(D).sum(0).max() < 2.0 ** 22
+        assert np.array_equal(host(got[3]), D.sum(0))
+        assert np.array_equal(host(got[4]), D[:, k:] @ c.W[:, k:].astype(np.float64).T)
+
+
+SECOND_PARTS = [(32, 512, 600), (33, 512, 600), (96, 512, 515), (200, 512, 1000), (4096, 300, 515), (4097, 300, 515), (9000, 300, 515),
+                (9001, 130, 1201), (40000, 128, 256), (33000, 50, 30), (220000, 40, 30), (66001, 52, 68), (3000, 40, 1200), (40000, 300, 30)]
+
+
+@pytest.mark.parametrize("n,m,k", SECOND_PARTS)
+@pytest.mark.parametrize("of_x", [True, False])
+def test_second_parts_reach_every_sum_of_the_gradients(n, m, k, of_x):
+    """dW = X^T D and dX = D W^T of whole numbers, D = [dH / 4 | dH / 2] by a kept Z of a = 0, U = 1: bit for bit, over chunks of
+    any number of steps, whichever of the operands has the second parts."""
+    rng = np.random.default_rng(n + m + k)
+    X, dH = (twelve_bits(rng, n, m), signs(rng, n, k)) if of_x else (signs(rng, n, m), twelve_bits(rng, n, k))
+    W = signs(rng, m, 2 * k)
+    Z = torch.cat([torch.zeros(n, k, device="cuda"), torch.ones(n, k, device="cuda")], 1)
+    dW, db, dX = space(m, 2 * k), space(1, 2 * k), space(n, m)
+    ws = B.alloc(B.gnn_gated_workspace_bytes(True, n, m, k))
+    ws.fill_(255)
+    B.gnn_gated_bwd(GATES["sigmoid"], n, m, k, dev(X), dev(W), None, Z, dev(dH), dW[0], db[0], dX[0], ws)
+    D = np.concatenate([dH / 4, dH / 2], 1).astype(np.float64)
+    assert np.array_equal(host(dW[0]), X.astype(np.float64).T @ D)
+    assert np.array_equal(host(db[0][0]), D.sum(0))
+    assert np.array_equal(host(dX[0]), D @ W.astype(np.float64).T)
+    for _, end in (dW, db, dX):
+        assert bool((end == 7.0).all())
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** 60])
+@pytest.mark.parametrize("n,k", [(20, 40), (3000, 40), (20000, 160), (45000, 160)])
+def test_gradients_of_magnitudes_far_from_one(n, k, scale):
+    """As above for X alone; a product or sum below 2^-126 may be taken as zero, each of which is worth that much at most."""
+    c = Case(n, 40, k, "sigmoid", bias=False, scale=scale)
+    c.dW_most = c.dW_most + n * 2.0 ** -126
+    c.db_most, c.dX_most = c.db_most + n * 2.0 ** -126, c.dX_most + 2 * k * 2.0 ** -126
+    for keep in (False, True):
+        check(c, run(c, keep), False)
+
+
+@pytest.mark.parametrize("n,m,k", [(2, 40, 32), (300, 512, 515), (4000, 32, 32), (40000, 40, 160), (60000, 40, 160), (9000, 300, 515),
+                                   (33000, 300, 12)])
+def test_infinite_sums_of_gradients_are_infinite(n, m, k):
+    """Positive operands, one infinity in X and one in dH: a row and two columns of dW, a row of dX and two sums are +inf, nothing is NaN
+    and the rest keeps its bounds."""
+    rng = np.random.default_rng(n)
+    pos = lambda *s: (0.5 + rng.random(s)).astype(np.float32)  # noqa: E731
+    X, W, dH = pos(n, m), pos(m, 2 * k), pos(n, k)
+    exact_D = np.concatenate([dH / 4, dH / 2], 1).astype(np.float64)
+    want_dW, want_db, want_dX = X.astype(np.float64).T @ exact_D, exact_D.sum(0), exact_D @ W.astype(np.float64).T
+    terms = 64 + 8 * ((min(n, 4096) + 15) // 16)
+    X[n // 2, 3] = np.inf
+    dH[n - 1, 5] = np.inf
+    Z = torch.cat([torch.zeros(n, k, device="cuda"), torch.ones(n, k, device="cuda")], 1)
+    dW, db, dX = (torch.full(s, NAN, device="cuda") for s in ((m, 2 * k), (2 * k,), (n, m)))
+    ws = B.alloc(B.gnn_gated_workspace_bytes(True, n, m, k))
+    B.gnn_gated_bwd(GATES["sigmoid"], n, m, k, dev(X), dev(W), None, Z, dev(dH), dW, db, dX, ws)
+    dW, db, dX = host(dW), host(db), host(dX)
+    inf_dW = np.zeros((m, 2 * k), bool)
+    inf_dW[3], inf_dW[:, [5, k + 5]] = True, True
+    assert np.array_equal(np.isposinf(dW), inf_dW) and np.isfinite(dW[~inf_dW]).all()
+    assert (np.abs(dW - want_dW) <= terms * U * want_dW)[~inf_dW].all()
+    assert np.isposinf(db[[5, k + 5]]).all() and np.isposinf(dX[n - 1]).all()
+    rest = np.delete(np.arange(2 * k), [5, k + 5])
+    assert (np.abs(db - want_db) <= terms * U * want_db)[rest].all()
+    assert (np.abs(dX - want_dX)[:-1] <= (8 * ((2 * k + 15) // 16) + 8) * U * want_dX[:-1]).all()
