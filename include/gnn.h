@@ -535,8 +535,12 @@ typedef enum { GNN_GATE_SIGMOID = 0, GNN_GATE_SILU = 1, GNN_GATE_GELU = 2 } gnn_
  *   Z [n, 2 f_out] or NULL: receives [A | U], which backward may read instead of forming it again.
  * gnn_gated_bwd - with D = [dH .* U .* act'(A) | dH .* act(A)]:  dW = X^T D [f_in, 2 f_out], db = D^T 1 [2 f_out] (NULL: not
  *   wanted), dX = D W^T [n, f_in] (NULL: not wanted).  Z as forward left it, or NULL: [A | U] is formed again from X, W and b.
- *   The products take three fp16 products of two parts per float (or fp32 products where rows are few): rounding errors are
- *   those of fp32 sums, for elements down to 2^-29 of the largest of their row or column; smaller ones are held to 2^-51 of it.
+ *   Sums are fp32 or better everywhere.  Products of many rows over 32 and more indices (f_in of them forward, 2 f_out in dX, n
+ *   in dW) take a float as two fp16 numbers: one is off by up to 8 u (u = 2^-24; a float product by u), and by an operand's
+ *   loss of 2^-50 of the largest of its row (of X, D) or column (of W; of X and D in dW, in chunks of 4096 rows), which shows where
+ *   operands lie below 2^-27 of it.  Root mean square errors are no larger than those of a chain of float multiplications and
+ *   additions.  Shorter products are those of floats.  Few rows: float products forward, gnn_gemm's for dX, doubles for dW, but for
+ *   dW of 2^19 elements and more the two fp16 numbers again, or floats below 32 rows.
  *   Outputs must not overlap inputs or each other.
  *   workspace: gnn_gated_workspace_bytes(backward, n, f_in, f_out), backward 0 or 1; what it returns does not fall as n grows.
  * Errors: INVALID_ARG (NULL X / W / H / dH / dW, negative n, f_in < 1 or f_out < 1, gate no gnn_gate_t, workspace NULL or not

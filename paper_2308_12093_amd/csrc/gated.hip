@@ -190,11 +190,13 @@ gated_gradient_kernel(long n, int k, int lanes, int rows, int parts, const float
 
 // the other kernels read four indices at a time, of f_in and of 2 f_out
 bool too_narrow(int64_t m, int64_t k) { return m < 4 || k < 2; }
-// Tiles of 32 x 32 of H up to which the kernels for few rows are the faster; their time goes with tiles times f_in, where the others
-// begin at five launches and 15 us, eight and 60 us backward.  Few rows / others in us, forward, with backward from Z:
-// 128000 x 8 -> 64, 8000 tiles, 26.9 / 30.8, 123 / 136; 176000, 11000, 35.3 / 33.8, 173 / 167; 16000 x 64 -> 256, 4000, 20.0 / 24.4,
-// 94 / 96; 24000, 6000, 27.6 / 26.5, 132 / 112; 32000 x 96 -> 96, 3000, 22.9 / 26.2, 99 / 96; 16000 x 128 -> 128, 2000, 19.3 / 20.6,
-// 87 / 85; 4000 x 256 -> 256, 1000, 19.8 / 21.7, 85 / 84; 1500, 26.6 / 23.8, 122 / 92; 1984 x 512 -> 512, 1000, 33.0 / 29.2, 123 / 100.
+// Tiles of 32 x 32 of H up to which the kernels for few rows are the faster, forward and back together; their time goes with tiles times
+// f_in, where the others begin at three launches forward (one below 32 features) and six or seven backward.  Few rows / others in us,
+// forward, with backward from Z: 40000 x 8 -> 64, 2500 tiles, 9.8 / 12.6, 54 / 76; 128000, 8000, 25.3 / 17.5, 119 / 120; 176000, 11000,
+// 34 / 26, 161 / 159; 16000 x 31 -> 256, 4000, 17.0 / 17.5, 82 / 84; 60000 x 40 -> 64, 3750, 17.8 / 22.0, 79 / 100; 120000, 7500, 32 /
+// 36, 138 / 140; 16000 x 64 -> 256, 4000, 20.7 / 21.9, 96 / 100; 24000, 6000, 29.3 / 25.7, 132 / 114; 32000 x 96 -> 96, 3000, 22.8 / 23.9,
+// 101 / 100; 16000 x 128 -> 128, 2000, 19.5 / 18.0, 89 / 91; 4000 x 256 -> 256, 1000, 18.2 / 18.8, 86 / 87; 6000, 1504, 26.5 / 21.3,
+// 125 / 93; 1500 x 512 -> 512, 752, 23.9 / 26.5, 98 / 99; 1984, 992, 32 / 27, 125 / 103.
 int64_t few_tiles(int64_t m) { return m < 32 ? 8000 : 260000 / m; }
 // Weights whose gradient is better off in float than through partial products of doubles and the pass over those, however few
 // the rows, forward and back, doubles / float: 1 x 512 -> 1024 57 / 27 us, 256 rows 75 / 63; half as many weights, 1 x 256 -> 512, 28

@@ -27,7 +27,7 @@ struct HalfOperand {
     long sk, sn;
 };
 
-// A product of two parts each is off by up to 7.4 u (u = 2^-24) where one of floats is by u at most, but is rounded less often on its way
+// A product of two parts each is off by up to 8 u (u = 2^-24) where one of floats is by u at most, but is rounded less often on its way
 // into the sum.  Root mean square of the errors of sums of K products of normal numbers, in u sqrt(K): parts 1.4 for K = 4 to 32, 1.5
 // for 64, 1.7 for 128; a chain of float multiplications and additions 0.7 for 4, 1.2 for 16, 1.5 for 24, 1.7 for 32, 3.4 for
 // 128.  So shorter reductions than this, one step of the kernels, are formed in float: [A | U] of the gated block on the

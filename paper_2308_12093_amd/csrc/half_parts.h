@@ -2,13 +2,17 @@
 //
 // A row of one operand and a column of the other are taken times a power of two each that brings their largest magnitude to
 // 2^14 .. 2^15, and every element is then the sum of two fp16 numbers, h + 2^-11 l: h rounds it to 11 bits and l rounds the
-// rest, times 2^11, to 11 bits.  What is left out is at most 2^-22 of the element, 2^-24.6 in the mean.  Products of two fp16
+// rest, times 2^11, to 11 bits.  What is left out is at most 2^-23 of the element, 2^-25.5 in the mean.  Products of two fp16
 // numbers are exact in float; three of the four are formed (l l, at most 2^-22 of the whole, is not) and added in float:
 // v_mfma_f32_32x32x16_f16 for h h, and for h l + l h into a sum of their own, which joins the other every 32 indices times 2^-11.
 // That is three instructions of 32 cycles for 16 indices, half of what three bf16 parts take (gemm_split.hip), a sixth of the
 // fp32 instruction's time.
 //
-// Elements below 2^-29 of their row's (column's) largest are held to 2^-51 of it.  The power of two is taken back exactly.
+// So a product is off by up to 8 u, 1.2 u in the root mean square, where one of floats is off by u = 2^-24 at most; sums of 32 and
+// more make up for it by their fewer roundings (kShortReduction in gemm_half.h).
+//
+// Small elements are held to 2^-50 of their row's (column's) largest, where that is more: l is no finer than 2^-25, 2^-36 of what it
+// stands for, beside 2^14 and more.  That begins at 2^-27 of the largest.  The power of two is taken back exactly.
 // Infinities and NaN are taken as they are and come out as NaN, upon which a wavefront forms its tile again with the fp32
 // instruction.
 #pragma once

@@ -425,3 +425,24 @@ def test_infinite_sums_of_gradients_are_infinite(n, m, k):
     rest = np.delete(np.arange(2 * k), [5, k + 5])
     assert (np.abs(db - want_db) <= terms * U * want_db)[rest].all()
     assert (np.abs(dX - want_dX)[:-1] <= (8 * ((2 * k + 15) // 16) + 8) * U * want_dX[:-1]).all()
+
+
+@pytest.mark.parametrize("n,k", [(50, 48), (3000, 700), (45000, 160)])
+def test_elements_far_below_the_largest_are_held_to_a_part_of_it(n, k):
+    """A feature, and below a row, of 2^40 that meets zeros: the others, of magnitude 1, are held to 2^-50 of it each.  Scaled by 2^-26 the
+    large one is 2^14; the second part, times 2^11, is rounded to a multiple of 2^-24, off by 2^-25: 2^-25 2^-11 2^26 = 2^-10."""
+    m, held = 40, 2.0 ** -10
+    c = Case(n, m, k, "sigmoid", bias=False)
+    c.X[:, 7], c.W[7] = 2.0 ** 40, 0.0
+    c.define()
+    _, Z, _, _, _ = run(c, True)
+    within(Z, c.Z, c.Z_most + held * np.abs(c.W).sum(0), "Z")
+    c = Case(n, m, k, "sigmoid", bias=False)
+    c.X[n // 3], c.dH[n // 3] = 2.0 ** 40, 0.0
+    Z = torch.cat([torch.zeros(n, k, device="cuda"), torch.ones(n, k, device="cuda")], 1)
+    dW, ws = torch.full((m, 2 * k), NAN, device="cuda"), B.alloc(B.gnn_gated_workspace_bytes(True, n, m, k))
+    B.gnn_gated_bwd(GATES["sigmoid"], n, m, k, dev(c.X), dev(c.W), None, Z, dev(c.dH), dW, None, None, ws)
+    D, X = np.concatenate([c.dH / 4, c.dH / 2], 1).astype(np.float64), c.X.astype(np.float64)
+    X[n // 3] = 0.0
+    C = 64 + 8 * ((min(n, 4096) + 15) // 16)
+    within(dW, X.T @ D, C * U * (np.abs(X).T @ np.abs(D)) + held * np.abs(D).sum(0), "dW")

@@ -469,3 +469,19 @@ def test_elu_backward_passes_nan_on(f):
     for got, ref in zip((dX, dg, db), want):
         assert np.array_equal(np.isnan(got), np.isnan(ref))
     assert np.isnan(db).all() and np.isnan(dX).any(1).sum() == 1
+
+
+@pytest.mark.parametrize("f", [5, 96, 203, 4100])
+def test_one_of_the_two_weights(f):
+    """gamma without beta and beta without gamma, each as if the other were ones or zeros."""
+    c = Case(33, f, "elu", 0.2)
+    X, dY, ws = dev(c.X), dev(c.dY), B.alloc(B.gnn_layer_norm_workspace_bytes(33, f))
+    for gamma, beta in ((dev(c.gamma), None), (None, dev(c.beta))):
+        results = []
+        for ga, be in ((gamma, beta), (torch.ones(f, device="cuda") if gamma is None else gamma,
+                                       torch.zeros(f, device="cuda") if beta is None else beta)):
+            Y, stat, dX, dg, db = (torch.full(s, NAN, device="cuda") for s in ((33, f), (33, 2), (33, f), (f,), (f,)))
+            B.gnn_layer_norm_fwd(33, f, X, ga, be, EPS, ACTS["elu"], c.drop, Y, stat)
+            B.gnn_layer_norm_bwd(33, f, X, stat, ga, be, ACTS["elu"], c.drop, dY, dX, dg, db, ws)
+            results.append((Y, stat, dX, dg, db))
+        assert all(torch.equal(a, b) for a, b in zip(*results))
