@@ -112,7 +112,8 @@ enum { kPlain, kGateForward, kGateBackward };
 // reads 16 consecutive floats of its row back and splits them.  A row's eight 16-byte pieces of a step lie in the order piece ^ (row / 2
 // mod 8), so that the reads of sixteen rows fall on different banks; whole lines are copied.  Rows read by the lanes themselves,
 // 16 bytes each, cost the L1 64 accesses an instruction instead of 8: 65536 x 512 x 2048 551 us, so 456, 300 TFLOP/s of the product and
-// 0.90 PFLOP/s on the instruction, at a clock that the power limit holds at 1.7 GHz (a library's bf16 product of these sizes: 0.82).
+// 0.90 PFLOP/s on the instruction (a library's bf16 product of these sizes: 0.82).  The clock falls to 1.66 GHz under it, where
+// kernels bound by memory run at 2.3, and the instruction is busy for 52 % of the cycles.
 // [A | U] of 65536 x 512 -> 1024, stored as well, 549 us; D of 2^17 x 128 -> 256 191 us, 0.47 GB in and out.
 // Each buffer is an array of its own: the compiler then knows which copies a read has to wait for.
 // GATE (gnn_gate_t) is known to the compiler: with all three in it the epilogue of 32 elements a lane outgrew the instruction cache

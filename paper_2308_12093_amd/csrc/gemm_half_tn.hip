@@ -7,7 +7,10 @@ namespace {
 using namespace half_parts;
 
 constexpr int64_t kChunkStep = 128;
-constexpr int64_t kMostRows = 4096;    // of a chunk, whose sums are in float; the chunks are added in double
+// Rows of a chunk.  Its sums are in float, rounded about twice per 32 rows, 256 times for 4096 of them, where a float chain
+// is 4096 times; the chunks are added in double.  In doubles throughout, as the layers' products of this form: 512 x 2048 over 65536
+// rows 2226 us where this takes 578.
+constexpr int64_t kMostRows = 4096;
 
 struct TnProduct {
     int M, N;
