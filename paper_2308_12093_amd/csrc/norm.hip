@@ -165,7 +165,8 @@ __device__ __forceinline__ void row_sums_of_pairs(float (&v)[2 * U], int lanes, 
 // well.  Far from zero one unit in the last place of m is as large as what rows of nearly equal values are normalised by, and
 // a sum over lanes divided by f misses the value of a row of f equal ones in a third of all cases.  Such a row's d are a few
 // units each, so the sums are exact; so is their quotient after the step behind the product with 1 / f: d - off and the variance
-// are zero, and m + off is the value.
+// are zero, and m + off is the value.  Forward forms xhat from d - off, backward from m + off rounded to a float, which is coarser far
+// from zero; with ReLU forward takes the coarser one as well, so that both see the same signs.
 __device__ __forceinline__ float rounded_mean(float sum, float inv_f) {
 #pragma clang fp contract(off)
     return sum * inv_f;                                    // not one with the subtraction that follows: d is exact so
@@ -259,7 +260,7 @@ norm_forward_kernel(Norm a) {
                 const float4 v = x[u][r];
                 const float d0 = c < f ? v.x - mean[u] : 0.f, d1 = c + 1 < f ? v.y - mean[u] : 0.f;
                 const float d2 = c + 2 < f ? v.z - mean[u] : 0.f, d3 = c + 3 < f ? v.w - mean[u] : 0.f;
-                x[u][r] = make_float4(d0, d1, d2, d3);
+                if constexpr (ACT != kActRelu) x[u][r] = make_float4(d0, d1, d2, d3);
                 s[2 * u] += (d0 + d1) + (d2 + d3);
                 s[2 * u + 1] += fmaf(d0, d0, d1 * d1) + fmaf(d2, d2, d3 * d3);
             }
@@ -267,14 +268,15 @@ norm_forward_kernel(Norm a) {
         row_sums_of_pairs<U, WIDE>(s, lanes, red);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float off = mean_off_by(s[2 * u], (float)f, inv_f);
+            const float off = mean_off_by(s[2 * u], (float)f, inv_f), whole = mean[u] + off;
             const float rstd = inverse_root(variance_and(a.eps, s[2 * u], s[2 * u + 1], off, inv_f));
+            const float less = ACT == kActRelu ? whole : off;      // x[u] is d but for ReLU
             if (row[u] >= (unsigned)a.n) continue;
-            if (gl == 0) *reinterpret_cast<floatx2u *>(a.stat + 2 * (size_t)row[u]) = floatx2u{mean[u] + off, rstd};
+            if (gl == 0) *reinterpret_cast<floatx2u *>(a.stat + 2 * (size_t)row[u]) = floatx2u{whole, rstd};
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int g = r * lanes + gl;
-                const float4 d = make_float4(x[u][r].x - off, x[u][r].y - off, x[u][r].z - off, x[u][r].w - off);
+                const float4 d = make_float4(x[u][r].x - less, x[u][r].y - less, x[u][r].z - less, x[u][r].w - less);
                 float4 y = make_float4(fmaf(d.x * rstd, ga[r].x, be[r].x), fmaf(d.y * rstd, ga[r].y, be[r].y),
                                        fmaf(d.z * rstd, ga[r].z, be[r].z), fmaf(d.w * rstd, ga[r].w, be[r].w));
                 if constexpr (!ADD) {
@@ -466,9 +468,10 @@ norm_forward_long_kernel(Norm a) {
     }
     differences = block_sum(differences, red);
     square = block_sum(square, red);
-    const float off = mean_off_by(differences, (float)f, inv_f);
+    const float off = mean_off_by(differences, (float)f, inv_f), whole = mean + off;
     const float rstd = inverse_root(variance_and(a.eps, differences, square, off, inv_f));
-    if (threadIdx.x == 0) { a.stat[2 * row] = mean + off; a.stat[2 * row + 1] = rstd; }
+    const float first = a.act == kActRelu ? whole : mean, then = a.act == kActRelu ? 0.f : off;
+    if (threadIdx.x == 0) { a.stat[2 * row] = whole; a.stat[2 * row + 1] = rstd; }
 #pragma unroll 2
     for (int c = 4 * threadIdx.x; c < f; c += 1024) {
         float z[4], ga[4], be[4];
@@ -476,7 +479,7 @@ norm_forward_long_kernel(Norm a) {
         weights4(a.gamma, c, f, 1.f, ga);
         weights4(a.beta, c, f, 0.f, be);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] = activation(fmaf(((z[j] - mean) - off) * rstd, ga[j], be[j]), a.act);
+        for (int j = 0; j < 4; ++j) z[j] = activation(fmaf(((z[j] - first) - then) * rstd, ga[j], be[j]), a.act);
         float4 y = make_float4(z[0], z[1], z[2], z[3]);
         if (!a.R) y = words.apply(y, (uint32_t)row, c / 4);
         store4(a.Y + row * f, c, f, y);

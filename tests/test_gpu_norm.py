@@ -485,3 +485,19 @@ def test_one_of_the_two_weights(f):
             B.gnn_layer_norm_bwd(33, f, X, stat, ga, be, ACTS["elu"], c.drop, dY, dX, dg, db, ws)
             results.append((Y, stat, dX, dg, db))
         assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("f", [48, 203, 256, 1024, 1030, 3000, 5003])
+def test_relu_backward_takes_every_sign_of_forward(f):
+    """Rows far from zero, where the mean's rounding is worth a hundredth of a deviation: of one row alone dbeta is dY where the
+    output is positive and 0 elsewhere, to the last column."""
+    rng = np.random.default_rng(f)
+    X = (rng.standard_normal((24, f)) * 2 + 3e5).astype(np.float32)
+    gamma, beta = dev((1 + rng.standard_normal(f) / 4).astype(np.float32)), dev((rng.standard_normal(f) / 4).astype(np.float32))
+    dY = dev((1 + rng.random((1, f))).astype(np.float32))
+    ws = B.alloc(B.gnn_layer_norm_workspace_bytes(1, f))
+    for i in range(24):
+        x, Y, stat, db = dev(X[i:i + 1]), torch.empty(1, f, device="cuda"), torch.empty(1, 2, device="cuda"), torch.empty(f, device="cuda")
+        B.gnn_layer_norm_fwd(1, f, x, gamma, beta, EPS, ACTS["relu"], None, Y, stat)
+        B.gnn_layer_norm_bwd(1, f, x, stat, gamma, beta, ACTS["relu"], None, dY, None, None, db, ws)
+        assert torch.equal(db, torch.where(Y[0] > 0, dY[0], torch.zeros_like(db)))
