@@ -544,9 +544,9 @@ typedef enum { GNN_GATE_SIGMOID = 0, GNN_GATE_SILU = 1, GNN_GATE_GELU = 2 } gnn_
  *   Outputs must not overlap inputs or each other.
  *   workspace: gnn_gated_workspace_bytes(backward, n, f_in, f_out), backward 0 or 1; what it returns does not fall as n grows.
  * Errors: INVALID_ARG (NULL X / W / H / dH / dW, negative n, f_in < 1 or f_out < 1, gate no gnn_gate_t, workspace NULL or not
- *   256-byte aligned), BUFFER_TOO_SMALL, UNSUPPORTED (f_in or f_out beyond 2^21; n, rounded up to a multiple of 32, times
- *   ceil(max(f_in, f_out) / 64) from 2^28 on; backward also (f_in + 1) f_out from 2^28 on, and 64 x 64 tiles of dW times n / 4096
- *   from 2^24 on).
+ *   256-byte aligned), BUFFER_TOO_SMALL, UNSUPPORTED (f_in or f_out beyond 2^21; ceil(n / 32) ceil(max(f_in, f_out) / 64) from 2^24
+ *   on, of f_in below 4 or f_out 1 ceil(n / 32) ceil(f_out / 32); backward also (f_in + 1) f_out from 2^28 on, and 64 x 64 tiles of
+ *   dW times n / 4096 from 2^24 on).
  */
 gnn_status_t gnn_gated_fwd(gnn_gate_t gate, int32_t n, int32_t f_in, int32_t f_out, const float *X, const float *W,
                            const float *b, float *H, float *Z, void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -222,8 +222,8 @@ gnn_status_t gradient(int64_t n, int k, int gate, const float *Z, const float *d
     const bool vec = k % 4 == 0 && aligned16(Z) && aligned16(dH);
     int lanes = 1;
     while (lanes < 64 && lanes * (vec ? 4 : 1) < k) lanes <<= 1;
-    const int rows = tops.cols ? top_rows(n) : 4 * (256 / lanes);
     *parts = (int)ceil_div(k, vec ? 256 : 64);
+    const int rows = tops.cols ? top_rows(n) : (int)free_rows(n, lanes, *parts);
     auto kernel = vec ? BY_GATE(gate, gated_gradient_kernel, 4) : BY_GATE(gate, gated_gradient_kernel, 1);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(n, rows) * *parts)), dim3(256), 0, st, (long)n, k, lanes, rows, *parts,
                        Z, dH, D, tops);
@@ -251,14 +251,13 @@ struct Backward {
 
 }  // namespace
 
-// A grid has less than 2^32 threads, 2^24 blocks of 256: the kernels for few rows take 32 x 32 elements of H a block, D and the
-// largest magnitudes are formed in blocks of 16 rows and 64 columns at least.  Both stay below it while there are less than 2^23
-// pieces of 32 x 64.
+// A grid has less than 2^32 threads, 2^24 blocks of 256: the kernels for few rows take 32 x 32 elements of H a block, columns' largest
+// magnitudes are formed in blocks of 32 rows and 64 columns at least.
 bool gated_fits(bool backward, int64_t n, int64_t m, int64_t k) {
     if (m > 1 << 21 || k > 1 << 21) return false;
-    const int64_t rows = ceil_div(n, 32), most = (int64_t)1 << 23;
+    const int64_t rows = ceil_div(n, 32), most = (int64_t)1 << 24;
     if (gated_few(n, m, k))
-        return rows * ceil_div(k, 64) < most && (!backward || (gemm_fits(n, m, 2 * k) && gemm_half_tn_fits(m, 2 * k, n)));
+        return rows * ceil_div(k, 32) < most && (!backward || (gemm_fits(n, m, 2 * k) && gemm_half_tn_fits(m, 2 * k, n)));
     return rows * ceil_div(m > k ? m : k, 64) < most && gemm_half_fits(n, 2 * k) &&
            (!backward || ((short_columns(k) ? gemm_fits(n, m, 2 * k) : gemm_half_fits(n, m)) && gemm_half_tn_fits(m, 2 * k, n)));
 }

@@ -21,6 +21,14 @@ static inline int64_t most_top_blocks(int64_t n) {
     return all > below ? all : below;
 }
 
+// Rows a block takes where only rows' largest magnitudes are wanted, or none: four for each group of lanes, and more where a grid
+// of these would have 2^24 blocks of 256 threads, which it cannot.
+static inline int64_t free_rows(int64_t n, int lanes, int64_t parts) {
+    int64_t rows = 4 * (256 / lanes);
+    while (ceil_div(n, rows) * parts >= (int64_t)1 << 24) rows *= 2;
+    return rows;
+}
+
 // columns of B as a product reads it: element (k, n) at k * sk + n * sn
 struct HalfOperand {
     const float *p;

@@ -531,8 +531,7 @@ gnn_status_t tops_launch(int64_t n, int m, const float *X, const Tops &tops, hip
     const bool vec = m % 4 == 0 && aligned16(X);
     int lanes = 1;
     while (lanes < 64 && lanes * (vec ? 4 : 1) < m) lanes <<= 1;
-    const int rows = tops.cols ? top_rows(n) : 4 * (256 / lanes);
-    const int parts = top_parts(m, X);
+    const int parts = top_parts(m, X), rows = tops.cols ? top_rows(n) : (int)free_rows(n, lanes, parts);
     hipLaunchKernelGGL(vec ? tops_kernel<4> : tops_kernel<1>, dim3((unsigned)(ceil_div(n, rows) * parts)), dim3(256), 0, st, (long)n,
                        m, lanes, rows, parts, X, tops);
     return launch_status();

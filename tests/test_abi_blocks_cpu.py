@@ -148,5 +148,6 @@ def test_gated_blocks_that_no_grid_covers_are_refused():
     # 32 x 32 elements of H a block: 256 x 65536
     for call in (gated, gated_backward):
         assert call(n=8176, m=3, k=1 << 21, nbytes=1 << 60) == no
-    # 16 rows and 64 columns of X a block, 65 columns are two: 8388608 x 2
-    assert gated(n=(1 << 27) - 1, m=65, k=64, nbytes=1 << 60) == no
+    # 32 rows and 64 columns of X a block, 65 columns are two: 8388608 x 2
+    for call in (gated, gated_backward):
+        assert call(n=1 << 28, m=65, k=64, nbytes=1 << 60) == no
