@@ -446,3 +446,28 @@ def test_elements_far_below_the_largest_are_held_to_a_part_of_it(n, k):
     X[n // 3] = 0.0
     C = 64 + 8 * ((min(n, 4096) + 15) // 16)
     within(dW, X.T @ D, C * U * (np.abs(X).T @ np.abs(D)) + held * np.abs(D).sum(0), "dW")
+
+
+@pytest.mark.parametrize("n,m,k", [(70000, 16, 160), (20, 512, 600), (40000, 260, 7), (33000, 31, 515)])
+def test_a_captured_step_of_short_products_replays(n, m, k):
+    test_a_captured_step_replays(n, m, k)
+
+
+@pytest.mark.parametrize("n,m,k", [(70000, 16, 160), (1, 513, 514), (33000, 31, 515), (31, 512, 600)])
+def test_short_products_pass_on_what_is_not_finite(n, m, k):
+    """An infinite or NaN input spoils its row of H, a NaN gradient the weights that it meets; all else keeps its bounds."""
+    c = Case(n, m, k, "silu")
+    keep_X = c.X
+    c.X = keep_X.copy()
+    c.X[n - 1, 0] = np.nan
+    H = host(run(c, False)[0])
+    c.X = keep_X
+    assert np.isnan(H[n - 1]).all() and (np.abs(H - c.H) <= c.H_most)[:n - 1].all()
+    keep_dH = c.dH
+    c.dH = keep_dH.copy()
+    c.dH[0, 3] = np.nan
+    dW, db = (host(t) for t in run(c, True)[2:4])
+    c.dH = keep_dH
+    rest = [j for j in range(2 * k) if j % k != 3]
+    assert np.isnan(dW[:, [3, k + 3]]).all() and np.isnan(db[[3, k + 3]]).all()
+    assert (np.abs(dW - c.dW) <= c.dW_most)[:, rest].all()
