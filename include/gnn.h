@@ -487,7 +487,10 @@ gnn_status_t gnn_rng_advance(uint64_t *state, uint64_t by, void *hip_stream);
 gnn_status_t gnn_dropout(int32_t n, int32_t f, const float *X, const float *R, const gnn_dropout_t *drop, float *Y,
                          void *hip_stream);
 
-typedef enum { GNN_ACT_NONE = 0, GNN_ACT_RELU = 1, GNN_ACT_ELU = 2 } gnn_act_t;
+/* ELU with alpha = 1; the last three are those of gnn_gate_t, for the products below (gnn_linear_..): a layer norm takes the first three. */
+typedef enum {
+    GNN_ACT_NONE = 0, GNN_ACT_RELU = 1, GNN_ACT_ELU = 2, GNN_ACT_SIGMOID = 3, GNN_ACT_SILU = 4, GNN_ACT_GELU = 5
+} gnn_act_t;
 
 /*
  * gnn_layer_norm_fwd - Y = dropout(act(gamma xhat + beta)), xhat = (x - mean) rstd over the f columns of a row,
@@ -554,6 +557,95 @@ gnn_status_t gnn_gated_bwd(gnn_gate_t gate, int32_t n, int32_t f_in, int32_t f_o
                            const float *b, const float *Z, const float *dH, float *dW, float *db, float *dX,
                            void *workspace, size_t workspace_bytes, void *hip_stream);
 size_t gnn_gated_workspace_bytes(int32_t backward, int32_t n, int32_t f_in, int32_t f_out);
+
+/* ---- rows in 8 bits; root-mean-square norm; products with their epilogue ---- */
+
+/*
+ * gnn_rows8_t - an [n, f] array held in 8 bits, a scale for each row: a HOST struct of device arrays.
+ *   q        integers from -127 to 127, rows gnn_rows8_stride(f) bytes apart (f rounded up to a multiple of 16); 16-byte aligned.  The
+ *            bytes behind a row's f may hold anything
+ *   scale    [n]
+ *   columns  [f], or NULL: all ones.  Read where the array is an input that says so
+ * Element (i, c) is q[i][c] * scale[i] * columns[c].
+ */
+typedef struct {
+    int8_t *q;
+    float *scale;
+    const float *columns;
+} gnn_rows8_t;
+int64_t gnn_rows8_stride(int32_t f);
+
+/*
+ * gnn_quantize_rows - out = X .* columns in 8 bits.  X [n, f], columns [f] or NULL.  With x a row of X .* columns and a its largest
+ *   magnitude: q = round(x * (127 / a)), ties to even, scale = a / 127; the product with columns, the quotients and the product are each
+ *   rounded to a float (with the exponent range of one extended below, so that rows of the least floats keep their digits; a scale
+ *   below the least normal float does not).  An element is off by at most (0.5 + 127 x 2^-23) scale.  A row of zeros has scale 0; a
+ *   row with an infinity or a NaN in it has integers 0 and scale NaN, so that every element of it is NaN.  out->columns has to be NULL.
+ * gnn_dequantize_rows - Y [n, f] = the elements of `in`, in->columns included.
+ * Errors: INVALID_ARG (NULL X / Y / struct / q / scale, q not 16-byte aligned, out->columns not NULL, negative n, f < 1), UNSUPPORTED
+ *   (f beyond 2^24, or 2^24 rows and more of f beyond 4096).
+ */
+gnn_status_t gnn_quantize_rows(int32_t n, int32_t f, const float *X, const float *columns, const gnn_rows8_t *out, void *hip_stream);
+gnn_status_t gnn_dequantize_rows(int32_t n, int32_t f, const gnn_rows8_t *in, float *Y, void *hip_stream);
+
+/*
+ * gnn_rms_norm_fwd - H = R + dropout(X), Y = gamma xhat with xhat = h rstd, rstd = 1 / sqrt(mean of h^2 over the f columns + eps).
+ *   X, R, H, Y [n, f]; gamma [f] or NULL (1).  R NULL: H is X, and H and drop have to be NULL (or p = 0).  H may be X or R; Y may be X where
+ *   R is NULL.
+ *   xhat8 or NULL: receives xhat (without gamma) in 8 bits.  Its integers are those of H (gnn_quantize_rows), its scale that of H times
+ *   rstd.  gnn_rms_norm_bwd reads them instead of H; with `columns` set to gamma the same rows are Y, for gnn_linear_bwd.
+ *   Y NULL: not wanted (xhat8 is then).  rstd_out [n] or NULL: for backward.
+ *   A row whose squares add up to more than the largest float has xhat = 0.
+ * gnn_rms_norm_bwd - dR = dH + rstd (g - xhat mean(g xhat)) with g = gamma dY, dX = dropout(dR), dgamma = sum over the rows of dY xhat;
+ *   any of them may be NULL.  dH [n, f] is what flows back into H from elsewhere, NULL: nothing.  xhat from H and rstd, or from xhat8
+ *   (whose columns are not read): one of them is NULL.  dR and dX may each be dY or dH, but not the same array.  The sums over the rows
+ *   have a fixed order.
+ *   workspace: gnn_rms_norm_workspace_bytes(n, f), which does not fall as n grows; not used where dgamma is NULL (then it may be NULL).
+ * Errors: INVALID_ARG (NULL X; with R NULL H or a dropout, with R H NULL or Y; Y and xhat8 both NULL; a bad xhat8 as in
+ *   gnn_quantize_rows; backward: NULL rstd / dY, H and xhat8 both or neither; dR == dX; negative n, f < 1, eps below the least normal
+ *   float or not finite, drop as in gnn_dropout, workspace NULL or not 256-byte aligned), BUFFER_TOO_SMALL, UNSUPPORTED (as
+ *   gnn_quantize_rows).
+ */
+gnn_status_t gnn_rms_norm_fwd(int32_t n, int32_t f, const float *X, const float *R, const gnn_dropout_t *drop, const float *gamma,
+                              float eps, float *H, float *Y, const gnn_rows8_t *xhat8, float *rstd_out, void *hip_stream);
+gnn_status_t gnn_rms_norm_bwd(int32_t n, int32_t f, const float *H, const gnn_rows8_t *xhat8, const float *rstd, const float *gamma,
+                              const gnn_dropout_t *drop, const float *dY, const float *dH, float *dR, float *dX, float *dgamma,
+                              void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t gnn_rms_norm_workspace_bytes(int32_t n, int32_t f);
+
+/*
+ * gnn_linear_fwd - Y = act(Z) + R, Z = X W + 1 b^T.  X [n, f_in], W [f_in, f_out], b [f_out] or NULL, R [n, f_out] or NULL, Y [n, f_out].
+ *   Z [n, f_out] or NULL: receives X W + b, which backward may read instead of forming it again.  Y may be R.
+ * gnn_linear_bwd - with D = dY .* act'(Z):  dW = X^T D [f_in, f_out], db = D^T 1 [f_out] (NULL: not wanted), dX = D W^T [n, f_in] (NULL: not
+ *   wanted).  (The gradient of R is dY.)  ReLU' = 0 at 0.
+ *   X, or X8: the rows in 8 bits, columns included; one of them is NULL.
+ *   Z as forward left it, or Z8: the same in 8 bits, columns included, or neither: Z is formed again from X, W and b, and X8 will not do.
+ *   GNN_ACT_NONE reads neither of them.
+ *   Sums and their operands are as in gnn_gated_fwd / _bwd, f_out in place of 2 f_out.  From X8 they are as exact: an integer is one fp16
+ *   number, and its row's scale goes to the row of D.
+ *   Outputs must not overlap inputs or each other, but for Y and R.
+ *   workspace: gnn_linear_workspace_bytes(backward, n, f_in, f_out), backward 0 or 1; what it returns does not fall as n grows.
+ * Errors: INVALID_ARG (NULL X / W / Y / dY / dW, X and X8 both or neither, Z and Z8 both, X8 without Z or Z8 where act is not
+ *   GNN_ACT_NONE, q not 16-byte aligned or NULL, scale NULL, negative n, f_in < 1 or f_out < 1, act no gnn_act_t, workspace NULL or not
+ *   256-byte aligned), BUFFER_TOO_SMALL, UNSUPPORTED (as gnn_gated_fwd / _bwd, f_out in place of 2 f_out).
+ */
+gnn_status_t gnn_linear_fwd(gnn_act_t act, int32_t n, int32_t f_in, int32_t f_out, const float *X, const float *W, const float *b,
+                            const float *R, float *Y, float *Z, void *workspace, size_t workspace_bytes, void *hip_stream);
+gnn_status_t gnn_linear_bwd(gnn_act_t act, int32_t n, int32_t f_in, int32_t f_out, const float *X, const gnn_rows8_t *X8,
+                            const float *W, const float *b, const float *Z, const gnn_rows8_t *Z8, const float *dY, float *dW,
+                            float *db, float *dX, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t gnn_linear_workspace_bytes(int32_t backward, int32_t n, int32_t f_in, int32_t f_out);
+
+/*
+ * gnn_linear8_fwd - Y = act(X W^T + 1 b^T) + R of two arrays in 8 bits: X [n, f_in], W [f_out, f_in], a row for each column of Y (gnn_quantize_rows
+ *   of the transposed weights, once); b [f_out] or NULL, R and Y [n, f_out], R or NULL.  The sums over f_in are of integers and exact.
+ *   Behind an RMS norm X is its xhat8, and gamma goes into the weights (gnn_quantize_rows' columns): both `columns` have to be NULL here.
+ *   Y may be R.  No workspace.
+ * Errors: INVALID_ARG (NULL Y, X or W or one of their arrays, columns not NULL, q not 16-byte aligned, negative n, f_in < 1 or f_out < 1, act
+ *   no gnn_act_t), UNSUPPORTED (f_in beyond 2^17, whose sums 32 bits hold, f_out beyond 2^21, ceil(n / 32) ceil(f_out / 32) from 2^24 on).
+ */
+gnn_status_t gnn_linear8_fwd(gnn_act_t act, int32_t n, int32_t f_in, int32_t f_out, const gnn_rows8_t *X, const gnn_rows8_t *W,
+                             const float *b, const float *R, float *Y, void *hip_stream);
 
 const char *gnn_status_string(gnn_status_t status);
 

@@ -98,3 +98,55 @@ def gated_backward(X, W, Z, dH, kind):
     D = np.concatenate([dH * Z[:, k:] * da, dH * a], axis=1)
     X, W = np.asarray(X, dtype=np.float64), np.asarray(W, dtype=np.float64)
     return X.T @ D, D.sum(axis=0), D @ W.T, D
+
+
+def held8(X, columns=None):
+    """(q, a / 127): a row of X .* columns in 8 bits.  The integers are defined by operations rounded to float32, with an exponent range
+    without end (rows below 2^-100 are taken times 2^64)."""
+    x = np.asarray(X, dtype=np.float32)
+    if columns is not None:
+        x = x * np.asarray(columns, dtype=np.float32)
+    top = np.abs(x).max(axis=1, keepdims=True)
+    up = np.where(top < np.float32(2.0 ** -100), np.float32(2.0 ** 64), np.float32(1.0))
+    a = top * up
+    with np.errstate(divide="ignore", invalid="ignore"):
+        per_unit = np.where(top > 0, np.float32(127.0) / a, np.float32(0.0))
+        q = np.rint(x * up * per_unit)
+    q = np.where(np.isfinite(top), q, 0.0)
+    scale = np.where(np.isfinite(top), top.astype(np.float64) / 127.0, np.nan)[:, 0]
+    return q.astype(np.int8), scale
+
+
+def rms_norm(H, eps):
+    """(xhat, rstd [n, 1])."""
+    H = np.asarray(H, dtype=np.float64)
+    rstd = 1.0 / np.sqrt((H ** 2).mean(axis=1, keepdims=True) + eps)
+    return H * rstd, rstd
+
+
+def rms_norm_backward(xhat, rstd, gamma, dY):
+    """(gradient with respect to H, dgamma)."""
+    dY = np.asarray(dY, dtype=np.float64)
+    g = dY * np.asarray(gamma, dtype=np.float64)
+    return rstd * (g - xhat * (g * xhat).mean(axis=1, keepdims=True)), (dY * xhat).sum(axis=0)
+
+
+def act(kind, z):
+    """An activation of the products and its derivative."""
+    return gate(kind, z) if kind in ("sigmoid", "silu", "gelu") else _activation(z, kind)
+
+
+def linear_forward(X, W, b, kind, R=None):
+    """(Y, Z): act(Z) + R and Z = X W + b."""
+    Z = np.asarray(X, dtype=np.float64) @ np.asarray(W, dtype=np.float64)
+    if b is not None:
+        Z = Z + np.asarray(b, dtype=np.float64)
+    Y = act(kind, Z)[0]
+    return Y if R is None else Y + np.asarray(R, dtype=np.float64), Z
+
+
+def linear_backward(X, W, Z, dY, kind):
+    """(dW, db, dX, D)."""
+    D = np.asarray(dY, dtype=np.float64) * act(kind, Z)[1]
+    X, W = np.asarray(X, dtype=np.float64), np.asarray(W, dtype=np.float64)
+    return X.T @ D, D.sum(axis=0), D @ W.T, D

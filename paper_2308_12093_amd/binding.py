@@ -34,7 +34,7 @@ GNN_BWD_AUTO, GNN_BWD_FUSED_PROPAGATE, GNN_BWD_SPLIT_PROPAGATE = 0, 1, 2
  GNN_CACHE_GAT_FEAT_EDGE) = range(6)
 GNN_SELECT_PAPER_RULE, GNN_SELECT_CALIBRATED = 0, 1
 GNN_AGG_GCN_SYM, GNN_AGG_MEAN, GNN_AGG_GIN_SUM = 0, 1, 2
-GNN_ACT_NONE, GNN_ACT_RELU, GNN_ACT_ELU = 0, 1, 2
+GNN_ACT_NONE, GNN_ACT_RELU, GNN_ACT_ELU, GNN_ACT_SIGMOID, GNN_ACT_SILU, GNN_ACT_GELU = range(6)
 GNN_GATE_SIGMOID, GNN_GATE_SILU, GNN_GATE_GELU = 0, 1, 2
 
 _vp = ctypes.c_void_p
@@ -68,6 +68,11 @@ class gnn_dropout_t(ctypes.Structure):
     _fields_ = [("p", ctypes.c_float), ("site", ctypes.c_uint32), ("state", _vp)]
 
 
+class gnn_rows8_t(ctypes.Structure):
+    _fields_ = [("q", _vp), ("scale", _vp), ("columns", _vp)]
+
+
+_ROWS8 = ctypes.POINTER(gnn_rows8_t)
 _BUFS = [_vp, _sz, _vp, _sz, _vp]
 # every symbol the header declares, with its prototype
 _PROTOS = {
@@ -122,6 +127,17 @@ _PROTOS = {
     "gnn_gated_fwd": (ctypes.c_int, [ctypes.c_int, _i32, _i32, _i32] + [_vp] * 6 + [_sz, _vp]),
     "gnn_gated_bwd": (ctypes.c_int, [ctypes.c_int, _i32, _i32, _i32] + [_vp] * 9 + [_sz, _vp]),
     "gnn_gated_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32]),
+    "gnn_rows8_stride": (_i64, [_i32]),
+    "gnn_quantize_rows": (ctypes.c_int, [_i32, _i32, _vp, _vp, _ROWS8, _vp]),
+    "gnn_dequantize_rows": (ctypes.c_int, [_i32, _i32, _ROWS8, _vp, _vp]),
+    "gnn_rms_norm_fwd": (ctypes.c_int, [_i32, _i32, _vp, _vp, ctypes.POINTER(gnn_dropout_t), _vp, ctypes.c_float, _vp, _vp, _ROWS8,
+                                        _vp, _vp]),
+    "gnn_rms_norm_bwd": (ctypes.c_int, [_i32, _i32, _vp, _ROWS8, _vp, _vp, ctypes.POINTER(gnn_dropout_t)] + [_vp] * 6 + [_sz, _vp]),
+    "gnn_rms_norm_workspace_bytes": (_sz, [_i32, _i32]),
+    "gnn_linear_fwd": (ctypes.c_int, [ctypes.c_int, _i32, _i32, _i32] + [_vp] * 7 + [_sz, _vp]),
+    "gnn_linear_bwd": (ctypes.c_int, [ctypes.c_int, _i32, _i32, _i32, _vp, _ROWS8, _vp, _vp, _vp, _ROWS8] + [_vp] * 5 + [_sz, _vp]),
+    "gnn_linear_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32]),
+    "gnn_linear8_fwd": (ctypes.c_int, [ctypes.c_int, _i32, _i32, _i32, _ROWS8, _ROWS8, _vp, _vp, _vp, _vp]),
 }
 EXPORTS = tuple(_PROTOS)
 for _name, (_res, _args) in _PROTOS.items():
@@ -445,3 +461,68 @@ def gnn_gated_fwd(gate, n, f_in, f_out, X, W, b, H, Z, workspace):
 def gnn_gated_bwd(gate, n, f_in, f_out, X, W, b, Z, dH, dW, db, dX, workspace):
     _check(lib.gnn_gated_bwd(int(gate), n, f_in, f_out, _ptr(X), _ptr(W), _ptr(b), _ptr(Z), _ptr(dH), _ptr(dW), _ptr(db),
                              _ptr(dX), _ptr(workspace), _nbytes(workspace), _stream()), "gnn_gated_bwd")
+
+
+# ---- rows in 8 bits; root-mean-square norm; products with their epilogue ------------------
+class Rows8:
+    """A ``gnn_rows8_t`` and the device tensors it points to: ``q`` int8 [n, gnn_rows8_stride(f)], ``scale`` float32 [n],
+    ``columns`` float32 [f] or None."""
+
+    def __init__(self, q, scale, columns=None):
+        self.q, self.scale, self.columns = q, scale, columns
+        self.c = gnn_rows8_t(_ptr(q), _ptr(scale), _ptr(columns))
+
+
+def _rows8(rows):
+    return None if rows is None else ctypes.byref(rows.c)
+
+
+def gnn_rows8_stride(f) -> int:
+    return lib.gnn_rows8_stride(f)
+
+
+def alloc_rows8(n, f, device="cuda"):
+    """Room for an [n, f] array in 8 bits (torch owns the memory)."""
+    return Rows8(torch.empty((n, gnn_rows8_stride(f)), dtype=torch.int8, device=device),
+                 torch.empty(n, dtype=torch.float32, device=device))
+
+
+def gnn_quantize_rows(n, f, X, columns, out):
+    _check(lib.gnn_quantize_rows(n, f, _ptr(X), _ptr(columns), _rows8(out), _stream()), "gnn_quantize_rows")
+
+
+def gnn_dequantize_rows(n, f, rows, Y):
+    _check(lib.gnn_dequantize_rows(n, f, _rows8(rows), _ptr(Y), _stream()), "gnn_dequantize_rows")
+
+
+def gnn_rms_norm_workspace_bytes(n, f):
+    return lib.gnn_rms_norm_workspace_bytes(n, f)
+
+
+def gnn_rms_norm_fwd(n, f, X, R, drop, gamma, eps, H, Y, xhat8, rstd_out):
+    _check(lib.gnn_rms_norm_fwd(n, f, _ptr(X), _ptr(R), _drop(drop), _ptr(gamma), float(eps), _ptr(H), _ptr(Y), _rows8(xhat8),
+                                _ptr(rstd_out), _stream()), "gnn_rms_norm_fwd")
+
+
+def gnn_rms_norm_bwd(n, f, H, xhat8, rstd, gamma, drop, dY, dH, dR, dX, dgamma, workspace):
+    _check(lib.gnn_rms_norm_bwd(n, f, _ptr(H), _rows8(xhat8), _ptr(rstd), _ptr(gamma), _drop(drop), _ptr(dY), _ptr(dH), _ptr(dR),
+                                _ptr(dX), _ptr(dgamma), _ptr(workspace), _nbytes(workspace), _stream()), "gnn_rms_norm_bwd")
+
+
+def gnn_linear_workspace_bytes(backward, n, f_in, f_out):
+    return lib.gnn_linear_workspace_bytes(int(backward), n, f_in, f_out)
+
+
+def gnn_linear_fwd(act, n, f_in, f_out, X, W, b, R, Y, Z, workspace):
+    _check(lib.gnn_linear_fwd(int(act), n, f_in, f_out, _ptr(X), _ptr(W), _ptr(b), _ptr(R), _ptr(Y), _ptr(Z), _ptr(workspace),
+                              _nbytes(workspace), _stream()), "gnn_linear_fwd")
+
+
+def gnn_linear_bwd(act, n, f_in, f_out, X, X8, W, b, Z, Z8, dY, dW, db, dX, workspace):
+    _check(lib.gnn_linear_bwd(int(act), n, f_in, f_out, _ptr(X), _rows8(X8), _ptr(W), _ptr(b), _ptr(Z), _rows8(Z8), _ptr(dY),
+                              _ptr(dW), _ptr(db), _ptr(dX), _ptr(workspace), _nbytes(workspace), _stream()), "gnn_linear_bwd")
+
+
+def gnn_linear8_fwd(act, n, f_in, f_out, X, W, b, R, Y):
+    _check(lib.gnn_linear8_fwd(int(act), n, f_in, f_out, _rows8(X), _rows8(W), _ptr(b), _ptr(R), _ptr(Y), _stream()),
+           "gnn_linear8_fwd")

@@ -5,6 +5,7 @@
 
 #include "dropout.h"
 #include "plan.h"
+#include "rows8.h"
 
 using namespace gnn;
 
@@ -70,6 +71,24 @@ gnn_status_t check_gated_workspace(bool backward, int32_t n, int32_t f_in, int32
     if (!gated_fits(backward, n, f_in, f_out)) return GNN_ERR_UNSUPPORTED;
     if (!workspace || bad_align(workspace)) return GNN_ERR_INVALID_ARG;
     return workspace_bytes < gated_workspace_bytes(backward, n, f_in, f_out) ? GNN_ERR_BUFFER_TOO_SMALL : GNN_OK;
+}
+
+bool bad_act(int act) { return act < GNN_ACT_NONE || act > GNN_ACT_GELU; }
+
+// a caller's rows in 8 bits as the kernels take them; NULL: none
+gnn_status_t take_rows8(const gnn_rows8_t *rows, bool columns, Rows8 *out) {
+    *out = no_rows8();
+    if (!rows) return GNN_OK;
+    if (!rows->q || !rows->scale || !aligned16(rows->q) || (rows->columns && !columns)) return GNN_ERR_INVALID_ARG;
+    *out = Rows8{rows->q, rows->scale, rows->columns};
+    return GNN_OK;
+}
+
+gnn_status_t check_linear_workspace(bool backward, int32_t n, int32_t f_in, int32_t f_out, const void *workspace,
+                                    size_t workspace_bytes) {
+    if (!linear_fits(backward, n, f_in, f_out)) return GNN_ERR_UNSUPPORTED;
+    if (!workspace || bad_align(workspace)) return GNN_ERR_INVALID_ARG;
+    return workspace_bytes < linear_workspace_bytes(backward, n, f_in, f_out) ? GNN_ERR_BUFFER_TOO_SMALL : GNN_OK;
 }
 
 }  // namespace
@@ -518,6 +537,105 @@ gnn_status_t gnn_gated_bwd(gnn_gate_t gate, int32_t n, int32_t f_in, int32_t f_o
     if (n > 0 && (!X || !W || !dH)) return GNN_ERR_INVALID_ARG;
     GNN_TRY(check_gated_workspace(true, n, f_in, f_out, workspace, workspace_bytes));
     return gated_backward_launch(gate, n, f_in, f_out, X, W, b, Z, dH, dW, db, dX, workspace, as_stream(hip_stream));
+}
+
+// ---- rows in 8 bits; root-mean-square norm; products with their epilogue -----------------
+
+int64_t gnn_rows8_stride(int32_t f) { return rows8_stride(f > 0 ? f : 1); }
+
+gnn_status_t gnn_quantize_rows(int32_t n, int32_t f, const float *X, const float *columns, const gnn_rows8_t *out, void *hip_stream) {
+    Rows8 rows;
+    if (n < 0 || f <= 0) return GNN_ERR_INVALID_ARG;
+    if (n == 0) return GNN_OK;
+    if (!X || !out) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_rows8(out, false, &rows));
+    if (!norm_fits(n, f)) return GNN_ERR_UNSUPPORTED;
+    return quantize_rows_launch(n, f, X, columns, rows, as_stream(hip_stream));
+}
+
+gnn_status_t gnn_dequantize_rows(int32_t n, int32_t f, const gnn_rows8_t *in, float *Y, void *hip_stream) {
+    Rows8 rows;
+    if (n < 0 || f <= 0) return GNN_ERR_INVALID_ARG;
+    if (n == 0) return GNN_OK;
+    if (!in || !Y) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_rows8(in, true, &rows));
+    if (!norm_fits(n, f)) return GNN_ERR_UNSUPPORTED;
+    return dequantize_rows_launch(n, f, rows, Y, as_stream(hip_stream));
+}
+
+size_t gnn_rms_norm_workspace_bytes(int32_t n, int32_t f) { return rms_norm_workspace_bytes(n > 0 ? n : 0, f > 0 ? f : 1); }
+
+gnn_status_t gnn_rms_norm_fwd(int32_t n, int32_t f, const float *X, const float *R, const gnn_dropout_t *drop, const float *gamma,
+                              float eps, float *H, float *Y, const gnn_rows8_t *xhat8, float *rstd_out, void *hip_stream) {
+    Dropout d;
+    Rows8 rows;
+    if (n < 0 || f <= 0 || bad_eps(eps)) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_dropout(drop, &d));
+    if (n == 0) return GNN_OK;
+    if (!X || (!Y && !xhat8)) return GNN_ERR_INVALID_ARG;
+    if (R ? !H || H == Y : H || d.below) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_rows8(xhat8, false, &rows));
+    if (!norm_fits(n, f)) return GNN_ERR_UNSUPPORTED;
+    return rms_norm_forward_launch(n, f, X, R, d, gamma, eps, H, Y, rows, rstd_out, as_stream(hip_stream));
+}
+
+gnn_status_t gnn_rms_norm_bwd(int32_t n, int32_t f, const float *H, const gnn_rows8_t *xhat8, const float *rstd, const float *gamma,
+                              const gnn_dropout_t *drop, const float *dY, const float *dH, float *dR, float *dX, float *dgamma,
+                              void *workspace, size_t workspace_bytes, void *hip_stream) {
+    Dropout d;
+    Rows8 rows = no_rows8();
+    if (n < 0 || f <= 0) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_dropout(drop, &d));
+    if (n > 0) {
+        if ((H != nullptr) == (xhat8 != nullptr) || !rstd || !dY || (dR && dR == dX)) return GNN_ERR_INVALID_ARG;
+        GNN_TRY(take_rows8(xhat8, true, &rows));
+    }
+    if (!norm_fits(n, f)) return GNN_ERR_UNSUPPORTED;
+    if (dgamma) {
+        if (!workspace || bad_align(workspace)) return GNN_ERR_INVALID_ARG;
+        if (workspace_bytes < rms_norm_workspace_bytes(n, f)) return GNN_ERR_BUFFER_TOO_SMALL;
+    }
+    return rms_norm_backward_launch(n, f, H, rows, rstd, gamma, d, dY, dH, dR, dX, dgamma, workspace, as_stream(hip_stream));
+}
+
+size_t gnn_linear_workspace_bytes(int32_t backward, int32_t n, int32_t f_in, int32_t f_out) {
+    return linear_workspace_bytes(backward != 0, n > 0 ? n : 1, f_in > 0 ? f_in : 1, f_out > 0 ? f_out : 1);
+}
+
+gnn_status_t gnn_linear_fwd(gnn_act_t act, int32_t n, int32_t f_in, int32_t f_out, const float *X, const float *W, const float *b,
+                            const float *R, float *Y, float *Z, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (bad_act(act) || n < 0 || f_in <= 0 || f_out <= 0) return GNN_ERR_INVALID_ARG;
+    if (n == 0) return GNN_OK;
+    if (!X || !W || !Y || Y == Z) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(check_linear_workspace(false, n, f_in, f_out, workspace, workspace_bytes));
+    return linear_forward_launch(act, n, f_in, f_out, X, W, b, R, Y, Z, workspace, as_stream(hip_stream));
+}
+
+gnn_status_t gnn_linear_bwd(gnn_act_t act, int32_t n, int32_t f_in, int32_t f_out, const float *X, const gnn_rows8_t *X8,
+                            const float *W, const float *b, const float *Z, const gnn_rows8_t *Z8, const float *dY, float *dW,
+                            float *db, float *dX, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    Rows8 x8 = no_rows8(), z8 = no_rows8();
+    if (bad_act(act) || n < 0 || f_in <= 0 || f_out <= 0 || !dW) return GNN_ERR_INVALID_ARG;
+    if (n > 0) {
+        if ((X != nullptr) == (X8 != nullptr) || (Z && Z8) || !W || !dY) return GNN_ERR_INVALID_ARG;
+        if (X8 && !Z && !Z8 && act != GNN_ACT_NONE) return GNN_ERR_INVALID_ARG;
+        GNN_TRY(take_rows8(X8, true, &x8));
+        GNN_TRY(take_rows8(Z8, true, &z8));
+    }
+    GNN_TRY(check_linear_workspace(true, n, f_in, f_out, workspace, workspace_bytes));
+    return linear_backward_launch(act, n, f_in, f_out, X, x8, W, b, Z, z8, dY, dW, db, dX, workspace, as_stream(hip_stream));
+}
+
+gnn_status_t gnn_linear8_fwd(gnn_act_t act, int32_t n, int32_t f_in, int32_t f_out, const gnn_rows8_t *X, const gnn_rows8_t *W,
+                             const float *b, const float *R, float *Y, void *hip_stream) {
+    Rows8 x, w;
+    if (bad_act(act) || n < 0 || f_in <= 0 || f_out <= 0) return GNN_ERR_INVALID_ARG;
+    if (n == 0) return GNN_OK;
+    if (!X || !W || !Y) return GNN_ERR_INVALID_ARG;
+    GNN_TRY(take_rows8(X, false, &x));
+    GNN_TRY(take_rows8(W, false, &w));
+    if (!linear8_fits(n, f_in, f_out)) return GNN_ERR_UNSUPPORTED;
+    return linear8_forward_launch(act, n, f_in, f_out, x, w, b, R, Y, as_stream(hip_stream));
 }
 
 }  // extern "C"

@@ -161,6 +161,8 @@ size_t norm_workspace_bytes(int64_t n, int64_t f);
 gnn_status_t norm_backward_launch(int n, int f, const float *X, const float *stat, const float *gamma, const float *beta,
                                   int act, const Dropout &drop, bool before, const float *dY, const float *dH, float *dR,
                                   float *dX, float *dgamma, float *dbeta, void *workspace, hipStream_t st);
+// part [blocks][width]: the sums of the rows' first f columns, and of the others
+gnn_status_t norm_sums_launch(int f, int64_t width, int64_t blocks, const float *part, float *first, float *behind, hipStream_t st);
 bool gated_fits(bool backward, int64_t n, int64_t m, int64_t k);
 size_t gated_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k);
 gnn_status_t gated_forward_launch(int gate, int n, int m, int k, const float *X, const float *W, const float *b, float *H,
@@ -168,6 +170,30 @@ gnn_status_t gated_forward_launch(int gate, int n, int m, int k, const float *X,
 gnn_status_t gated_backward_launch(int gate, int n, int m, int k, const float *X, const float *W, const float *b,
                                    const float *Z, const float *dH, float *dW, float *db, float *dX, void *workspace,
                                    hipStream_t st);
+
+// ---- rows in 8 bits, RMS norm, products with their epilogue (rms_norm.hip, linear.hip, linear8.hip) ---------------------
+struct Rows8;                          // rows8.h
+gnn_status_t quantize_rows_launch(int n, int f, const float *X, const float *columns, const Rows8 &out, hipStream_t st);
+gnn_status_t dequantize_rows_launch(int n, int f, const Rows8 &in, float *Y, hipStream_t st);
+// without R: H = X, not written; Y, held.q and rstd may be NULL
+gnn_status_t rms_norm_forward_launch(int n, int f, const float *X, const float *R, const Dropout &drop, const float *gamma, float eps,
+                                     float *H, float *Y, const Rows8 &held, float *rstd, hipStream_t st);
+// H NULL: xhat from `held`; workspace: rms_norm_workspace_bytes, with dgamma only
+size_t rms_norm_workspace_bytes(int64_t n, int64_t f);
+gnn_status_t rms_norm_backward_launch(int n, int f, const float *H, const Rows8 &held, const float *rstd, const float *gamma,
+                                      const Dropout &drop, const float *dY, const float *dH, float *dR, float *dX, float *dgamma,
+                                      void *workspace, hipStream_t st);
+bool linear_fits(bool backward, int64_t n, int64_t m, int64_t k);
+size_t linear_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k);
+gnn_status_t linear_forward_launch(int act, int n, int m, int k, const float *X, const float *W, const float *b, const float *R, float *Y,
+                                   float *Z, void *workspace, hipStream_t st);
+// X NULL: from X8; Z NULL: from Z8, and where that has none formed again from X, W and b
+gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X, const Rows8 &X8, const float *W, const float *b,
+                                    const float *Z, const Rows8 &Z8, const float *dY, float *dW, float *db, float *dX, void *workspace,
+                                    hipStream_t st);
+bool linear8_fits(int64_t n, int64_t m, int64_t k);
+gnn_status_t linear8_forward_launch(int act, int n, int m, int k, const Rows8 &X, const Rows8 &W, const float *b, const float *R, float *Y,
+                                    hipStream_t st);
 
 // ---- preprocessing (prep.hip) -------------------------------------------------------
 size_t scan_workspace_bytes(int64_t n);

@@ -1,0 +1,336 @@
+// The product with its epilogue, Y = act(X W + b) + R, forward and backward.  Its large products are those of gemm_half_kernel.h and
+// gemm_half_tn.hip; those of few rows are here and in gemm.hip.
+#include "linear.h"
+
+namespace gnn {
+namespace {
+
+using namespace half_parts;
+
+// Few rows: four wavefronts per 32 rows and 32 columns of Y share the reduction, operands straight from memory into
+// registers two steps ahead (the two lane halves of v_mfma_f32_32x32x2_f32 take P consecutive indices each), one launch, no scratch.
+template <bool BACK, int ACT>
+__global__ void __launch_bounds__(256)
+linear_few_kernel(int M, int N, int K, const float *__restrict__ X, const float *__restrict__ W, const float *__restrict__ bias, Linear g,
+                  int tiles_n) {
+    constexpr int AHEAD = 2, P = 8;            // steps ahead; indices of a step for each lane half
+    __shared__ floatx4 sums[4][4][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, l = lane % 32, half = lane / 32;
+    const int m0 = (int)(blockIdx.x / tiles_n) * 32, j = (int)(blockIdx.x % tiles_n) * 32 + l;
+    const int all = (K + 2 * P - 1) / (2 * P), first = all * wave / 4, total = all * (wave + 1) / 4;
+    const float *x = X + (size_t)min(m0 + l, M - 1) * K, *w = W + min(j, N - 1);       // what is past the end re-reads the last
+    const size_t ld = N;
+    float xs[AHEAD][P], ws[AHEAD][P];
+    auto load = [&](int step, int s) __attribute__((always_inline)) {
+        const int k0 = (2 * step + half) * P;
+        if (k0 + P <= K) {
+#pragma unroll
+            for (int i = 0; i < P / 4; ++i) {
+                const float4u v = *reinterpret_cast<const float4u *>(x + k0 + 4 * i);
+                xs[s][4 * i] = v.x; xs[s][4 * i + 1] = v.y; xs[s][4 * i + 2] = v.z; xs[s][4 * i + 3] = v.w;
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i) ws[s][i] = w[(k0 + i) * ld];
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                xs[s][i] = k0 + i < K ? x[k0 + i] : 0.f;
+                ws[s][i] = k0 + i < K ? w[(k0 + i) * ld] : 0.f;
+            }
+        }
+    };
+    floatx16 acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s)
+        if (first + s < total) load(first + s, s);
+    for (int step = first; step < total; step += AHEAD) {
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) {
+            if (step + s < total) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(xs[s][i], ws[s][i], acc, 0, 0, 0);
+                if (step + s + AHEAD < total) load(step + s + AHEAD, s);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[wave][i][lane] = floatx4{acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]};
+    __syncthreads();
+    if (j >= N) return;
+    // a wavefront finishes a quarter of the tile: accumulator register v of lane (half, l) is row 8 (v / 4) + 4 half + v % 4
+    const floatx4 z = (sums[0][wave][lane] + sums[1][wave][lane]) + (sums[2][wave][lane] + sums[3][wave][lane]) + (bias ? bias[j] : 0.f);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const int m = m0 + 8 * wave + 4 * half + v;
+        if (m >= M) continue;
+        float y, slope;
+        activate<ACT, BACK>(z[v], y, slope);
+        const size_t at = (size_t)m * N + j;
+        if constexpr (BACK) {
+            g.D[at] = g.dY[at] * slope;
+        } else {
+            if (g.Z) g.Z[at] = z[v];
+            g.Y[at] = g.R ? y + g.R[at] : y;
+        }
+    }
+}
+
+// D = dY .* act'(Z) from the Z that forward has kept, as it is or in 8 bits, and the largest magnitudes of its rows and of its columns,
+// those with each row times row_scale.  A block takes `rows` rows (top_rows where columns' are wanted) and 64 VEC columns, `lanes` lanes a
+// row; the `parts` blocks of the same rows stand side by side.  D NULL: not wanted (it is dY).
+template <int VEC, int ACT, bool HELD>
+__global__ void __launch_bounds__(256)
+linear_gradient_kernel(long n, int k, int lanes, int rows, int parts, const float *__restrict__ Z, Rows8 held, const float *__restrict__ dY,
+                       const float *__restrict__ row_scale, float *__restrict__ D, Tops tops) {
+    __shared__ unsigned across[256][VEC];
+    const int gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
+    const int part = blockIdx.x % parts, block = blockIdx.x / parts, c = (part * 64 + gl) * VEC;
+    const long r0 = (long)block * rows, r1 = min(n, r0 + rows), ld = rows8_stride(k);
+    unsigned top[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) top[v] = 0;
+    constexpr int U = 4;                                   // rows under way
+    for (long first = r0; first < r1; first += U * groups) {
+        float z[U][VEC], d[U][VEC], factor[U];
+        unsigned most[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp, at = row * k + c;
+            factor[i] = 1.f;
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) z[i][v] = d[i][v] = 0.f;
+            if (row >= r1 || c >= k) continue;
+            if (row_scale) factor[i] = row_scale[row];
+            if constexpr (VEC == 4) {
+                const float4 y = *reinterpret_cast<const float4 *>(dY + at);
+                d[i][0] = y.x; d[i][1] = y.y; d[i][2] = y.z; d[i][3] = y.w;
+                if constexpr (ACT != GNN_ACT_NONE) {
+                    float4 x;
+                    if constexpr (HELD) {
+                        const float s = held.scale[row];
+                        x = integers(*reinterpret_cast<const unsigned *>(held.q + row * ld + c));
+                        x = make_float4(x.x * s, x.y * s, x.z * s, x.w * s);
+                        if (held.columns) {
+                            const float4u e = *reinterpret_cast<const float4u *>(held.columns + c);
+                            x = make_float4(x.x * e.x, x.y * e.y, x.z * e.z, x.w * e.w);
+                        }
+                    } else {
+                        x = *reinterpret_cast<const float4 *>(Z + at);
+                    }
+                    z[i][0] = x.x; z[i][1] = x.y; z[i][2] = x.z; z[i][3] = x.w;
+                }
+            } else {
+                d[i][0] = dY[at];
+                if constexpr (ACT != GNN_ACT_NONE) {
+                    if constexpr (HELD) z[i][0] = (float)held.q[row * ld + c] * held.scale[row] * (held.columns ? held.columns[c] : 1.f);
+                    else z[i][0] = Z[at];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp, at = row * k + c;
+            most[i] = 0;
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                if constexpr (ACT != GNN_ACT_NONE) {
+                    float y, slope;
+                    activate<ACT, true>(z[i][v], y, slope);
+                    d[i][v] *= slope;
+                }
+                most[i] = max(most[i], magnitude(d[i][v]));
+                top[v] = max(top[v], magnitude(d[i][v] * factor[i]));
+            }
+            if (!D || row >= r1 || c >= k) continue;
+            if constexpr (VEC == 4) *reinterpret_cast<float4 *>(D + at) = make_float4(d[i][0], d[i][1], d[i][2], d[i][3]);
+            else D[at] = d[i][0];
+        }
+        if (!tops.rows) continue;
+        for (int q = lanes >> 1; q > 0; q >>= 1)
+#pragma unroll
+            for (int i = 0; i < U; ++i) most[i] = max(most[i], (unsigned)__shfl_xor((int)most[i], q, 64));
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp;
+            if (gl == 0 && row < r1) tops.rows[(size_t)part * n + row] = most[i];
+        }
+    }
+    if (!tops.cols) return;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) across[threadIdx.x][v] = top[v];
+    __syncthreads();
+    if (grp == 0 && c < k)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            for (int q = 1; q < groups; ++q) top[v] = max(top[v], across[q * lanes + gl][v]);
+            tops.cols[(size_t)block * k + c + v] = top[v];
+        }
+}
+
+// the other kernels read four indices at a time
+bool too_narrow(int64_t m, int64_t k) { return m < 4 || k < 4; }
+// Tiles of 32 x 32 of Y up to which the kernels for few rows are taken
+int64_t few_tiles(int64_t m) { return m < 32 ? 8000 : 260000 / m; }
+// weights whose gradient is better off in float than through partial products of doubles and the pass over those, however few the rows
+bool wide_weights(int64_t m, int64_t k) { return !too_narrow(m, k) && m * k >= 1 << 19; }
+// D W^T is a product of the layers
+bool short_columns(int64_t k) { return k < kShortReduction; }
+bool linear_few(int64_t n, int64_t m, int64_t k) { return too_narrow(m, k) || ceil_div(n, 32) * ceil_div(k, 32) <= few_tiles(m); }
+// the rows up to which that is so
+int64_t few_rows(int64_t n, int64_t m, int64_t k) {
+    if (too_narrow(m, k)) return n;
+    const int64_t rows = 32 * (few_tiles(m) / ceil_div(k, 32));
+    return n < rows ? n : rows;
+}
+
+#define BY_ACT(ACT_, KERNEL_, ...)                                             \
+    ((ACT_) == GNN_ACT_RELU      ? KERNEL_(GNN_ACT_RELU, __VA_ARGS__)          \
+     : (ACT_) == GNN_ACT_ELU     ? KERNEL_(GNN_ACT_ELU, __VA_ARGS__)           \
+     : (ACT_) == GNN_ACT_SIGMOID ? KERNEL_(GNN_ACT_SIGMOID, __VA_ARGS__)       \
+     : (ACT_) == GNN_ACT_SILU    ? KERNEL_(GNN_ACT_SILU, __VA_ARGS__) : KERNEL_(GNN_ACT_GELU, __VA_ARGS__))
+#define FEW_KERNEL(ACT_, BACK_) linear_few_kernel<BACK_, ACT_>
+#define GRADIENT_KERNEL(ACT_, VEC_, HELD_) linear_gradient_kernel<VEC_, ACT_, HELD_>
+
+gnn_status_t few(int act, int64_t n, int64_t m, int64_t k, const float *X, const float *W, const float *b, const Linear &g, hipStream_t st) {
+    const int64_t tiles_n = ceil_div(k, 32), blocks = ceil_div(n, 32) * tiles_n;
+    auto kernel = g.D ? BY_ACT(act, FEW_KERNEL, true) : act == GNN_ACT_NONE ? linear_few_kernel<false, GNN_ACT_NONE> : BY_ACT(act, FEW_KERNEL, false);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, (int)n, (int)k, (int)m, X, W, b, g, (int)tiles_n);
+    return launch_status();
+}
+
+gnn_status_t gradient(int act, int64_t n, int k, const float *Z, const Rows8 &held, const float *dY, const float *row_scale, float *D,
+                      const Tops &tops, int *parts, hipStream_t st) {
+    const bool vec = k % 4 == 0 && aligned16(Z) && aligned16(dY);
+    int lanes = 1;
+    while (lanes < 64 && lanes * (vec ? 4 : 1) < k) lanes <<= 1;
+    *parts = (int)ceil_div(k, vec ? 256 : 64);
+    const int rows = tops.cols ? top_rows(n) : (int)free_rows(n, lanes, *parts);
+    auto kernel = act == GNN_ACT_NONE ? (vec ? linear_gradient_kernel<4, GNN_ACT_NONE, false> : linear_gradient_kernel<1, GNN_ACT_NONE, false>)
+                  : Z ? (vec ? BY_ACT(act, GRADIENT_KERNEL, 4, false) : BY_ACT(act, GRADIENT_KERNEL, 1, false))
+                      : (vec ? BY_ACT(act, GRADIENT_KERNEL, 4, true) : BY_ACT(act, GRADIENT_KERNEL, 1, true));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(n, rows) * *parts)), dim3(256), 0, st, (long)n, k, lanes, rows, *parts, Z, held,
+                       dY, row_scale, D, tops);
+    return launch_status();
+}
+
+// scratch of a backward pass behind D and X
+struct Backward {
+    unsigned *x_rows, *x_cols, *d_rows, *d_cols;
+    void *rest;
+    size_t bytes;
+    Backward(char *at, int64_t n, int64_t m, int64_t k) {
+        Carver carve(at);
+        x_rows = carve.take<unsigned>(n * ceil_div(m, 64));
+        x_cols = carve.take<unsigned>(most_top_blocks(n) * m);
+        d_rows = carve.take<unsigned>(n * ceil_div(k, 64));      // linear_row_parts(n, k), those of `gradient` or top_parts
+        d_cols = carve.take<unsigned>(most_top_blocks(n) * k);
+        rest = carve.take<char>(0);
+        size_t most = linear_half_workspace_bytes(k, m);
+        for (size_t b : {gemm_half_workspace_bytes(m, k), gemm_half_tn_workspace_bytes(m, k, n), gemm_workspace_bytes(0, 1, n, m, k)})
+            if (b > most) most = b;
+        bytes = carve.off + most;
+    }
+};
+
+}  // namespace
+
+// A grid has less than 2^32 threads, 2^24 blocks of 256: the kernels for few rows take 32 x 32 elements of Y a block, columns' largest
+// magnitudes are formed in blocks of 32 rows and 64 columns at least.
+bool linear_fits(bool backward, int64_t n, int64_t m, int64_t k) {
+    if (m > 1 << 21 || k > 1 << 21) return false;
+    const int64_t rows = ceil_div(n, 32), most = (int64_t)1 << 24;
+    if (linear_few(n, m, k))
+        return rows * ceil_div(k, 32) < most && (!backward || (gemm_fits(n, m, k) && gemm_half_tn_fits(m, k, n)));
+    return rows * ceil_div(m > k ? m : k, 64) < most && gemm_half_fits(n, k) &&
+           (!backward || ((short_columns(k) ? gemm_fits(n, m, k) : gemm_half_fits(n, m)) && gemm_half_tn_fits(m, k, n)));
+}
+
+// What n rows take, or fewer: a product of few rows needs less.
+size_t linear_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k) {
+    if (!backward) return linear_few(n, m, k) ? kAlign : align_up((size_t)n * ceil_div(m, 64) * sizeof(unsigned)) + linear_half_workspace_bytes(k, m);
+    const size_t d = align_up((size_t)n * k * sizeof(float)) + align_up((size_t)n * m * sizeof(float));
+    size_t most = 0;
+    const int64_t small = few_rows(n, m, k);
+    if (small > 0 && !wide_weights(m, k)) {
+        const size_t tn = gemm_workspace_bytes(1, 0, m, k, small);         // a row of sums per chunk is an m-th of it
+        most = tn + align_up(tn / m);
+        const size_t x = gemm_workspace_bytes(0, 1, small, m, k);
+        if (x > most) most = x;
+    }
+    if (!linear_few(n, m, k) || wide_weights(m, k)) {
+        const Backward w(nullptr, n, m, k);
+        if (w.bytes > most) most = w.bytes;
+    }
+    return d + most;
+}
+
+gnn_status_t linear_forward_launch(int act, int n, int m, int k, const float *X, const float *W, const float *b, const float *R, float *Y,
+                                   float *Z, void *workspace, hipStream_t st) {
+    if (n <= 0) return GNN_OK;
+    const Linear g{R, Y, Z, nullptr, nullptr};
+    if (linear_few(n, m, k)) return few(act, n, m, k, X, W, b, g, st);
+    Carver carve(workspace);
+    const Tops tops{carve.take<unsigned>((size_t)n * ceil_div(m, 64)), nullptr};
+    if (m >= kShortReduction) GNN_TRY(tops_launch(n, m, X, tops, st));
+    return linear_half_launch(act, n, k, m, X, tops.rows, W, b, g, Tops{nullptr, nullptr}, carve.take<char>(0), st);
+}
+
+gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X, const Rows8 &X8, const float *W, const float *b,
+                                    const float *Z, const Rows8 &Z8, const float *dY, float *dW, float *db, float *dX, void *workspace,
+                                    hipStream_t st) {
+    if (n <= 0) {
+        GNN_TRY(fill_zero_launch((int64_t)m * k, dW, st));
+        return db ? fill_zero_launch(k, db, st) : GNN_OK;
+    }
+    Carver carve(workspace);
+    float *d_space = carve.take<float>((size_t)n * k), *x_space = carve.take<float>((size_t)n * m);
+    const bool plain = act == GNN_ACT_NONE, kept = Z || Z8.q;
+    const float *d = plain ? dY : d_space;
+    if (!X) {
+        GNN_TRY(dequantize_rows_launch(n, m, X8, x_space, st));
+        X = x_space;
+    }
+    const Linear g{nullptr, nullptr, nullptr, dY, d_space};
+    const bool one_step = n < kShortReduction;             // X^T D does without largest magnitudes
+    int parts = 0;
+    if (linear_few(n, m, k)) {
+        void *rest = carve.take<char>(0);
+        const bool wide = wide_weights(m, k);
+        const Backward w(static_cast<char *>(rest), n, m, k);
+        const Tops of_d{nullptr, wide && !one_step ? w.d_cols : nullptr};
+        if (!plain && kept) {
+            GNN_TRY(gradient(act, n, k, Z, Z8, dY, nullptr, d_space, of_d, &parts, st));
+        } else {
+            if (!plain) GNN_TRY(few(act, n, m, k, X, W, b, g, st));
+            if (of_d.cols) GNN_TRY(tops_launch(n, k, d, of_d, st));
+        }
+        if (dX) GNN_TRY(gemm_launch(0, 1, n, m, k, d, W, dX, nullptr, 0, wide ? w.rest : rest, st));
+        if (wide) {
+            if (!one_step) GNN_TRY(tops_launch(n, m, X, Tops{nullptr, w.x_cols}, st));
+            return gemm_half_tn_launch(m, k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
+        }
+        GemmExtras extras{};
+        extras.sums = db;
+        extras.workspace = static_cast<char *>(rest) + gemm_workspace_bytes(1, 0, m, k, n);
+        return gemm_launch(1, 0, m, k, n, X, d, dW, nullptr, 0, rest, st, nullptr, 0, 0, nullptr, nullptr, &extras);
+    }
+    const Backward w(static_cast<char *>(workspace) + carve.off, n, m, k);
+    const Tops of_x{plain || kept || m < kShortReduction ? nullptr : w.x_rows, one_step ? nullptr : w.x_cols}, of_d{w.d_rows, w.d_cols};
+    if (of_x.rows || of_x.cols) GNN_TRY(tops_launch(n, m, X, of_x, st));
+    if (plain) {
+        GNN_TRY(tops_launch(n, k, dY, of_d, st));
+        parts = top_parts(k, dY);
+    } else if (kept) {
+        GNN_TRY(gradient(act, n, k, Z, Z8, dY, nullptr, d_space, of_d, &parts, st));
+    } else {
+        GNN_TRY(linear_half_launch(act, n, k, m, X, w.x_rows, W, b, g, of_d, w.rest, st));
+        parts = linear_row_parts(n, k);
+    }
+    if (dX && short_columns(k)) GNN_TRY(gemm_launch(0, 1, n, m, k, d, W, dX, nullptr, 0, w.rest, st));
+    else if (dX) GNN_TRY(gemm_half_launch(n, m, k, d, w.d_rows, parts, W, dX, w.rest, st));
+    return gemm_half_tn_launch(m, k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
+}
+
+}  // namespace gnn

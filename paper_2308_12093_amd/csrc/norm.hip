@@ -1,85 +1,12 @@
 // Dropout, layer norm and the two around a residual connection, forward and backward.
+#include "activation.h"
 #include "dropout.h"
+#include "rows.h"
 
 namespace gnn {
 namespace {
 
-typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
-
-typedef float floatx2u __attribute__((ext_vector_type(2), aligned(4)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-
-typedef float floatx3u __attribute__((ext_vector_type(3), aligned(4)));
-
-// Columns c .. c + 3 < f + 3 of a row of f, at any 4-byte aligned address; zeros past the row's end.  The one to three of the last
-// lane are one access, too: f % 4 is the same for all.
-__device__ __forceinline__ float4 load4(const float *row, int c, int f) {
-    if (c + 4 <= f) {
-        const float4u v = *reinterpret_cast<const float4u *>(row + c);
-        return make_float4(v.x, v.y, v.z, v.w);
-    }
-    const int left = f & 3;
-    if (left == 1) return make_float4(row[c], 0.f, 0.f, 0.f);
-    if (left == 2) {
-        const floatx2u v = *reinterpret_cast<const floatx2u *>(row + c);
-        return make_float4(v.x, v.y, 0.f, 0.f);
-    }
-    const floatx3u v = *reinterpret_cast<const floatx3u *>(row + c);
-    return make_float4(v.x, v.y, v.z, 0.f);
-}
-
-__device__ __forceinline__ void store4(float *row, int c, int f, float4 v) {
-    if (c + 4 <= f) {
-        *reinterpret_cast<float4u *>(row + c) = float4u{v.x, v.y, v.z, v.w};
-        return;
-    }
-    const int left = f & 3;
-    if (left == 1) row[c] = v.x;
-    else if (left == 2) *reinterpret_cast<floatx2u *>(row + c) = floatx2u{v.x, v.y};
-    else *reinterpret_cast<floatx3u *>(row + c) = floatx3u{v.x, v.y, v.z};
-}
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
-}
-
-// exp(x) for x <= 0: off by at most (1 + |x|) units in the last place, one instruction and a multiplication
-__device__ __forceinline__ float exp_down(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
-
-// exp(x) - 1 for x <= 0: the series up to x^7 / 7! near zero (what it leaves out is below 2^-25 of the result), the difference
-// where it keeps its digits
-__device__ __forceinline__ float expm1_down(float x) {
-    const float p = fmaf(fmaf(fmaf(fmaf(fmaf(1.f / 5040, x, 1.f / 720), x, 1.f / 120), x, 1.f / 24), x, 1.f / 6), x, 0.5f);
-    return x > -0.35f ? fmaf(x * x, p, x) : exp_down(x) - 1.f;
-}
-
-template <int ACT>
-__device__ __forceinline__ float activation(float z) {
-    if constexpr (ACT == kActRelu) return z < 0.f ? 0.f : z;                // NaN stays
-    if constexpr (ACT == kActElu) return z > 0.f ? z : expm1_down(z);
-    return z;
-}
-template <int ACT>
-__device__ __forceinline__ float slope(float z) {
-    if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : 0.f;
-    if constexpr (ACT == kActElu) return z > 0.f ? 1.f : exp_down(z);      // NaN stays
-    return 1.f;
-}
-__device__ __forceinline__ float activation(float z, int act) {
-    return act == kActRelu ? activation<kActRelu>(z) : act == kActElu ? activation<kActElu>(z) : z;
-}
-__device__ __forceinline__ float slope(float z, int act) {
-    return act == kActRelu ? slope<kActRelu>(z) : act == kActElu ? slope<kActElu>(z) : 1.f;
-}
-
-// 1 / sqrt(x): the instruction's, and a Newton step (an IEEE division and root take thirty instructions, for each lane of a row)
-__device__ __forceinline__ float inverse_root(float x) {
-    const float y = __builtin_amdgcn_rsqf(x);
-    const float r = fmaf(fmaf(-0.5f * x * y, y, 0.5f), y, y);
-    return x > 0x1p-100f && x < 0x1p100f ? r : y;          // x y y keeps its range there; infinities and NaN as they are
-}
+using namespace rows;
 
 // Four columns a thread, one generator's block each.  Bound by memory: 2^20 x 256 with a residual 3.2 GB in 525 us, 6.1 TB/s (a copy
 // reaches 5.0, a sum of two arrays 5.9); the ten rounds of the generator, 40 multiplications for 48 bytes, hide behind it.
@@ -113,54 +40,6 @@ struct Norm {
     float *H, *Y, *stat;
 };
 
-// v: the sums of a wavefront's lanes of a row; then those of the row's wavefronts, two or four
-template <int U>
-__device__ __forceinline__ void wide_sums(float (&v)[U], int lanes, float *red) {
-    const int wave = threadIdx.x / 64, first = threadIdx.x / lanes * (lanes / 64);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0)
-#pragma unroll
-        for (int u = 0; u < U; ++u) red[4 * u + wave] = v[u];
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        float s = red[4 * u + first] + red[4 * u + first + 1];
-        if (lanes == 256) s += red[4 * u + 2] + red[4 * u + 3];
-        v[u] = s;
-    }
-}
-
-// the sums of each of U values over the lanes of a row, in all of them
-template <int U, bool WIDE>
-__device__ __forceinline__ void row_sums(float (&v)[U], int lanes, float *red) {
-    for (int d = (WIDE ? 64 : lanes) >> 1; d > 0; d >>= 1)
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u] += __shfl_xor(v[u], d, 64);
-    if constexpr (WIDE) wide_sums(v, lanes, red);
-}
-// The same of U pairs: each half of the lanes goes on with one value of a pair and hands it to the other in the end, two
-// exchanges more than for one value.
-template <int U, bool WIDE>
-__device__ __forceinline__ void row_sums_of_pairs(float (&v)[2 * U], int lanes, float *red) {
-    const int half = (WIDE ? 64 : lanes) >> 1;
-    if (half > 0) {
-        const bool upper = threadIdx.x & half;
-        float s[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) s[u] = (upper ? v[2 * u + 1] : v[2 * u]) + __shfl_xor(upper ? v[2 * u] : v[2 * u + 1], half, 64);
-        for (int d = half >> 1; d > 0; d >>= 1)
-#pragma unroll
-            for (int u = 0; u < U; ++u) s[u] += __shfl_xor(s[u], d, 64);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const float other = __shfl_xor(s[u], half, 64);
-            v[2 * u] = upper ? other : s[u];
-            v[2 * u + 1] = upper ? s[u] : other;
-        }
-    }
-    if constexpr (WIDE) wide_sums(v, lanes, red);
-}
-
 // What the mean m of a row is off by, from the sum of the differences d to it, and its variance + eps, from the sum of their squares as
 // well.  Far from zero one unit in the last place of m is as large as what rows of nearly equal values are normalised by, and
 // a sum over lanes divided by f misses the value of a row of f equal ones in a third of all cases.  Such a row's d are a few
@@ -178,29 +57,6 @@ __device__ __forceinline__ float mean_off_by(float sum, float f, float inv_f) {
 __device__ __forceinline__ float variance_and(float eps, float sum, float square, float off, float inv_f) {
     const float left = fmaf(-off, sum, square);
     return fmaf(left < 0.f ? 0.f : left, inv_f, eps);      // NaN stays
-}
-
-// How rows are read and written.  kStreamed: aligned rows of arrays beyond the caches, past them (2^20 x 256 backward 645 -> 600
-// us, 2^18 x 512 around a residual connection 511 -> 488 and forward 398 -> 379; arrays that the caches hold would lose
-// what the next kernel finds there).
-enum { kAnyRow, kAlignedRow, kStreamed };
-
-template <int MEM>
-__device__ __forceinline__ float4 read4(const float *row, int c, int f, bool valid) {
-    if (!valid || c >= f) return make_float4(0.f, 0.f, 0.f, 0.f);
-    if constexpr (MEM == kAnyRow) return load4(row, c, f);
-    else if constexpr (MEM == kAlignedRow) return *reinterpret_cast<const float4 *>(row + c);
-    else {
-        const floatx4 v = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(row + c));
-        return make_float4(v.x, v.y, v.z, v.w);
-    }
-}
-template <int MEM>
-__device__ __forceinline__ void write4(float *row, int c, int f, float4 v) {
-    if (c >= f) return;
-    if constexpr (MEM == kAnyRow) store4(row, c, f, v);
-    else if constexpr (MEM == kAlignedRow) *reinterpret_cast<float4 *>(row + c) = v;
-    else __builtin_nontemporal_store(floatx4{v.x, v.y, v.z, v.w}, reinterpret_cast<floatx4 *>(row + c));
 }
 
 // Bound by memory: 2^20 x 256 with ELU and dropout 2.1 GB in 409 us, 5.3 TB/s; 2^18 x 512 around a residual connection 2.1 GB in 344 to
@@ -420,20 +276,6 @@ norm_backward_kernel(NormBack a) {
 
 // Rows beyond 4096 columns: a block per row, which it reads several times (16 KB and more, from the caches; for the columns' sums
 // from memory again).  16384 x 8192 forward 282 us, 3.8 TB/s, backward 648 us, 2.5 TB/s of X, dY and dX.
-constexpr int kNormRow = 4096;
-
-__device__ __forceinline__ float block_sum(float v, float *red) {
-    v = wave_sum(v);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
-    __syncthreads();
-    return (red[0] + red[1]) + (red[2] + red[3]);
-}
-__device__ __forceinline__ void unpack(float4 v, float (&o)[4]) { o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w; }
-__device__ __forceinline__ void weights4(const float *p, int c, int f, float without, float (&o)[4]) {
-    unpack(p ? load4(p, c, f) : make_float4(without, without, without, without), o);
-}
-
 __global__ void __launch_bounds__(256)
 norm_forward_long_kernel(Norm a) {
     __shared__ float red[4];
@@ -560,13 +402,13 @@ norm_sums_long_kernel(NormBack a, bool after) {
     }
 }
 
-// dgamma, dbeta = the sums of the partial rows, in double and in a fixed order: 16 columns a block, 64 lanes each, four of them in a
+// first, behind = the sums of the partial rows' first f and other columns, in double and in a fixed order: 16 columns a block, 64 lanes each, four of them in a
 // wavefront.  What it waits for is memory, four partial rows of a lane at a time: 1024 rows of 94 floats 4.0 us (16 lanes each: 6.7).
 __global__ void __launch_bounds__(1024)
-norm_sums_final_kernel(int f, int blocks, const float *__restrict__ part, float *dgamma, float *dbeta) {
+norm_sums_final_kernel(int f, long w, int blocks, const float *__restrict__ part, float *first, float *behind) {
     __shared__ double red[16][16];
     const int o = threadIdx.x % 16, sl = threadIdx.x / 16;
-    const long c = (long)blockIdx.x * 16 + o, w = 2 * (long)f;
+    const long c = (long)blockIdx.x * 16 + o;
     double a0 = 0.0, a1 = 0.0, a2 = 0.0, a3 = 0.0;
     if (c < w) {
         long b = sl;
@@ -586,39 +428,9 @@ norm_sums_final_kernel(int f, int blocks, const float *__restrict__ part, float 
     if (threadIdx.x < 16 && c < w) {
         double t = 0.0;
         for (int k = 0; k < 16; ++k) t += red[k][o];
-        float *out = c < f ? dgamma : dbeta;
+        float *out = c < f ? first : behind;
         if (out) out[c < f ? c : c - f] = (float)t;
     }
-}
-
-// How a row is dealt to lanes: as few of four columns as hold it, then more per lane.
-struct Shape {
-    int lanes, per;                    // lanes a row; times four columns of each
-    bool wide;
-};
-Shape norm_shape(int f) {
-    const int groups = (f + 3) / 4;
-    int lanes = 1;
-    while (lanes < 64 && lanes < groups) lanes <<= 1;
-    int per = 1;
-    while (per < 4 && lanes * per < groups) per <<= 1;
-    while (lanes * per < groups) lanes <<= 1;              // up to kNormRow: 256 lanes
-    return Shape{lanes, per, lanes > 64};
-}
-// Blocks of the backward pass, one partial row of sums each: a group of lanes adds at most 256 rows in float.
-constexpr int kNormChain = 256;
-int64_t norm_blocks(int64_t n, int f) {
-    if (n <= 0) return 0;
-    if (f > kNormRow) {                                    // a grid's y; more rows of this length no memory holds
-        const int64_t blocks = ceil_div(n, kNormChain) > 64 ? ceil_div(n, kNormChain) : (n < 64 ? n : 64);
-        return blocks < 65535 ? blocks : 65535;
-    }
-    const Shape s = norm_shape(f);
-    const int64_t groups = 256 / s.lanes;
-    const int64_t most = ceil_div(n, groups * 2);          // two rows a group at least
-    int64_t blocks = ceil_div(n, groups * kNormChain);
-    if (blocks < 1024) blocks = most < 1024 ? most : 1024;
-    return blocks;
 }
 
 __global__ void rng_advance_kernel(uint64_t *state, uint64_t by) { state[1] += by; }
@@ -627,6 +439,12 @@ __global__ void rng_advance_kernel(uint64_t *state, uint64_t by) { state[1] += b
 
 gnn_status_t rng_advance_launch(uint64_t *state, uint64_t by, hipStream_t st) {
     hipLaunchKernelGGL(rng_advance_kernel, dim3(1), dim3(1), 0, st, state, by);
+    return launch_status();
+}
+
+gnn_status_t norm_sums_launch(int f, int64_t width, int64_t blocks, const float *part, float *first, float *behind, hipStream_t st) {
+    hipLaunchKernelGGL(norm_sums_final_kernel, dim3((unsigned)ceil_div(width, 16)), dim3(1024), 0, st, f, (long)width, (int)blocks, part,
+                       first, behind);
     return launch_status();
 }
 
@@ -654,10 +472,6 @@ gnn_status_t dropout_launch(int n, int f, const float *X, const float *R, const 
     }
 #define NORM_LAUNCH(KERNEL_, PER_, U_, ACT_, ADD_, MEM_, WIDE_) \
     hipLaunchKernelGGL((KERNEL_<PER_, U_, ACT_, ADD_, MEM_, WIDE_>), grid, dim3(256), 0, st, a)
-
-static int norm_memory(int64_t n, int f, bool aligned) {
-    return !aligned ? kAnyRow : (size_t)n * f * sizeof(float) > kStreamBytes ? kStreamed : kAlignedRow;
-}
 
 gnn_status_t norm_forward_launch(int n, int f, const float *X, const float *R, const float *gamma, const float *beta,
                                  float eps, int act, const Dropout &drop, float *H, float *Y, float *stat, hipStream_t st) {
@@ -716,9 +530,7 @@ gnn_status_t norm_backward_launch(int n, int f, const float *X, const float *sta
     }
     GNN_TRY(launch_status());
     if (!sums) return GNN_OK;
-    hipLaunchKernelGGL(norm_sums_final_kernel, dim3((unsigned)ceil_div(2 * (int64_t)f, 16)), dim3(1024), 0, st, f, (int)blocks,
-                       a.part, dgamma, dbeta);
-    return launch_status();
+    return norm_sums_launch(f, 2 * (int64_t)f, blocks, a.part, dgamma, dbeta, st);
 }
 #undef NORM_CASE
 #undef NORM_ACT

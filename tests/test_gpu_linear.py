@@ -1,0 +1,391 @@
+"""The product with bias, activation and residual, forward and backward, from floats and from rows in 8 bits, against its definition in
+double precision; and the forward product of rows in 8 bits.
+
+Bounds in units of u = 2^-24.  The products take at most eight roundings per 16 indices and term, as the library's other products, so
+Z is within ez = (8 ceil(m / 16) + 8) u (|X||W| + |b|).  The activations have slopes of at most 1.13 and second derivatives of at most 1
+and are taken within 16 u of themselves (relative to max(1, |z|) for their slopes); a ReLU whose input is within ez of zero may fall on
+either side.  What is held in 8 bits is an input: an element of it takes three roundings."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import blocks
+from paper_2308_12093_amd import binding as B
+from tests._util import dev, host
+from tests.test_gpu_norm import NAN, shifted, space, within
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+ACTS = ["none", "relu", "elu", "sigmoid", "silu", "gelu"]
+ID = {name: getattr(B, "GNN_ACT_" + name.upper()) for name in ACTS}
+
+
+def rows8(a, columns=None):
+    """Rows on the device as the definition has them, anything behind a row's end, and the values that they stand for."""
+    q, unit = blocks.held8(a)
+    n, f = q.shape
+    room = np.full((n, B.gnn_rows8_stride(f)), 101, np.int8)
+    room[:, :f] = q
+    scale = unit.astype(np.float32)
+    held = q * scale.astype(np.float64)[:, None] * (1.0 if columns is None else columns.astype(np.float64))
+    return B.Rows8(dev(room), dev(scale), None if columns is None else dev(columns)), held
+
+
+class Case:
+    def __init__(self, n, m, k, act, bias=True, residual=True, scale=1.0, seed=0):
+        rng = np.random.default_rng(n + 7 * m + 31 * k + seed)
+        f32 = lambda *s: rng.standard_normal(s).astype(np.float32)  # noqa: E731
+        self.n, self.m, self.k, self.act = n, m, k, act
+        self.X, self.W = f32(n, m) * np.float32(scale), f32(m, k) / np.float32(np.sqrt(m))
+        self.b = f32(k) / 4 if bias else None
+        self.R = f32(n, k) if residual else None
+        self.columns = 1 + f32(m) / 4
+        self.dY = f32(n, k)
+        self.define()
+
+    def define(self):
+        self.Y, self.Z = blocks.linear_forward(self.X, self.W, self.b, self.act, self.R)
+        aX, aW = np.abs(self.X).astype(np.float64), np.abs(self.W).astype(np.float64)
+        mag = aX @ aW + (0.0 if self.b is None else np.abs(self.b))
+        self.Z_most = (8 * ((self.m + 15) // 16) + 8) * U * mag
+        a, _ = blocks.act(self.act, self.Z)
+        self.Y_most = 1.13 * self.Z_most + 16 * U * np.abs(a) + 2 * U * np.abs(self.Y)
+        self.gradients(self.X, self.Z, self.Z_most, 0.0)
+
+    def gradients(self, X, Z, ez, x_off):
+        _, slope = blocks.act(self.act, Z)
+        es = ez + 16 * U * np.maximum(1.0, np.abs(Z)) if self.act != "none" else np.zeros_like(Z)
+        if self.act == "relu":
+            es = (np.abs(Z) <= ez).astype(np.float64)
+        self.dW, self.db, self.dX, D = blocks.linear_backward(X, self.W, Z, self.dY, self.act)
+        eD = np.abs(self.dY) * es + 2 * U * np.abs(D)
+        aD, aX, aW = np.abs(D) + eD, np.abs(X), np.abs(self.W).astype(np.float64)
+        self.dX_most = eD @ aW.T + (8 * ((self.k + 15) // 16) + 8) * U * (aD @ aW.T)
+        C = 64 + 8 * ((min(self.n, 4096) + 15) // 16)      # sums over the nodes: in float for 4096 of them at most, then in double
+        self.dW_most = aX.T @ eD + (C * U + x_off) * (aX.T @ aD)
+        self.db_most = eD.sum(0) + C * U * aD.sum(0)
+
+
+def workspace(c, back):
+    ws = B.alloc(B.gnn_linear_workspace_bytes(back, c.n, c.m, c.k))
+    ws.fill_(255)
+    return ws
+
+
+def forward(c, keep=True, by=0, over=False):
+    X, W, b = shifted(c.X, by), shifted(c.W, by), None if c.b is None else shifted(c.b, by)
+    R = None if c.R is None else shifted(c.R, by)
+    Y, Z = space(c.n, c.k, by), space(c.n, c.k, by)
+    out = R if over else Y[0]
+    B.gnn_linear_fwd(ID[c.act], c.n, c.m, c.k, X, W, b, R, out, Z[0] if keep else None, workspace(c, False))
+    assert bool((Y[1] == 7.0).all()) and bool((Z[1] == 7.0).all())
+    return out, Z[0]
+
+
+def backward(c, X=None, X8=None, Z=None, Z8=None, by=0, want_dx=True):
+    W, b, dY = shifted(c.W, by), None if c.b is None else shifted(c.b, by), shifted(c.dY, by)
+    dW, db, dX = space(c.m, c.k, by), space(1, c.k, by), space(c.n, c.m, by)
+    B.gnn_linear_bwd(ID[c.act], c.n, c.m, c.k, X, X8, W, b, Z, Z8, dY, dW[0], db[0], dX[0] if want_dx else None, workspace(c, True))
+    for _, end in (dW, db, dX):
+        assert bool((end == 7.0).all())
+    return dW[0], db[0][0], dX[0]
+
+
+def check(c, got, names=("dW", "db", "dX")):
+    for t, name in zip(got, names):
+        within(t, getattr(c, name), getattr(c, name + "_most"), name)
+
+
+def every_way(c, by=0):
+    """Forward; backward from Z kept and formed again; backward from 8 bits."""
+    Y, Z = forward(c, True, by)
+    check(c, (Y, Z), ("Y", "Z"))
+    X = shifted(c.X, by)
+    check(c, backward(c, X, None, None, None, by))
+    check(c, backward(c, X, None, Z, None, by))
+    X8, held_x = rows8(c.X, c.columns)
+    Z8, held_z = rows8(c.Z.astype(np.float32))
+    c.gradients(held_x, held_z, 3 * U * np.abs(held_z), 3 * U)
+    check(c, backward(c, None, X8, None, Z8, by))
+    check(c, backward(c, None, X8, dev(held_z.astype(np.float32)), None, 0))
+    c.define()
+    c.gradients(c.X.astype(np.float64), held_z, 3 * U * np.abs(held_z), 0.0)
+    check(c, backward(c, X, None, None, Z8, by))
+
+
+SHAPES = [(1, 1, 1), (1, 256, 512), (2, 3, 5), (5, 16, 16), (7, 64, 33), (31, 100, 47), (33, 33, 65), (64, 512, 100), (129, 47, 130), (200, 5, 300),
+          (300, 203, 259), (1000, 64, 64), (2049, 32, 96), (3001, 130, 70), (10000, 96, 48), (20011, 40, 129), (66001, 24, 36), (40000, 128, 256),
+          (9000, 300, 515), (5000, 700, 33), (1, 2050, 7), (17, 1030, 1026), (3000, 40, 1200), (3000, 41, 1201), (40000, 20, 1), (40000, 3, 40),
+          (30000, 300, 30), (40000, 301, 3), (33000, 50, 30), (40001, 33, 65), (2000, 512, 1000), (32767, 36, 130), (32768, 36, 130), (1, 520, 1100),
+          (33, 513, 1024), (31, 512, 1030), (200, 260, 2050), (32767, 68, 130), (32769, 67, 129), (66001, 52, 68), (3000, 41, 2401), (100000, 24, 65),
+          (300000, 4, 20), (260000, 5, 30), (60000, 64, 513), (4097, 1000, 300)]
+
+
+@pytest.mark.parametrize("i", range(len(SHAPES)))
+def test_product(i):
+    every_way(Case(*SHAPES[i], ["none", "relu", "silu"][i % 3]))
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("n,m,k", [(7, 64, 33), (300, 203, 259), (33000, 50, 30), (20000, 64, 260), (2000, 512, 1000)])
+def test_activations(n, m, k, act):
+    every_way(Case(n, m, k, act, seed=1))
+
+
+UNALIGNED = [(1, 40, 30), (33, 33, 65), (300, 203, 259), (3001, 130, 70), (20011, 40, 129), (40000, 128, 256), (66001, 24, 36),
+             (9000, 300, 515), (3000, 41, 1201), (40000, 7, 65), (60000, 16, 260)]
+
+
+@pytest.mark.parametrize("i", range(len(UNALIGNED)))
+def test_product_unaligned(i):
+    every_way(Case(*UNALIGNED[i], ["none", "elu", "sigmoid", "gelu"][i % 4], bias=False, residual=False), 1)
+    every_way(Case(*UNALIGNED[i], ["elu", "sigmoid", "gelu"][i % 3], seed=2), 1)
+
+
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 32, 33, 64, 65, 127, 128, 129, 255, 256, 257, 511, 513])
+def test_few_rows(n):
+    every_way(Case(n, 72, 40, "gelu"))
+
+
+@pytest.mark.parametrize("act", ["elu", "sigmoid", "silu", "gelu"])
+@pytest.mark.parametrize("n,k", [(400, 50), (45000, 160)])
+def test_far_from_zero(act, n, k):
+    """Activations that are shut or open all the way: exp and erf at their ends."""
+    c = Case(n, 48, k, act, scale=60.0)
+    assert np.abs(c.Z).max() > 100
+    Y, Z = forward(c)
+    check(c, (Y, Z), ("Y", "Z"))
+    check(c, backward(c, dev(c.X), None, Z))
+    check(c, backward(c, dev(c.X)))
+
+
+@pytest.mark.parametrize("n,m,k", [(4, 16, 16), (3000, 64, 64), (60000, 130, 200)])
+def test_outputs_that_are_not_wanted_and_outputs_over_the_residual(n, m, k):
+    c = Case(n, m, k, "gelu")
+    Y, Z = forward(c)
+    assert torch.equal(forward(c, keep=False)[0], Y) and torch.equal(forward(c, over=True)[0], Y)
+    X = dev(c.X)
+    got, again = backward(c, X, None, Z), backward(c, X, None, Z, want_dx=False)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1]) and bool(torch.isnan(again[2]).all())
+
+
+@pytest.mark.parametrize("n,m,k", [(3, 24, 20), (500, 64, 96), (20000, 64, 320), (3000, 40, 2400), (60000, 64, 200), (3000, 41, 2401), (70000, 16, 320)])
+def test_what_is_not_finite_stays_where_it_belongs(n, m, k):
+    """An infinite or NaN input spoils its row of Y, a NaN gradient its row of dX and the weights that it meets; every other one is exact."""
+    c = Case(n, m, k, "silu")
+    clean, c.X = c.X, c.X.copy()
+    c.X[1, 2], c.X[n - 1, 0] = np.inf, np.nan
+    Y = host(forward(c)[0])
+    rest = [i for i in range(n) if i not in (1, n - 1)]
+    assert np.isnan(Y[n - 1]).all() and not np.isfinite(Y[1]).all()
+    assert (np.abs(Y[rest] - c.Y[rest]) <= c.Y_most[rest]).all()
+    c.X, clean = clean, c.dY
+    c.dY = c.dY.copy()
+    c.dY[0, 3] = np.nan
+    cols = [j for j in range(k) if j != 3]
+    for how in ({}, dict(Z=dev(c.Z.astype(np.float32)))):
+        dW, db, dX = (host(t) for t in backward(c, dev(c.X), **how))
+        assert np.isnan(dW[:, 3]).all() and np.isnan(db[3]) and np.isnan(dX[0]).all()
+        assert (np.abs(dX[1:] - c.dX[1:]) <= c.dX_most[1:]).all()
+        assert (np.abs(dW[:, cols] - c.dW[:, cols]) <= c.dW_most[:, cols]).all()
+    c.dY = clean
+
+
+@pytest.mark.parametrize("n,m,k", [(300, 40, 60), (3000, 40, 1200), (60000, 64, 200), (5000, 700, 1000)])
+def test_a_lost_row_in_8_bits_spoils_every_weight(n, m, k):
+    """Its scale is NaN, and it is in every sum over the rows; as with the same row in floats."""
+    c = Case(n, m, k, "none")
+    c.X[n // 2, 1] = np.inf
+    X8, _ = rows8(c.X)
+    dW, db, dX = (host(t) for t in backward(c, None, X8))
+    assert np.isnan(dW).all() and np.isfinite(db).all() and np.isfinite(dX).all()
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** 60])
+@pytest.mark.parametrize("n,k", [(20, 40), (3000, 40), (20000, 320), (60000, 320)])
+def test_magnitudes_far_from_one(n, k, scale):
+    c = Case(n, 40, k, "none", scale=scale)
+    c.dW_most = c.dW_most + n * 2.0 ** -126
+    Y, Z = forward(c)
+    check(c, (Y, Z), ("Y", "Z"))
+    check(c, backward(c, dev(c.X)))
+    X8, held = rows8(c.X, c.columns)
+    c.gradients(held, c.Z, 0.0, 3 * U)
+    c.dW_most = c.dW_most + n * 2.0 ** -126
+    check(c, backward(c, None, X8))
+
+
+@pytest.mark.parametrize("n,m,k", [(50, 48, 40), (5000, 64, 1100), (60000, 64, 320), (9000, 300, 1030)])
+def test_rows_in_8_bits_of_all_magnitudes(n, m, k):
+    """Scales over sixty powers of two: the rows of D times them are, too."""
+    c = Case(n, m, k, "silu")
+    c.X *= (2.0 ** np.random.default_rng(5).integers(-30, 31, (n, 1))).astype(np.float32)
+    X8, held = rows8(c.X, c.columns)
+    Z = c.Z.astype(np.float32)
+    c.gradients(held, Z.astype(np.float64), 0.0, 3 * U)
+    check(c, backward(c, None, X8, dev(Z)))
+
+
+def signs(rng, *shape):
+    return rng.choice(np.array([-1.0, 1.0], np.float32), shape)
+
+
+def twelve_bits(rng, *shape):
+    """Odd whole numbers of 2049 .. 4095 and either sign: one fp16 number holds eleven bits, so that each has a second part."""
+    return (2 * rng.integers(1024, 2048, shape) + 1).astype(np.float32) * signs(rng, *shape)
+
+
+@pytest.mark.parametrize("n,m,k", [(32, 512, 1030), (33, 512, 600), (200, 512, 1100), (4096, 300, 515), (4097, 300, 515), (9001, 130, 1201),
+                                   (40000, 128, 256), (33000, 50, 30), (66001, 52, 68), (3000, 40, 2400)])
+def test_second_parts_reach_every_sum(n, m, k):
+    """Whole numbers of twelve bits times +-1: every sum is exact (below 2^24 where few enough stand in it), bit for bit, from floats and
+    from rows in 8 bits (+-127 .. of scale 1), whichever operand has the second parts."""
+    rng = np.random.default_rng(n + m)
+    c = Case(n, m, k, "none", bias=False, residual=False)
+    c.X, c.W, c.dY = twelve_bits(rng, n, m), signs(rng, m, k), signs(rng, n, k)
+    Z = c.X.astype(np.float64) @ c.W
+    assert np.array_equal(host(forward(c)[1]), Z)
+    few = rng.random((n, 1)) < 4096.0 / n                  # so that sums of twelve bits over the rows stay below 2^24
+    X = (c.X * few).astype(np.float32)
+    got = [host(t) for t in backward(c, dev(X))]
+    dY = c.dY.astype(np.float64)
+    want = X.astype(np.float64).T @ dY
+    assert np.abs(want).max() < 2 ** 24 and np.array_equal(got[0], want) and np.array_equal(got[2], dY @ c.W.astype(np.float64).T)
+    # 8 bits: a 127 in each row makes its scale 1; sums over the rows of 7 bits times 12
+    q = rng.integers(-127, 128, (n, m)).astype(np.float32)
+    q[:, 0] = 127
+    c.dY = twelve_bits(rng, n, k) * (rng.random((n, k)) < 30.0 / n)
+    X8, held = rows8(q)
+    assert np.array_equal(held, q)
+    want = q.astype(np.float64).T @ c.dY
+    assert np.abs(want).max() < 2 ** 24
+    dW, db, dX = (host(t) for t in backward(c, None, X8))
+    assert np.array_equal(dW, want) and np.array_equal(db, c.dY.astype(np.float64).sum(0))
+
+
+def test_no_rows():
+    dW, db = torch.full((5, 6), NAN, device="cuda"), torch.full((6,), NAN, device="cuda")
+    B.gnn_linear_bwd(ID["silu"], 0, 5, 6, None, None, None, None, None, None, None, dW, db, None, B.alloc(B.gnn_linear_workspace_bytes(True, 0, 5, 6)))
+    assert not host(dW).any() and not host(db).any()
+
+
+@pytest.mark.parametrize("n,m,k", [(1, 100, 60), (300, 64, 96), (20000, 64, 320), (3000, 40, 2400), (70000, 16, 320), (33000, 31, 515), (20, 512, 1100)])
+def test_a_captured_step_replays(n, m, k):
+    c = Case(n, m, k, "gelu")
+    X, W, b, R, dY = (dev(a) for a in (c.X, c.W, c.b, c.R, c.dY))
+    X8, _ = rows8(c.X, c.columns)
+    ws = B.alloc(max(B.gnn_linear_workspace_bytes(back, n, m, k) for back in (0, 1)))
+    o = {name: torch.full(s, NAN, device="cuda") for name, s in dict(Y=(n, k), Z=(n, k), dW=(m, k), db=(k,), dX=(n, m), dW8=(m, k), dWa=(m, k)).items()}
+
+    def step():
+        B.gnn_linear_fwd(ID["gelu"], n, m, k, X, W, b, R, o["Y"], o["Z"], ws)
+        B.gnn_linear_bwd(ID["gelu"], n, m, k, X, None, W, b, o["Z"], None, dY, o["dW"], o["db"], o["dX"], ws)
+        B.gnn_linear_bwd(ID["gelu"], n, m, k, None, X8, W, b, o["Z"], None, dY, o["dW8"], None, None, ws)
+        B.gnn_linear_bwd(ID["gelu"], n, m, k, X, None, W, b, None, None, dY, o["dWa"], None, None, ws)
+
+    step()
+    want = {name: t.clone() for name, t in o.items()}
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    for _ in range(3):
+        for t in o.values():
+            t.fill_(NAN)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o[name], want[name]) for name in o)
+
+
+# ---- both operands in 8 bits ---------------------------------------------------------------------------------
+def check8(n, m, k, act, bias=True, residual=True, seed=0, over=False):
+    rng = np.random.default_rng(n + 3 * m + 5 * k + seed)
+    f32 = lambda *s: rng.standard_normal(s).astype(np.float32)  # noqa: E731
+    X8, _ = rows8(f32(n, m))
+    W8, _ = rows8(f32(k, m) / np.float32(np.sqrt(m)))
+    b, R = f32(k) / 4 if bias else None, f32(n, k) if residual else None
+    # whole numbers, so that a sum that cancels is zero here as well
+    x, w = (host(a.q)[:, :m].astype(np.float64) for a in (X8, W8))
+    acc = (x @ w.T) * host(X8.scale).astype(np.float64)[:, None] * host(W8.scale).astype(np.float64)
+    Z = acc + (b.astype(np.float64) if bias else 0.0)
+    a, _ = blocks.act(act, Z)
+    want = a + (R if residual else 0.0)
+    most = 1.13 * 4 * U * (np.abs(acc) + np.abs(Z)) + 16 * U * np.abs(a) + 2 * U * np.abs(want)
+    Y = space(n, k)
+    r = dev(R) if residual else None
+    out = r if over else Y[0]
+    B.gnn_linear8_fwd(ID[act], n, m, k, X8, W8, dev(b) if bias else None, r, out)
+    within(out, want, most, "Y")
+    assert bool((Y[1] == 7.0).all())
+
+
+SHAPES8 = [(1, 1, 1), (1, 512, 1024), (2, 3, 5), (5, 16, 16), (7, 64, 33), (31, 100, 47), (33, 33, 65), (64, 512, 100), (129, 47, 130), (200, 5, 300),
+           (300, 203, 259), (1000, 64, 64), (3001, 130, 70), (20011, 40, 129), (66001, 24, 36), (40000, 128, 256), (9000, 300, 515), (1, 5000, 7),
+           (17, 1030, 1026), (3000, 41, 1201), (40000, 20, 1), (2000, 2048, 513), (4097, 1000, 300), (128, 128, 128), (127, 127, 127), (256, 96, 2050)]
+
+
+@pytest.mark.parametrize("i", range(len(SHAPES8)))
+def test_product_in_8_bits(i):
+    n, m, k = SHAPES8[i]
+    check8(n, m, k, ACTS[i % 6])
+    check8(n, m, k, ACTS[(i + 3) % 6], bias=False, residual=False, seed=1)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("n", [5, 3000])
+def test_activations_of_the_product_in_8_bits(n, act):
+    check8(n, 96, 130, act)
+
+
+def test_product_in_8_bits_over_its_residual():
+    for n in (3, 5000):
+        check8(n, 100, 70, "gelu", over=True)
+
+
+@pytest.mark.parametrize("n,k", [(2, 40), (300, 300)])
+def test_sums_of_the_largest_integers_are_exact(n, k):
+    m = 1 << 17
+    q = np.full((max(n, k), m), 127, np.int8)
+    sign = np.where(np.arange(max(n, k)) % 2, -1, 1).astype(np.int8)
+    q *= sign[:, None]
+    one = lambda r: torch.ones(r, device="cuda")  # noqa: E731
+    Y = torch.full((n, k), NAN, device="cuda")
+    B.gnn_linear8_fwd(0, n, m, k, B.Rows8(dev(q[:n]), one(n)), B.Rows8(dev(q[:k]), one(k)), None, None, Y)
+    assert np.array_equal(host(Y), np.outer(sign[:n], sign[:k]) * np.float32(127 * 127 * m))
+
+
+@pytest.mark.parametrize("n,m,k", [(3, 40, 50), (5000, 203, 300)])
+def test_a_lost_row_is_lost_alone(n, m, k):
+    rng = np.random.default_rng(8)
+    x = rng.standard_normal((n, m)).astype(np.float32)
+    x[1, 2] = np.nan
+    X8, _ = rows8(x)
+    W8, _ = rows8(rng.standard_normal((k, m)).astype(np.float32))
+    Y = torch.empty(n, k, device="cuda")
+    B.gnn_linear8_fwd(0, n, m, k, X8, W8, None, None, Y)
+    Y = host(Y)
+    assert np.isnan(Y[1]).all() and np.isfinite(np.delete(Y, 1, 0)).all()
+
+
+@pytest.mark.parametrize("n", [1, 4000])
+def test_a_captured_product_in_8_bits_replays(n):
+    m, k = 200, 300
+    rng = np.random.default_rng(9)
+    (X8, _), (W8, _) = (rows8(rng.standard_normal((r, m)).astype(np.float32)) for r in (n, k))
+    Y = torch.full((n, k), NAN, device="cuda")
+    call = lambda: B.gnn_linear8_fwd(ID["silu"], n, m, k, X8, W8, None, None, Y)  # noqa: E731
+    call()
+    want = Y.clone()
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            call()
+    for _ in range(3):
+        Y.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, want)
