@@ -276,19 +276,31 @@ gemm_half_kernel(HalfProduct g) {
         float bias[NT];
 #pragma unroll
         for (int c = 0; c < NT; ++c) bias[c] = g.bias ? g.bias[min((ct0 + c) * 32 + l, g.N - 1)] : 0.f;
+        // all of R that the lane needs is under way at once, none of it behind a branch
+        float r[NT][16];
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+#pragma unroll
+            for (int c = 0; c < NT; ++c) r[c][v] = 0.f;
+        if (g.linear.R)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    r[c][v] = g.linear.R[(size_t)min(row0 + 8 * (v / 4) + 4 * half + v % 4, g.M - 1) * g.N + min((ct0 + c) * 32 + l, g.N - 1)];
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int row = row0 + 8 * (v / 4) + 4 * half + v % 4;
 #pragma unroll
             for (int c = 0; c < NT; ++c) {                 // the columns of a row one after the other
                 const int n = (ct0 + c) * 32 + l;
-                if (row >= g.M || n >= g.N) continue;
-                const size_t at = (size_t)row * g.N + n;
                 const float z = value(c, v) + bias[c];
                 float y, slope;
                 activate<GATE, false>(z, y, slope);
+                if (row >= g.M || n >= g.N) continue;
+                const size_t at = (size_t)row * g.N + n;
                 if (g.linear.Z) out(g.linear.Z + at, z);
-                out(g.linear.Y + at, g.linear.R ? y + g.linear.R[at] : y);
+                out(g.linear.Y + at, y + r[c][v]);
             }
         }
     } else {
