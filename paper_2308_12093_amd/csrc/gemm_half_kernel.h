@@ -273,36 +273,48 @@ gemm_half_kernel(HalfProduct g) {
             }
         }
     } else if constexpr (OUT == kLinearForward) {
-        float bias[NT];
+        // two tiles at a time, the part of R that they need under way at once.  Addresses are a scalar base and the lane's own 32-bit offset;
+        // only blocks at an edge compare rows and columns.
+        auto finish = [&](auto whole) __attribute__((always_inline)) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            const size_t corner = (size_t)row0 * g.N + ct0 * 32;
+            const unsigned mine = 4u * half * (unsigned)g.N + l;
+            auto there = [&](int c, int v) __attribute__((always_inline)) {
+                return WHOLE || (row0 + 8 * (v / 4) + 4 * half + v % 4 < g.M && (ct0 + c) * 32 + l < g.N);
+            };
+            auto at = [&](int c, int v) __attribute__((always_inline)) { return corner + (size_t)(8 * (v / 4) + v % 4) * g.N + 32 * c; };
 #pragma unroll
-        for (int c = 0; c < NT; ++c) bias[c] = g.bias ? g.bias[min((ct0 + c) * 32 + l, g.N - 1)] : 0.f;
-        // all of R that the lane needs is under way at once, none of it behind a branch
-        float r[NT][16];
+            for (int c0 = 0; c0 < NT; c0 += 2) {
+                float r[2][16], bias[2];
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
+                for (int i = 0; i < 2; ++i) bias[i] = g.bias ? g.bias[min((ct0 + c0 + i) * 32 + l, g.N - 1)] : 0.f;
+                if constexpr (WHOLE) {
 #pragma unroll
-            for (int c = 0; c < NT; ++c) r[c][v] = 0.f;
-        if (g.linear.R)
+                    for (int v = 0; v < 16; ++v)
 #pragma unroll
-            for (int v = 0; v < 16; ++v)
+                        for (int i = 0; i < 2; ++i) r[i][v] = 0.f;
+                    if (g.linear.R)
 #pragma unroll
-                for (int c = 0; c < NT; ++c)
-                    r[c][v] = g.linear.R[(size_t)min(row0 + 8 * (v / 4) + 4 * half + v % 4, g.M - 1) * g.N + min((ct0 + c) * 32 + l, g.N - 1)];
+                        for (int v = 0; v < 16; ++v)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int row = row0 + 8 * (v / 4) + 4 * half + v % 4;
+                            for (int i = 0; i < 2; ++i) r[i][v] = (g.linear.R + at(c0 + i, v))[mine];
+                }
 #pragma unroll
-            for (int c = 0; c < NT; ++c) {                 // the columns of a row one after the other
-                const int n = (ct0 + c) * 32 + l;
-                const float z = value(c, v) + bias[c];
-                float y, slope;
-                activate<GATE, false>(z, y, slope);
-                if (row >= g.M || n >= g.N) continue;
-                const size_t at = (size_t)row * g.N + n;
-                if (g.linear.Z) out(g.linear.Z + at, z);
-                out(g.linear.Y + at, y + r[c][v]);
+                for (int v = 0; v < 16; ++v)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int c = c0 + i;
+                        const float z = value(c, v) + bias[i];
+                        float y, slope;
+                        activate<GATE, false>(z, y, slope);
+                        if (!there(c, v)) continue;
+                        if (g.linear.Z) (g.linear.Z + at(c, v))[mine] = z;
+                        (g.linear.Y + at(c, v))[mine] = y + (WHOLE ? r[i][v] : g.linear.R ? (g.linear.R + at(c, v))[mine] : 0.f);
+                    }
             }
-        }
+        };
+        if (g.M - row0 >= 32 && g.N - ct0 * 32 >= 32 * NT) finish(std::true_type());
+        else finish(std::false_type());
     } else {
         const int k = GATED ? g.gated.half : g.N, width = GATED ? 2 * k : k;   // of D
         unsigned col_top[NT], row_top[16];

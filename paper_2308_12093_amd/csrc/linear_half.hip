@@ -12,7 +12,6 @@ int linear_row_parts(int64_t n, int64_t k) { return (int)ceil_div(k, 32 * half_t
 gnn_status_t linear_half_launch(int act, int64_t M, int64_t N, int64_t K, const float *X, const unsigned *row_tops, const float *W,
                                 const float *bias, const Linear &out, const Tops &tops, void *workspace, hipStream_t st) {
     HalfProduct g{};
-    const int w = half_tiles(M, N);
     set_product(g, M, N, K, workspace);
     g.A = X; g.row_tops = row_tops; g.top_parts = top_parts(K, X);
     g.B = HalfOperand{W, (long)N, 1};
@@ -20,8 +19,9 @@ gnn_status_t linear_half_launch(int act, int64_t M, int64_t N, int64_t K, const 
     g.linear = out;
     g.tops = tops;
     const bool back = out.D != nullptr;
-    g.stream = !back && (size_t)M * N * sizeof(float) > kStreamBytes;       // D is read next
     const int rows = K < kShortReduction ? kShort : K % 4 == 0 && K < 1 << 24 && aligned16(X) ? kCopied : kLoaded;
+    const int w = half_tiles(M, N);
+    g.stream = !back && (size_t)M * N * sizeof(float) > kStreamBytes;       // D is read next
     if (rows != kShort) GNN_TRY(split_weights(g, w, 0, st));
     const dim3 grid = product_grid(g);
 #define LINEAR_CASE(NT_, ROWS_, ACT_)                                                                                       \
