@@ -215,6 +215,20 @@ gnn_status_t gradient(int act, int64_t n, int k, const float *Z, const Rows8 &he
     return launch_status();
 }
 
+// of X W, whichever kernel forms it
+size_t product_bytes(int64_t k, int64_t m) {
+    const size_t pair = pair_workspace_bytes(k, m), half = linear_half_workspace_bytes(k, m);
+    return pair > half ? pair : half;
+}
+
+// act(X W + b) + R, or D and its largest magnitudes, `parts` a row
+gnn_status_t product(int act, int64_t n, int64_t m, int64_t k, const float *X, const unsigned *row_tops, const float *W, const float *b,
+                     const Linear &g, const Tops &tops, int *parts, void *workspace, hipStream_t st) {
+    const bool pair = pair_product_fits(n, k, m, X);
+    *parts = pair ? pair_row_parts(k) : linear_row_parts(n, k);
+    return (pair ? pair_linear_launch : linear_half_launch)(act, n, k, m, X, row_tops, W, b, g, tops, workspace, st);
+}
+
 // scratch of a backward pass behind D and X
 struct Backward {
     unsigned *x_rows, *x_cols, *d_rows, *d_cols;
@@ -224,11 +238,11 @@ struct Backward {
         Carver carve(at);
         x_rows = carve.take<unsigned>(n * ceil_div(m, 64));
         x_cols = carve.take<unsigned>(most_top_blocks(n) * m);
-        d_rows = carve.take<unsigned>(n * ceil_div(k, 64));      // linear_row_parts(n, k), those of `gradient` or top_parts
+        d_rows = carve.take<unsigned>(n * (ceil_div(k, 64) + 1));  // those of `product`, of `gradient` or top_parts
         d_cols = carve.take<unsigned>(most_top_blocks(n) * k);
         rest = carve.take<char>(0);
-        size_t most = linear_half_workspace_bytes(k, m);
-        for (size_t b : {gemm_half_workspace_bytes(m, k), gemm_half_tn_workspace_bytes(m, k, n), gemm_workspace_bytes(0, 1, n, m, k)})
+        size_t most = product_bytes(k, m);
+        for (size_t b : {pair_workspace_bytes(m, k), gemm_half_workspace_bytes(m, k), gemm_half_tn_workspace_bytes(m, k, n), gemm_workspace_bytes(0, 1, n, m, k)})
             if (b > most) most = b;
         bytes = carve.off + most;
     }
@@ -249,7 +263,7 @@ bool linear_fits(bool backward, int64_t n, int64_t m, int64_t k) {
 
 // What n rows take, or fewer: a product of few rows needs less.
 size_t linear_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k) {
-    if (!backward) return linear_few(n, m, k) ? kAlign : align_up((size_t)n * ceil_div(m, 64) * sizeof(unsigned)) + linear_half_workspace_bytes(k, m);
+    if (!backward) return linear_few(n, m, k) ? kAlign : align_up((size_t)n * ceil_div(m, 64) * sizeof(unsigned)) + product_bytes(k, m);
     const size_t d = align_up((size_t)n * k * sizeof(float)) + align_up((size_t)n * m * sizeof(float));
     size_t most = 0;
     const int64_t small = few_rows(n, m, k);
@@ -274,7 +288,8 @@ gnn_status_t linear_forward_launch(int act, int n, int m, int k, const float *X,
     Carver carve(workspace);
     const Tops tops{carve.take<unsigned>((size_t)n * ceil_div(m, 64)), nullptr};
     if (m >= kShortReduction) GNN_TRY(tops_launch(n, m, X, tops, st));
-    return linear_half_launch(act, n, k, m, X, tops.rows, W, b, g, Tops{nullptr, nullptr}, carve.take<char>(0), st);
+    int parts;
+    return product(act, n, m, k, X, tops.rows, W, b, g, Tops{nullptr, nullptr}, &parts, carve.take<char>(0), st);
 }
 
 gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X, const Rows8 &X8, const float *W, const float *b,
@@ -325,10 +340,10 @@ gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X
     } else if (kept) {
         GNN_TRY(gradient(act, n, k, Z, Z8, dY, nullptr, d_space, of_d, &parts, st));
     } else {
-        GNN_TRY(linear_half_launch(act, n, k, m, X, w.x_rows, W, b, g, of_d, w.rest, st));
-        parts = linear_row_parts(n, k);
+        GNN_TRY(product(act, n, m, k, X, w.x_rows, W, b, g, of_d, &parts, w.rest, st));
     }
     if (dX && short_columns(k)) GNN_TRY(gemm_launch(0, 1, n, m, k, d, W, dX, nullptr, 0, w.rest, st));
+    else if (dX && pair_product_fits(n, m, k, d)) GNN_TRY(pair_plain_launch(n, m, k, d, w.d_rows, parts, W, dX, w.rest, st));
     else if (dX) GNN_TRY(gemm_half_launch(n, m, k, d, w.d_rows, parts, W, dX, w.rest, st));
     return gemm_half_tn_launch(m, k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
 }
