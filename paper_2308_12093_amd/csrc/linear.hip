@@ -104,7 +104,8 @@ linear_gradient_kernel(long n, int k, int lanes, int rows, int parts, const floa
             if (row >= r1 || c >= k) continue;
             if (row_scale) factor[i] = row_scale[row];
             if constexpr (VEC == 4) {
-                const float4 y = *reinterpret_cast<const float4 *>(dY + at);
+                // each read once: not in the place of D, which the products read next
+                const floatx4 y = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(dY + at));
                 d[i][0] = y.x; d[i][1] = y.y; d[i][2] = y.z; d[i][3] = y.w;
                 if constexpr (ACT != GNN_ACT_NONE) {
                     float4 x;
@@ -117,7 +118,8 @@ linear_gradient_kernel(long n, int k, int lanes, int rows, int parts, const floa
                             x = make_float4(x.x * e.x, x.y * e.y, x.z * e.z, x.w * e.w);
                         }
                     } else {
-                        x = *reinterpret_cast<const float4 *>(Z + at);
+                        const floatx4 v = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(Z + at));
+                        x = make_float4(v.x, v.y, v.z, v.w);
                     }
                     z[i][0] = x.x; z[i][1] = x.y; z[i][2] = x.z; z[i][3] = x.w;
                 }
@@ -242,7 +244,7 @@ struct Backward {
         d_cols = carve.take<unsigned>(most_top_blocks(n) * k);
         rest = carve.take<char>(0);
         size_t most = product_bytes(k, m);
-        for (size_t b : {pair_workspace_bytes(m, k), gemm_half_workspace_bytes(m, k), gemm_half_tn_workspace_bytes(m, k, n), gemm_workspace_bytes(0, 1, n, m, k)})
+        for (size_t b : {pair_workspace_bytes(m, k), pair_tn_workspace_bytes(m, k, n), gemm_half_workspace_bytes(m, k), gemm_half_tn_workspace_bytes(m, k, n), gemm_workspace_bytes(0, 1, n, m, k)})
             if (b > most) most = b;
         bytes = carve.off + most;
     }
@@ -303,14 +305,18 @@ gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X
     float *d_space = carve.take<float>((size_t)n * k), *x_space = carve.take<float>((size_t)n * m);
     const bool plain = act == GNN_ACT_NONE, kept = Z || Z8.q;
     const float *d = plain ? dY : d_space;
-    if (!X) {
+    const bool is_few = linear_few(n, m, k), pair_tn = !is_few && pair_tn_fits(m, k, n, !X);
+    const float *row_scale = nullptr;                      // what X8's rows are to be taken times, where its integers are read as they are
+    if (!X && pair_tn) {
+        row_scale = X8.scale;
+    } else if (!X) {
         GNN_TRY(dequantize_rows_launch(n, m, X8, x_space, st));
         X = x_space;
     }
     const Linear g{nullptr, nullptr, nullptr, dY, d_space};
     const bool one_step = n < kShortReduction;             // X^T D does without largest magnitudes
     int parts = 0;
-    if (linear_few(n, m, k)) {
+    if (is_few) {
         void *rest = carve.take<char>(0);
         const bool wide = wide_weights(m, k);
         const Backward w(static_cast<char *>(rest), n, m, k);
@@ -332,19 +338,20 @@ gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X
         return gemm_launch(1, 0, m, k, n, X, d, dW, nullptr, 0, rest, st, nullptr, 0, 0, nullptr, nullptr, &extras);
     }
     const Backward w(static_cast<char *>(workspace) + carve.off, n, m, k);
-    const Tops of_x{plain || kept || m < kShortReduction ? nullptr : w.x_rows, one_step ? nullptr : w.x_cols}, of_d{w.d_rows, w.d_cols};
+    const Tops of_x{plain || kept || m < kShortReduction ? nullptr : w.x_rows, one_step || !X ? nullptr : w.x_cols}, of_d{w.d_rows, w.d_cols};
     if (of_x.rows || of_x.cols) GNN_TRY(tops_launch(n, m, X, of_x, st));
-    if (plain) {
+    if (plain && !row_scale) {
         GNN_TRY(tops_launch(n, k, dY, of_d, st));
         parts = top_parts(k, dY);
-    } else if (kept) {
-        GNN_TRY(gradient(act, n, k, Z, Z8, dY, nullptr, d_space, of_d, &parts, st));
+    } else if (plain || kept) {
+        GNN_TRY(gradient(act, n, k, Z, Z8, dY, row_scale, plain ? nullptr : d_space, of_d, &parts, st));
     } else {
         GNN_TRY(product(act, n, m, k, X, w.x_rows, W, b, g, of_d, &parts, w.rest, st));
     }
     if (dX && short_columns(k)) GNN_TRY(gemm_launch(0, 1, n, m, k, d, W, dX, nullptr, 0, w.rest, st));
     else if (dX && pair_product_fits(n, m, k, d)) GNN_TRY(pair_plain_launch(n, m, k, d, w.d_rows, parts, W, dX, w.rest, st));
     else if (dX) GNN_TRY(gemm_half_launch(n, m, k, d, w.d_rows, parts, W, dX, w.rest, st));
+    if (pair_tn) return pair_tn_launch(m, k, n, X, X8, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
     return gemm_half_tn_launch(m, k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
 }
 

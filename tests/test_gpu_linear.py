@@ -119,7 +119,10 @@ SHAPES = [(1, 1, 1), (1, 256, 512), (2, 3, 5), (5, 16, 16), (7, 64, 33), (31, 10
           (9000, 300, 515), (5000, 700, 33), (1, 2050, 7), (17, 1030, 1026), (3000, 40, 1200), (3000, 41, 1201), (40000, 20, 1), (40000, 3, 40),
           (30000, 300, 30), (40000, 301, 3), (33000, 50, 30), (40001, 33, 65), (2000, 512, 1000), (32767, 36, 130), (32768, 36, 130), (1, 520, 1100),
           (33, 513, 1024), (31, 512, 1030), (200, 260, 2050), (32767, 68, 130), (32769, 67, 129), (66001, 52, 68), (3000, 41, 2401), (100000, 24, 65),
-          (300000, 4, 20), (260000, 5, 30), (60000, 64, 513), (4097, 1000, 300)]
+          (300000, 4, 20), (260000, 5, 30), (60000, 64, 513), (4097, 1000, 300),
+          # pairs in one scale: tiles of 128 x 128 and 128 x 256, ragged rows, columns and reductions, chunks that end inside a step
+          (33001, 132, 256), (17003, 260, 390), (17000, 68, 516), (8200, 100, 1028), (32769, 36, 640), (45000, 200, 200), (16400, 516, 260),
+          (33001, 131, 257), (9001, 400, 900)]
 
 
 @pytest.mark.parametrize("i", range(len(SHAPES)))
@@ -170,7 +173,8 @@ def test_outputs_that_are_not_wanted_and_outputs_over_the_residual(n, m, k):
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1]) and bool(torch.isnan(again[2]).all())
 
 
-@pytest.mark.parametrize("n,m,k", [(3, 24, 20), (500, 64, 96), (20000, 64, 320), (3000, 40, 2400), (60000, 64, 200), (3000, 41, 2401), (70000, 16, 320)])
+@pytest.mark.parametrize("n,m,k", [(3, 24, 20), (500, 64, 96), (20000, 64, 320), (3000, 40, 2400), (60000, 64, 200), (3000, 41, 2401), (70000, 16, 320),
+                                   (33001, 132, 256), (16400, 260, 516)])
 def test_what_is_not_finite_stays_where_it_belongs(n, m, k):
     """An infinite or NaN input spoils its row of Y, a NaN gradient its row of dX and the weights that it meets; every other one is exact."""
     c = Case(n, m, k, "silu")
@@ -192,7 +196,7 @@ def test_what_is_not_finite_stays_where_it_belongs(n, m, k):
     c.dY = clean
 
 
-@pytest.mark.parametrize("n,m,k", [(300, 40, 60), (3000, 40, 1200), (60000, 64, 200), (5000, 700, 1000)])
+@pytest.mark.parametrize("n,m,k", [(300, 40, 60), (3000, 40, 1200), (60000, 64, 200), (5000, 700, 1000), (33001, 132, 256)])
 def test_a_lost_row_in_8_bits_spoils_every_weight(n, m, k):
     """Its scale is NaN, and it is in every sum over the rows; as with the same row in floats."""
     c = Case(n, m, k, "none")
@@ -203,9 +207,9 @@ def test_a_lost_row_in_8_bits_spoils_every_weight(n, m, k):
 
 
 @pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** 60])
-@pytest.mark.parametrize("n,k", [(20, 40), (3000, 40), (20000, 320), (60000, 320)])
-def test_magnitudes_far_from_one(n, k, scale):
-    c = Case(n, 40, k, "none", scale=scale)
+@pytest.mark.parametrize("n,m,k", [(20, 40, 40), (3000, 40, 40), (20000, 40, 320), (60000, 40, 320), (33001, 132, 256)])
+def test_magnitudes_far_from_one(n, m, k, scale):
+    c = Case(n, m, k, "none", scale=scale)
     c.dW_most = c.dW_most + n * 2.0 ** -126
     Y, Z = forward(c)
     check(c, (Y, Z), ("Y", "Z"))
@@ -216,7 +220,7 @@ def test_magnitudes_far_from_one(n, k, scale):
     check(c, backward(c, None, X8))
 
 
-@pytest.mark.parametrize("n,m,k", [(50, 48, 40), (5000, 64, 1100), (60000, 64, 320), (9000, 300, 1030)])
+@pytest.mark.parametrize("n,m,k", [(50, 48, 40), (5000, 64, 1100), (60000, 64, 320), (9000, 300, 1030), (33001, 132, 256)])
 def test_rows_in_8_bits_of_all_magnitudes(n, m, k):
     """Scales over sixty powers of two: the rows of D times them are, too."""
     c = Case(n, m, k, "silu")
@@ -237,7 +241,8 @@ def twelve_bits(rng, *shape):
 
 
 @pytest.mark.parametrize("n,m,k", [(32, 512, 1030), (33, 512, 600), (200, 512, 1100), (4096, 300, 515), (4097, 300, 515), (9001, 130, 1201),
-                                   (40000, 128, 256), (33000, 50, 30), (66001, 52, 68), (3000, 40, 2400)])
+                                   (40000, 128, 256), (33000, 50, 30), (66001, 52, 68), (3000, 40, 2400), (33001, 132, 256), (17003, 260, 390),
+                                   (16400, 516, 260)])
 def test_second_parts_reach_every_sum(n, m, k):
     """Whole numbers of twelve bits times +-1: every sum is exact (below 2^24 where few enough stand in it), bit for bit, from floats and
     from rows in 8 bits (+-127 .. of scale 1), whichever operand has the second parts."""
@@ -264,13 +269,30 @@ def test_second_parts_reach_every_sum(n, m, k):
     assert np.array_equal(dW, want) and np.array_equal(db, c.dY.astype(np.float64).sum(0))
 
 
+@pytest.mark.parametrize("n,m,k", [(33001, 132, 256), (50, 48, 40), (9000, 300, 515)])
+def test_elements_far_below_the_largest_are_held_to_a_part_of_it(n, m, k):
+    """A feature, and below a row, of 2^30 that meets zeros: the others, of magnitude 1, are held to 2^-40 of it each."""
+    held = 2.0 ** -10
+    c = Case(n, m, k, "none", residual=False)
+    c.X[:, 7], c.W[7] = 2.0 ** 30, 0.0
+    c.define()
+    within(forward(c)[1], c.Z, c.Z_most + held * np.abs(c.W).sum(0), "Z")
+    c = Case(n, m, k, "none", residual=False)
+    c.X[n // 3], c.dY[n // 3] = 2.0 ** 30, 0.0
+    dW = backward(c, dev(c.X))[0]
+    X, dY = c.X.astype(np.float64), c.dY.astype(np.float64)
+    X[n // 3] = 0.0
+    C = 64 + 8 * ((min(n, 4096) + 15) // 16)
+    within(dW, X.T @ dY, C * U * (np.abs(X).T @ np.abs(dY)) + held * np.abs(dY).sum(0), "dW")
+
+
 def test_no_rows():
     dW, db = torch.full((5, 6), NAN, device="cuda"), torch.full((6,), NAN, device="cuda")
     B.gnn_linear_bwd(ID["silu"], 0, 5, 6, None, None, None, None, None, None, None, dW, db, None, B.alloc(B.gnn_linear_workspace_bytes(True, 0, 5, 6)))
     assert not host(dW).any() and not host(db).any()
 
 
-@pytest.mark.parametrize("n,m,k", [(1, 100, 60), (300, 64, 96), (20000, 64, 320), (3000, 40, 2400), (70000, 16, 320), (33000, 31, 515), (20, 512, 1100)])
+@pytest.mark.parametrize("n,m,k", [(33001, 132, 256), (1, 100, 60), (300, 64, 96), (20000, 64, 320), (3000, 40, 2400), (70000, 16, 320), (33000, 31, 515), (20, 512, 1100)])
 def test_a_captured_step_replays(n, m, k):
     c = Case(n, m, k, "gelu")
     X, W, b, R, dY = (dev(a) for a in (c.X, c.W, c.b, c.R, c.dY))
