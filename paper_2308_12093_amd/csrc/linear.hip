@@ -173,17 +173,25 @@ linear_gradient_kernel(long n, int k, int lanes, int rows, int parts, const floa
 
 // the other kernels read four indices at a time
 bool too_narrow(int64_t m, int64_t k) { return m < 4 || k < 4; }
-// Tiles of 32 x 32 of Y up to which the kernels for few rows are taken
-int64_t few_tiles(int64_t m) { return m < 32 ? 8000 : 260000 / m; }
+// Tiles of 32 x 32 of Y up to which the kernels for few rows are the faster; their time goes with tiles times f_in, where the others begin at
+// three launches forward (one below 32 features) and six backward.  Few rows / others in us, forward with SiLU and Z: 128000 x 32 -> 64,
+// 8000 tiles, 21 / 23; 256000, 16000, 39 / 37; 32000 x 64 -> 256, 8000, 24.6 / 24.2; 16000 x 128 -> 128, 2000, 14.4 / 17.0; 32000, 4000,
+// 23 / 21; 1984 x 256 -> 1024, 2000, 20.8 / 20.8; 1984 x 512 -> 512, 1000, 19.8 / 24.8; 4000, 2000, 35 / 27; 992 x 1024 -> 1024, 1000,
+// 33.5 / 37.7; 1984, 2000, 63 / 40; 7104 x 203 -> 259, 2000, 22.2 / 23.7.  Backward from Z: 32000 x 64 -> 256, 8000, 71 / 76; 64000, 16000,
+// 112 / 97; 32000 x 128 -> 128, 4000, 60 / 61; 4000 x 256 -> 256, 1000, 45 / 54; 8000, 2000, 67 / 64; 992 x 512 -> 512, 500, 42 / 54;
+// 1984, 1000, 68 / 65; 480 x 1024 -> 1024, 500, 53 / 66; 992, 1000, 87 / 73; 3552 x 203 -> 259, 1000, 47 / 51.
+int64_t few_tiles(bool backward, int64_t m) { return m < 32 ? 8000 : backward ? 500000 / m + 150 : 380000 / m + 650; }
 // weights whose gradient is better off in float than through partial products of doubles and the pass over those, however few the rows
 bool wide_weights(int64_t m, int64_t k) { return !too_narrow(m, k) && m * k >= 1 << 19; }
 // D W^T is a product of the layers
 bool short_columns(int64_t k) { return k < kShortReduction; }
-bool linear_few(int64_t n, int64_t m, int64_t k) { return too_narrow(m, k) || ceil_div(n, 32) * ceil_div(k, 32) <= few_tiles(m); }
-// the rows up to which that is so
+bool linear_few(bool backward, int64_t n, int64_t m, int64_t k) {
+    return too_narrow(m, k) || ceil_div(n, 32) * ceil_div(k, 32) <= few_tiles(backward, m);
+}
+// the rows up to which a backward pass takes them
 int64_t few_rows(int64_t n, int64_t m, int64_t k) {
     if (too_narrow(m, k)) return n;
-    const int64_t rows = 32 * (few_tiles(m) / ceil_div(k, 32));
+    const int64_t rows = 32 * (few_tiles(true, m) / ceil_div(k, 32));
     return n < rows ? n : rows;
 }
 
@@ -257,7 +265,7 @@ struct Backward {
 bool linear_fits(bool backward, int64_t n, int64_t m, int64_t k) {
     if (m > 1 << 21 || k > 1 << 21) return false;
     const int64_t rows = ceil_div(n, 32), most = (int64_t)1 << 24;
-    if (linear_few(n, m, k))
+    if (linear_few(backward, n, m, k))
         return rows * ceil_div(k, 32) < most && (!backward || (gemm_fits(n, m, k) && gemm_half_tn_fits(m, k, n)));
     return rows * ceil_div(m > k ? m : k, 64) < most && gemm_half_fits(n, k) &&
            (!backward || ((short_columns(k) ? gemm_fits(n, m, k) : gemm_half_fits(n, m)) && gemm_half_tn_fits(m, k, n)));
@@ -265,7 +273,7 @@ bool linear_fits(bool backward, int64_t n, int64_t m, int64_t k) {
 
 // What n rows take, or fewer: a product of few rows needs less.
 size_t linear_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k) {
-    if (!backward) return linear_few(n, m, k) ? kAlign : align_up((size_t)n * ceil_div(m, 64) * sizeof(unsigned)) + product_bytes(k, m);
+    if (!backward) return linear_few(false, n, m, k) ? kAlign : align_up((size_t)n * ceil_div(m, 64) * sizeof(unsigned)) + product_bytes(k, m);
     const size_t d = align_up((size_t)n * k * sizeof(float)) + align_up((size_t)n * m * sizeof(float));
     size_t most = 0;
     const int64_t small = few_rows(n, m, k);
@@ -275,7 +283,7 @@ size_t linear_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k) {
         const size_t x = gemm_workspace_bytes(0, 1, small, m, k);
         if (x > most) most = x;
     }
-    if (!linear_few(n, m, k) || wide_weights(m, k)) {
+    if (!linear_few(true, n, m, k) || wide_weights(m, k)) {
         const Backward w(nullptr, n, m, k);
         if (w.bytes > most) most = w.bytes;
     }
@@ -286,7 +294,7 @@ gnn_status_t linear_forward_launch(int act, int n, int m, int k, const float *X,
                                    float *Z, void *workspace, hipStream_t st) {
     if (n <= 0) return GNN_OK;
     const Linear g{R, Y, Z, nullptr, nullptr};
-    if (linear_few(n, m, k)) return few(act, n, m, k, X, W, b, g, st);
+    if (linear_few(false, n, m, k)) return few(act, n, m, k, X, W, b, g, st);
     Carver carve(workspace);
     const Tops tops{carve.take<unsigned>((size_t)n * ceil_div(m, 64)), nullptr};
     if (m >= kShortReduction) GNN_TRY(tops_launch(n, m, X, tops, st));
@@ -305,7 +313,7 @@ gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X
     float *d_space = carve.take<float>((size_t)n * k), *x_space = carve.take<float>((size_t)n * m);
     const bool plain = act == GNN_ACT_NONE, kept = Z || Z8.q;
     const float *d = plain ? dY : d_space;
-    const bool is_few = linear_few(n, m, k), pair_tn = !is_few && pair_tn_fits(m, k, n, !X);
+    const bool is_few = linear_few(true, n, m, k), pair_tn = !is_few && pair_tn_fits(m, k, n, !X);
     const float *row_scale = nullptr;                      // what X8's rows are to be taken times, where its integers are read as they are
     if (!X && pair_tn) {
         row_scale = X8.scale;

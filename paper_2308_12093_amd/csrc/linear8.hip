@@ -195,7 +195,11 @@ linear8_few_kernel(Product8 g) {
     }
 }
 
-bool linear8_few(int64_t n, int64_t k) { return ceil_div(n, 128) * ceil_div(k, 128) < 128; }
+// Tiles of 32 x 32 of Y up to which the kernel for few rows is the faster: its time goes with tiles times f_in.  It / the other in us, with
+// SiLU: 4096 x 128 -> 512, 2048 tiles, 6.0 / 5.7; 1024 x 512 -> 512, 512, 5.0 / 6.5; 2048, 1024, 7.3 / 6.7; 2048 x 1024 -> 256, 512,
+// 6.6 / 8.3; 4096, 1024, 11.6 / 8.6; 512 x 2048 -> 1024, 512, 10.2 / 12.2; 1024, 1024, 18.1 / 12.5; 8192 x 203 -> 259, 2304, 8.4 / 8.8;
+// 32768 x 64 -> 64, 2048, 4.9 / 11.9.
+bool linear8_few(int64_t n, int64_t m, int64_t k) { return ceil_div(n, 32) * ceil_div(k, 32) <= 300 + 350000 / m; }
 
 }  // namespace
 
@@ -207,7 +211,7 @@ bool linear8_fits(int64_t n, int64_t m, int64_t k) {
 gnn_status_t linear8_forward_launch(int act, int n, int m, int k, const Rows8 &X, const Rows8 &W, const float *b, const float *R, float *Y,
                                     hipStream_t st) {
     if (n <= 0) return GNN_OK;
-    const bool few = linear8_few(n, k);
+    const bool few = linear8_few(n, m, k);
     const int tile = few ? 32 : 128;
     const Product8 g{n, k, m, (long)rows8_stride(m), X, W, b, R, Y, (int)ceil_div(n, tile), (int)ceil_div(k, tile)};
     const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n;

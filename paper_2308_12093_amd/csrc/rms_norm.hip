@@ -155,7 +155,7 @@ rms_backward_kernel(RmsBack a) {
         dg[r] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     for (long base = (long)blockIdx.x * groups * U; base < a.n; base += (long)gridDim.x * groups * U) {
-        float4 x[U][R], d[U][R];
+        float4 x[U][R], d[U][R], h[U][R];
         long row[U];
         float rstd[U], s[U];
 #pragma unroll
@@ -166,6 +166,7 @@ rms_backward_kernel(RmsBack a) {
                 const int c = 4 * (r * lanes + gl);
                 x[u][r] = rms_row<MEM, HELD>(a, row[u], c, row[u] < a.n);
                 d[u][r] = read4<MEM>(a.dY + row[u] * f, c, f, row[u] < a.n);
+                h[u][r] = a.dH && write ? read4<MEM>(a.dH + row[u] * f, c, f, row[u] < a.n) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
         }
 #pragma unroll
@@ -191,13 +192,9 @@ rms_backward_kernel(RmsBack a) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int g = r * lanes + gl;
-                const float4 v = x[u][r], e = d[u][r];
-                float4 o = make_float4(rstd[u] * fmaf(-v.x, m, e.x), rstd[u] * fmaf(-v.y, m, e.y), rstd[u] * fmaf(-v.z, m, e.z),
-                                       rstd[u] * fmaf(-v.w, m, e.w));
-                if (a.dH) {
-                    const float4 h = read4<MEM>(a.dH + row[u] * f, 4 * g, f, true);
-                    o = make_float4(o.x + h.x, o.y + h.y, o.z + h.z, o.w + h.w);
-                }
+                const float4 v = x[u][r], e = d[u][r], b = h[u][r];
+                const float4 o = make_float4(fmaf(rstd[u], fmaf(-v.x, m, e.x), b.x), fmaf(rstd[u], fmaf(-v.y, m, e.y), b.y),
+                                             fmaf(rstd[u], fmaf(-v.z, m, e.z), b.z), fmaf(rstd[u], fmaf(-v.w, m, e.w), b.w));
                 if (a.dR) write4<MEM>(a.dR + row[u] * f, 4 * g, f, o);
                 if (a.dX) write4<MEM>(a.dX + row[u] * f, 4 * g, f, words.apply(o, (uint32_t)row[u], g));
             }
@@ -414,7 +411,7 @@ static gnn_status_t backward(RmsBack a, int64_t blocks, hipStream_t st) {
                          aligned16(a.dH);
     const int mem = norm_memory(a.n, a.f, aligned);
     const dim3 grid((unsigned)blocks);
-    RMS_CASE(rms_backward_kernel, HELD, 1, 2, 4, false)
+    RMS_CASE(rms_backward_kernel, HELD, 1, 4, 4, false)
     RMS_CASE(rms_backward_kernel, HELD, 2, 1, 2, false)
     RMS_CASE(rms_backward_kernel, HELD, 4, 1, 1, false)
     RMS_CASE(rms_backward_kernel, HELD, 4, 1, 1, true)
