@@ -171,6 +171,147 @@ linear_gradient_kernel(long n, int k, int lanes, int rows, int parts, const floa
         }
 }
 
+// The whole backward pass of a small product in one launch: blocks of 32 x 32 elements of dX, then of dW, whose eight wavefronts share the
+// reduction as above; D = dY .* act'(Z) is formed where it is read, and so is X from its integers.  What such a pass takes is
+// launches: 61 x 11 -> 768 in 8 bits 16.7 us by way of X and D in floats, gnn_gemm's products and a sum of their parts.
+struct SmallBack {
+    int n, m, k, tiles_x, tiles_k, tiles_dx;               // tiles_dx: blocks of dX, in front
+    const float *X;                                        // NULL: from `x8`
+    Rows8 x8;
+    const float *W, *Z;                                    // Z NULL: from `z8`
+    Rows8 z8;
+    const float *dY;
+    float *dW, *db, *dX;                                   // db: or NULL
+};
+
+template <int ACT, bool HELD>
+__global__ void __launch_bounds__(512)
+linear_small_back_kernel(SmallBack g) {
+    constexpr int WAVES = 8, AHEAD = 2, P = 8;
+    __shared__ floatx4 sums[WAVES][4][64];
+    __shared__ float s_db[WAVES][32];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, l = lane % 32, half = lane / 32;
+    const bool weights = (int)blockIdx.x >= g.tiles_dx;    // uniform
+    const int block = weights ? (int)blockIdx.x - g.tiles_dx : (int)blockIdx.x, across = weights ? g.tiles_k : g.tiles_x;
+    const int r0 = block / across * 32, c0 = block % across * 32, K = weights ? g.n : g.k;
+    const int all = (K + 2 * P - 1) / (2 * P), first = all * wave / WAVES, total = all * (wave + 1) / WAVES;
+    const long z_ld = rows8_stride(g.k), x_ld = rows8_stride(g.m);
+    floatx16 acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+    float db = 0.f;
+    auto d_of = [&](float dy, float z) __attribute__((always_inline)) {
+        if constexpr (ACT == GNN_ACT_NONE) return dy;
+        float y, slope;
+        activate<ACT, true>(z, y, slope);
+        return dy * slope;
+    };
+    // P operands of each of two matrices, and what the second (dW) or first (dX) has to be formed from
+    float a[AHEAD][P], b[AHEAD][P], z[AHEAD][P];
+    if (weights) {
+        const int m = min(r0 + l, g.m - 1), j = min(c0 + l, g.k - 1);
+        const float column = ACT != GNN_ACT_NONE && HELD && g.z8.columns ? g.z8.columns[j] : 1.f;
+        auto load = [&](int step, int s) __attribute__((always_inline)) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int row = (2 * step + half) * P + p;
+                const bool in = row < g.n;
+                const size_t i = in ? row : 0;             // what is past the end is read from the first row and not used
+                a[s][p] = g.X ? g.X[i * g.m + m] : (float)g.x8.q[i * x_ld + m] * g.x8.scale[i];
+                b[s][p] = g.dY[i * g.k + j];
+                if constexpr (ACT != GNN_ACT_NONE)
+                    z[s][p] = HELD ? (float)g.z8.q[i * z_ld + j] * g.z8.scale[i] * column : g.Z[i * g.k + j];
+                if (!in) a[s][p] = b[s][p] = z[s][p] = 0.f;
+            }
+        };
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s)
+            if (first + s < total) load(first + s, s);
+        for (int step = first; step < total; step += AHEAD) {
+#pragma unroll
+            for (int s = 0; s < AHEAD; ++s)
+                if (step + s < total) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const float d = d_of(b[s][p], z[s][p]);
+                        db += d;
+                        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[s][p], d, acc, 0, 0, 0);
+                    }
+                    if (step + s + AHEAD < total) load(step + s + AHEAD, s);
+                }
+        }
+    } else {
+        const size_t i = min(r0 + l, g.n - 1), c = min(c0 + l, g.m - 1);
+        const float scale = ACT != GNN_ACT_NONE && HELD ? g.z8.scale[i] : 1.f;
+        const float *dy = g.dY + i * g.k, *zs = HELD || ACT == GNN_ACT_NONE ? nullptr : g.Z + i * g.k, *w = g.W + c * g.k;
+        const int8_t *q = HELD ? g.z8.q + i * z_ld : nullptr;
+        auto load = [&](int step, int s) __attribute__((always_inline)) {
+            const int k0 = (2 * step + half) * P;
+            if (k0 + P <= g.k) {
+#pragma unroll
+                for (int h = 0; h < P; h += 4) {
+                    const float4u u = *reinterpret_cast<const float4u *>(dy + k0 + h), v = *reinterpret_cast<const float4u *>(w + k0 + h);
+                    float4u e = {0.f, 0.f, 0.f, 0.f};
+                    if constexpr (ACT != GNN_ACT_NONE && !HELD) e = *reinterpret_cast<const float4u *>(zs + k0 + h);
+                    if constexpr (ACT != GNN_ACT_NONE && HELD) {
+                        const float4 f = integers(*reinterpret_cast<const unsigned *>(q + k0 + h));
+                        e = float4u{f.x * scale, f.y * scale, f.z * scale, f.w * scale};
+                        if (g.z8.columns) e *= *reinterpret_cast<const float4u *>(g.z8.columns + k0 + h);
+                    }
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) { a[s][h + p] = u[p]; b[s][h + p] = v[p]; z[s][h + p] = e[p]; }
+                }
+            } else {
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const bool in = k0 + p < g.k;
+                    a[s][p] = in ? dy[k0 + p] : 0.f;
+                    b[s][p] = in ? w[k0 + p] : 0.f;
+                    z[s][p] = 0.f;
+                    if constexpr (ACT != GNN_ACT_NONE) {
+                        if (in) z[s][p] = HELD ? (float)q[k0 + p] * scale * (g.z8.columns ? g.z8.columns[k0 + p] : 1.f) : zs[k0 + p];
+                    }
+                }
+            }
+        };
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s)
+            if (first + s < total) load(first + s, s);
+        for (int step = first; step < total; step += AHEAD) {
+#pragma unroll
+            for (int s = 0; s < AHEAD; ++s)
+                if (step + s < total) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+                        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(d_of(a[s][p], z[s][p]), b[s][p], acc, 0, 0, 0);
+                    if (step + s + AHEAD < total) load(step + s + AHEAD, s);
+                }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[wave][i][lane] = floatx4{acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]};
+    db += __shfl_xor(db, 32, 64);
+    if (half == 0) s_db[wave][l] = db;
+    __syncthreads();
+    if (weights && g.db && r0 == 0 && wave == 0 && half == 0 && c0 + l < g.k) {
+        float s = 0.f;
+        for (int w = 0; w < WAVES; ++w) s += s_db[w][l];
+        g.db[c0 + l] = s;
+    }
+    // four wavefronts finish a quarter of the tile each: accumulator register v of lane (half, l) is row 8 (v / 4) + 4 half + v % 4
+    const int col = c0 + l, rows = weights ? g.m : g.n, cols = weights ? g.k : g.m;
+    if (wave >= 4 || col >= cols) return;
+    floatx4 s = sums[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) s += sums[w][wave][lane];
+    float *out = weights ? g.dW : g.dX;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const int row = r0 + 8 * wave + 4 * half + v;
+        if (row < rows) out[(size_t)row * cols + col] = weights && !g.X && g.x8.columns ? s[v] * g.x8.columns[row] : s[v];
+    }
+}
+
 // the other kernels read four indices at a time
 bool too_narrow(int64_t m, int64_t k) { return m < 4 || k < 4; }
 // Tiles of 32 x 32 of Y up to which the kernels for few rows are the faster; their time goes with tiles times f_in, where the others begin at
@@ -237,6 +378,25 @@ gnn_status_t product(int act, int64_t n, int64_t m, int64_t k, const float *X, c
     const bool pair = pair_product_fits(n, k, m, X);
     *parts = pair ? pair_row_parts(k) : linear_row_parts(n, k);
     return (pair ? pair_linear_launch : linear_half_launch)(act, n, k, m, X, row_tops, W, b, g, tops, workspace, st);
+}
+
+// Rows and widths up to which one launch is the faster; its time goes with n times the blocks.  One launch / the others in us, SiLU from
+// floats and from 8 bits: 128 x 64 -> 64 5.8 / 15.0, 5.5 / 17.7; 512 x 64 -> 64 8.3 / 15.3, 12.3 / 19.9; 1024 13.7 / 15.5, 21.9 / 18.0;
+// 2048 25 / 16; 512 x 256 -> 1024 21 / 36, 23 / 40; 1024 29 / 41, 43 / 45; 128 x 1024 -> 1024 17 / 40, 21 / 44; 512 51 / 53, 66 / 58;
+// 1 x 1024 -> 2048 18.7 / 19.2, 21.5 / 21.6.
+bool small_back(bool held, int64_t n, int64_t m, int64_t k) {
+    return n <= (held ? 512 : 1024) && k <= 2048 && n * ceil_div(m, 32) * (ceil_div(n, 32) + ceil_div(k, 32)) <= 800000;
+}
+
+gnn_status_t small_backward(int act, int64_t n, int64_t m, int64_t k, const float *X, const Rows8 &X8, const float *W, const float *Z,
+                            const Rows8 &Z8, const float *dY, float *dW, float *db, float *dX, hipStream_t st) {
+    const int tiles_x = (int)ceil_div(m, 32), tiles_k = (int)ceil_div(k, 32), tiles_dx = dX ? (int)ceil_div(n, 32) * tiles_x : 0;
+    const SmallBack g{(int)n, (int)m, (int)k, tiles_x, tiles_k, tiles_dx, X, X8, W, Z, Z8, dY, dW, db, dX};
+#define SMALL_KERNEL(ACT_, HELD_) linear_small_back_kernel<ACT_, HELD_>
+    auto kernel = act == GNN_ACT_NONE ? linear_small_back_kernel<GNN_ACT_NONE, false>
+                  : Z ? BY_ACT(act, SMALL_KERNEL, false) : BY_ACT(act, SMALL_KERNEL, true);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_dx + tiles_x * tiles_k)), dim3(512), 0, st, g);
+    return launch_status();
 }
 
 // scratch of a backward pass behind D and X
@@ -313,6 +473,12 @@ gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X
     float *d_space = carve.take<float>((size_t)n * k), *x_space = carve.take<float>((size_t)n * m);
     const bool plain = act == GNN_ACT_NONE, kept = Z || Z8.q;
     const float *d = plain ? dY : d_space;
+    const Linear g{nullptr, nullptr, nullptr, dY, d_space};
+    if (small_back(!X, n, m, k)) {
+        if (plain || kept) return small_backward(act, n, m, k, X, X8, W, Z, Z8, dY, dW, db, dX, st);
+        GNN_TRY(few(act, n, m, k, X, W, b, g, st));
+        return small_backward(GNN_ACT_NONE, n, m, k, X, X8, W, nullptr, no_rows8(), d, dW, db, dX, st);
+    }
     const bool is_few = linear_few(true, n, m, k), pair_tn = !is_few && pair_tn_fits(m, k, n, !X);
     const float *row_scale = nullptr;                      // what X8's rows are to be taken times, where its integers are read as they are
     if (!X && pair_tn) {
@@ -321,7 +487,6 @@ gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X
         GNN_TRY(dequantize_rows_launch(n, m, X8, x_space, st));
         X = x_space;
     }
-    const Linear g{nullptr, nullptr, nullptr, dY, d_space};
     const bool one_step = n < kShortReduction;             // X^T D does without largest magnitudes
     int parts = 0;
     if (is_few) {

@@ -125,6 +125,8 @@ struct RmsBack {
     const float *dY, *dH;              // dH: or NULL
     float *dR, *dX;                    // either or both may be NULL
     float *part;                       // [block][f]: sums of dY xhat, or NULL
+    int row_blocks;                    // few rows: the blocks behind these form dgamma, 64 columns each
+    float *dgamma;
 };
 
 // four columns of xhat, not yet times the row's factor: H, or the integers; zeros past the row's end and the last row
@@ -138,12 +140,40 @@ __device__ __forceinline__ float4 rms_row(const RmsBack &a, long row, int c, boo
 template <bool HELD>
 __device__ __forceinline__ float rms_factor(const RmsBack &a, long row) { return HELD ? a.held.scale[row] : a.rstd[row]; }
 
+// 64 columns of dgamma over all rows, 16 groups of lanes every sixteenth row each: they need no more of a row than its factor, so that they
+// go with the rows in one launch (28 x 29 forward and back 14.7 us in three).
+template <bool HELD>
+__device__ __forceinline__ void rms_columns(const RmsBack &a, int block, float4 *across) {
+    const int c = block * 64 + 4 * (threadIdx.x % 16), group = threadIdx.x / 16;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < a.f) {
+#pragma unroll 4
+        for (long row = group; row < a.n; row += 16) {
+            const float4 v = rms_row<kAnyRow, HELD>(a, row, c, true), d = load4(a.dY + row * a.f, c, a.f);
+            const float k = rms_factor<HELD>(a, row);
+            s = make_float4(fmaf(d.x, v.x * k, s.x), fmaf(d.y, v.y * k, s.y), fmaf(d.z, v.z * k, s.z), fmaf(d.w, v.w * k, s.w));
+        }
+    }
+    across[threadIdx.x] = s;
+    __syncthreads();
+    if (group != 0 || c >= a.f) return;
+    for (int k = 1; k < 16; ++k) {
+        const float4 o = across[threadIdx.x + 16 * k];
+        s = make_float4(s.x + o.x, s.y + o.y, s.z + o.z, s.w + o.w);
+    }
+    store4(a.dgamma, c, a.f, s);
+}
+
 // dR = dH + rstd (g - xhat mean(g xhat)) with g = gamma dY, dX = dropout(dR)
 template <int R, int U, bool HELD, int MEM, bool WIDE>
 __global__ void __launch_bounds__(256)
 rms_backward_kernel(RmsBack a) {
     __shared__ float red[4 * U];
     __shared__ float4 across[256];
+    if ((int)blockIdx.x >= a.row_blocks) {                 // uniform
+        rms_columns<HELD>(a, blockIdx.x - a.row_blocks, across);
+        return;
+    }
     const DropoutWords words(a.drop);
     const float inv_f = 1.f / (float)a.f;
     const int f = a.f, lanes = a.lanes, gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
@@ -154,7 +184,7 @@ rms_backward_kernel(RmsBack a) {
         ga[r] = a.gamma ? read4<MEM == kStreamed ? kAlignedRow : MEM>(a.gamma, 4 * (r * lanes + gl), f, true) : make_float4(1.f, 1.f, 1.f, 1.f);
         dg[r] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    for (long base = (long)blockIdx.x * groups * U; base < a.n; base += (long)gridDim.x * groups * U) {
+    for (long base = (long)blockIdx.x * groups * U; base < a.n; base += (long)a.row_blocks * groups * U) {
         float4 x[U][R], d[U][R], h[U][R];
         long row[U];
         float rstd[U], s[U];
@@ -395,6 +425,19 @@ size_t rms_norm_workspace_bytes(int64_t n, int64_t f) {
     return align_up((size_t)(blocks > 1024 ? blocks : 1024) * f * sizeof(float));
 }
 
+// Rows up to which dgamma comes from blocks of its own beside them instead of a launch of its own
+constexpr int kFewRows = 512;
+
+template <bool HELD>
+static gnn_status_t rows_launch(const RmsBack &a, const Shape &shape, int mem, int64_t blocks, hipStream_t st) {
+    const dim3 grid((unsigned)blocks);
+    RMS_CASE(rms_backward_kernel, HELD, 1, 4, 4, false)
+    RMS_CASE(rms_backward_kernel, HELD, 2, 1, 2, false)
+    RMS_CASE(rms_backward_kernel, HELD, 4, 1, 1, false)
+    RMS_CASE(rms_backward_kernel, HELD, 4, 1, 1, true)
+    return launch_status();
+}
+
 template <bool HELD>
 static gnn_status_t backward(RmsBack a, int64_t blocks, hipStream_t st) {
     if (a.f > kNormRow) {
@@ -410,12 +453,20 @@ static gnn_status_t backward(RmsBack a, int64_t blocks, hipStream_t st) {
     const bool aligned = a.f % 4 == 0 && aligned16(a.H) && aligned16(a.dY) && aligned16(a.gamma) && aligned16(a.dX) && aligned16(a.dR) &&
                          aligned16(a.dH);
     const int mem = norm_memory(a.n, a.f, aligned);
-    const dim3 grid((unsigned)blocks);
-    RMS_CASE(rms_backward_kernel, HELD, 1, 4, 4, false)
-    RMS_CASE(rms_backward_kernel, HELD, 2, 1, 2, false)
-    RMS_CASE(rms_backward_kernel, HELD, 4, 1, 1, false)
-    RMS_CASE(rms_backward_kernel, HELD, 4, 1, 1, true)
-    return launch_status();
+    a.row_blocks = (int)blocks;
+    const int64_t columns = a.dgamma ? ceil_div(a.f, 64) : 0;
+    if (columns && !a.dR && !a.dX) {
+        a.row_blocks = 0;
+        return rows_launch<HELD>(a, shape, mem, columns, st);
+    }
+    if (columns && (a.dR == a.dY || a.dX == a.dY)) {       // they read dY: before it is written
+        a.row_blocks = 0;
+        GNN_TRY((rows_launch<HELD>(a, shape, mem, columns, st)));
+        a.dgamma = nullptr;
+        a.row_blocks = (int)blocks;
+        return rows_launch<HELD>(a, shape, mem, blocks, st);
+    }
+    return rows_launch<HELD>(a, shape, mem, blocks + columns, st);
 }
 #undef RMS_CASE
 
@@ -425,9 +476,11 @@ gnn_status_t rms_norm_backward_launch(int n, int f, const float *H, const Rows8 
     if (n <= 0) return dgamma ? fill_zero_launch(f, dgamma, st) : GNN_OK;
     if (!dgamma && !dX && !dR) return GNN_OK;
     const int64_t blocks = norm_blocks(n, f);
-    const RmsBack a{n, f, 0, H, held, rstd, gamma, drop, dY, dH, dR, dX, dgamma ? static_cast<float *>(workspace) : nullptr};
+    const bool beside = n <= kFewRows && f <= kNormRow && dgamma;
+    const RmsBack a{n, f, 0, H, held, rstd, gamma, drop, dY, dH, dR, dX, dgamma && !beside ? static_cast<float *>(workspace) : nullptr, 0,
+                    beside ? dgamma : nullptr};
     GNN_TRY(H ? backward<false>(a, blocks, st) : backward<true>(a, blocks, st));
-    return dgamma ? norm_sums_launch(f, f, blocks, a.part, dgamma, nullptr, st) : GNN_OK;
+    return dgamma && !beside ? norm_sums_launch(f, f, blocks, a.part, dgamma, nullptr, st) : GNN_OK;
 }
 
 }  // namespace gnn
