@@ -1,6 +1,7 @@
 // The product with its epilogue, Y = act(X W + b) + R, forward and backward.  Its large products are those of gemm_half_kernel.h and
 // gemm_half_tn.hip; those of few rows are here and in gemm.hip.
 #include "linear.h"
+#include "rows.h"
 
 namespace gnn {
 namespace {
@@ -78,76 +79,64 @@ linear_few_kernel(int M, int N, int K, const float *__restrict__ X, const float 
 }
 
 // D = dY .* act'(Z) from the Z that forward has kept, as it is or in 8 bits, and the largest magnitudes of its rows and of its columns,
-// those with each row times row_scale.  A block takes `rows` rows (top_rows where columns' are wanted) and 64 VEC columns, `lanes` lanes a
-// row; the `parts` blocks of the same rows stand side by side.  D NULL: not wanted (it is dY).
-template <int VEC, int ACT, bool HELD>
+// those with each row times row_scale.  A block takes `rows` rows (top_rows where columns' are wanted) and 256 columns, `lanes` lanes a
+// row, four columns each; the `parts` blocks of the same rows stand side by side.  D NULL: not wanted (it is dY).  Bound by memory: 65536 x
+// 2048 with SiLU 1.6 GB in 304 us, 5.3 TB/s; Z and dY are read once and not into the place of D, which the products read next (335 us).
+template <bool ALIGNED, int ACT, bool HELD>
 __global__ void __launch_bounds__(256)
 linear_gradient_kernel(long n, int k, int lanes, int rows, int parts, const float *__restrict__ Z, Rows8 held, const float *__restrict__ dY,
                        const float *__restrict__ row_scale, float *__restrict__ D, Tops tops) {
-    __shared__ unsigned across[256][VEC];
+    __shared__ unsigned across[256][4];
     const int gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
-    const int part = blockIdx.x % parts, block = blockIdx.x / parts, c = (part * 64 + gl) * VEC;
+    const int part = blockIdx.x % parts, block = blockIdx.x / parts, c = (part * 64 + gl) * 4;
     const long r0 = (long)block * rows, r1 = min(n, r0 + rows), ld = rows8_stride(k);
-    unsigned top[VEC];
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) top[v] = 0;
+    auto read = [&](const float *row) __attribute__((always_inline)) {
+        if constexpr (!ALIGNED) return rows::load4(row, c, k);
+        const floatx4 v = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(row + c));
+        return make_float4(v.x, v.y, v.z, v.w);
+    };
+    unsigned top[4] = {0, 0, 0, 0};
     constexpr int U = 4;                                   // rows under way
     for (long first = r0; first < r1; first += U * groups) {
-        float z[U][VEC], d[U][VEC], factor[U];
+        float4 z[U], d[U];
+        float factor[U];
         unsigned most[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const long row = first + i * groups + grp, at = row * k + c;
+            const long row = first + i * groups + grp;
             factor[i] = 1.f;
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) z[i][v] = d[i][v] = 0.f;
+            z[i] = d[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (row >= r1 || c >= k) continue;
             if (row_scale) factor[i] = row_scale[row];
-            if constexpr (VEC == 4) {
-                // each read once: not in the place of D, which the products read next
-                const floatx4 y = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(dY + at));
-                d[i][0] = y.x; d[i][1] = y.y; d[i][2] = y.z; d[i][3] = y.w;
-                if constexpr (ACT != GNN_ACT_NONE) {
-                    float4 x;
-                    if constexpr (HELD) {
-                        const float s = held.scale[row];
-                        x = integers(*reinterpret_cast<const unsigned *>(held.q + row * ld + c));
-                        x = make_float4(x.x * s, x.y * s, x.z * s, x.w * s);
-                        if (held.columns) {
-                            const float4u e = *reinterpret_cast<const float4u *>(held.columns + c);
-                            x = make_float4(x.x * e.x, x.y * e.y, x.z * e.z, x.w * e.w);
-                        }
-                    } else {
-                        const floatx4 v = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(Z + at));
-                        x = make_float4(v.x, v.y, v.z, v.w);
-                    }
-                    z[i][0] = x.x; z[i][1] = x.y; z[i][2] = x.z; z[i][3] = x.w;
-                }
-            } else {
-                d[i][0] = dY[at];
-                if constexpr (ACT != GNN_ACT_NONE) {
-                    if constexpr (HELD) z[i][0] = (float)held.q[row * ld + c] * held.scale[row] * (held.columns ? held.columns[c] : 1.f);
-                    else z[i][0] = Z[at];
-                }
+            d[i] = read(dY + row * k);
+            if constexpr (ACT != GNN_ACT_NONE && !HELD) z[i] = read(Z + row * k);
+            if constexpr (ACT != GNN_ACT_NONE && HELD) {   // what lies behind a row's end is any integer, but dY is zero there
+                const float s = held.scale[row];
+                const float4 x = integers(*reinterpret_cast<const unsigned *>(held.q + row * ld + c));
+                const float4 e = held.columns ? rows::load4(held.columns, c, k) : make_float4(1.f, 1.f, 1.f, 1.f);
+                z[i] = make_float4(x.x * s * e.x, x.y * s * e.y, x.z * s * e.z, x.w * s * e.w);
             }
         }
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const long row = first + i * groups + grp, at = row * k + c;
-            most[i] = 0;
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                if constexpr (ACT != GNN_ACT_NONE) {
-                    float y, slope;
-                    activate<ACT, true>(z[i][v], y, slope);
-                    d[i][v] *= slope;
-                }
-                most[i] = max(most[i], magnitude(d[i][v]));
-                top[v] = max(top[v], magnitude(d[i][v] * factor[i]));
+            const long row = first + i * groups + grp;
+            float4 &v = d[i];
+            if constexpr (ACT != GNN_ACT_NONE) {
+                float y, s[4];
+                activate<ACT, true>(z[i].x, y, s[0]);
+                activate<ACT, true>(z[i].y, y, s[1]);
+                activate<ACT, true>(z[i].z, y, s[2]);
+                activate<ACT, true>(z[i].w, y, s[3]);
+                v = make_float4(v.x * s[0], v.y * s[1], v.z * s[2], v.w * s[3]);
             }
+            most[i] = largest(v);
+            top[0] = max(top[0], magnitude(v.x * factor[i]));
+            top[1] = max(top[1], magnitude(v.y * factor[i]));
+            top[2] = max(top[2], magnitude(v.z * factor[i]));
+            top[3] = max(top[3], magnitude(v.w * factor[i]));
             if (!D || row >= r1 || c >= k) continue;
-            if constexpr (VEC == 4) *reinterpret_cast<float4 *>(D + at) = make_float4(d[i][0], d[i][1], d[i][2], d[i][3]);
-            else D[at] = d[i][0];
+            if constexpr (ALIGNED) *reinterpret_cast<float4 *>(D + row * k + c) = v;
+            else rows::store4(D + row * k, c, k, v);
         }
         if (!tops.rows) continue;
         for (int q = lanes >> 1; q > 0; q >>= 1)
@@ -161,13 +150,13 @@ linear_gradient_kernel(long n, int k, int lanes, int rows, int parts, const floa
     }
     if (!tops.cols) return;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) across[threadIdx.x][v] = top[v];
+    for (int v = 0; v < 4; ++v) across[threadIdx.x][v] = top[v];
     __syncthreads();
-    if (grp == 0 && c < k)
+    if (grp == 0)
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
+        for (int v = 0; v < 4; ++v) {
             for (int q = 1; q < groups; ++q) top[v] = max(top[v], across[q * lanes + gl][v]);
-            tops.cols[(size_t)block * k + c + v] = top[v];
+            if (c + v < k) tops.cols[(size_t)block * k + c + v] = top[v];
         }
 }
 
@@ -342,7 +331,7 @@ int64_t few_rows(int64_t n, int64_t m, int64_t k) {
      : (ACT_) == GNN_ACT_SIGMOID ? KERNEL_(GNN_ACT_SIGMOID, __VA_ARGS__)       \
      : (ACT_) == GNN_ACT_SILU    ? KERNEL_(GNN_ACT_SILU, __VA_ARGS__) : KERNEL_(GNN_ACT_GELU, __VA_ARGS__))
 #define FEW_KERNEL(ACT_, BACK_) linear_few_kernel<BACK_, ACT_>
-#define GRADIENT_KERNEL(ACT_, VEC_, HELD_) linear_gradient_kernel<VEC_, ACT_, HELD_>
+#define GRADIENT_KERNEL(ACT_, ALIGNED_, HELD_) linear_gradient_kernel<ALIGNED_, ACT_, HELD_>
 
 gnn_status_t few(int act, int64_t n, int64_t m, int64_t k, const float *X, const float *W, const float *b, const Linear &g, hipStream_t st) {
     const int64_t tiles_n = ceil_div(k, 32), blocks = ceil_div(n, 32) * tiles_n;
@@ -353,14 +342,14 @@ gnn_status_t few(int act, int64_t n, int64_t m, int64_t k, const float *X, const
 
 gnn_status_t gradient(int act, int64_t n, int k, const float *Z, const Rows8 &held, const float *dY, const float *row_scale, float *D,
                       const Tops &tops, int *parts, hipStream_t st) {
-    const bool vec = k % 4 == 0 && aligned16(Z) && aligned16(dY);
+    const bool aligned = k % 4 == 0 && aligned16(Z) && aligned16(dY);
     int lanes = 1;
-    while (lanes < 64 && lanes * (vec ? 4 : 1) < k) lanes <<= 1;
-    *parts = (int)ceil_div(k, vec ? 256 : 64);
+    while (lanes < 64 && lanes * 4 < k) lanes <<= 1;
+    *parts = (int)ceil_div(k, 256);
     const int rows = tops.cols ? top_rows(n) : (int)free_rows(n, lanes, *parts);
-    auto kernel = act == GNN_ACT_NONE ? (vec ? linear_gradient_kernel<4, GNN_ACT_NONE, false> : linear_gradient_kernel<1, GNN_ACT_NONE, false>)
-                  : Z ? (vec ? BY_ACT(act, GRADIENT_KERNEL, 4, false) : BY_ACT(act, GRADIENT_KERNEL, 1, false))
-                      : (vec ? BY_ACT(act, GRADIENT_KERNEL, 4, true) : BY_ACT(act, GRADIENT_KERNEL, 1, true));
+    auto kernel = act == GNN_ACT_NONE ? (aligned ? linear_gradient_kernel<true, GNN_ACT_NONE, false> : linear_gradient_kernel<false, GNN_ACT_NONE, false>)
+                  : Z ? (aligned ? BY_ACT(act, GRADIENT_KERNEL, true, false) : BY_ACT(act, GRADIENT_KERNEL, false, false))
+                      : (aligned ? BY_ACT(act, GRADIENT_KERNEL, true, true) : BY_ACT(act, GRADIENT_KERNEL, false, true));
     hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(n, rows) * *parts)), dim3(256), 0, st, (long)n, k, lanes, rows, *parts, Z, held,
                        dY, row_scale, D, tops);
     return launch_status();

@@ -22,31 +22,31 @@ struct PairTn {
     float *sums;                       // [split][N]: column sums of B, or NULL
 };
 
-// A block of four wavefronts owns 128 columns of A and 256 of B over one chunk, a wavefront 64 x 128 outputs.  Per step of 16 indices
+// A block of four wavefronts owns 128 columns of A and 64 NJ of B over one chunk, a wavefront 64 x 32 NJ outputs.  Per step of 16 indices
 // the block reads 16 rows of its columns (a lane eight rows of one column: rows of 128 bytes side by side), splits them in registers and
 // shares the pairs through LDS in the order of the instruction's lanes, double-buffered, one barrier a step; the floats of a step are
-// loaded two steps ahead.  24 matrix instructions a step to 12 reads and 6 writes of 1 KB and about a hundred vector instructions.
+// loaded two steps ahead.  With NJ = 4 there are 24 matrix instructions a step to 12 reads and 6 writes of 1 KB and about a hundred vector instructions.
 //
 // HELD: an integer of 8 bits is one fp16 number, exactly, so A has one part, and there are 16 matrix instructions a step.  The scale
 // of its row, from LDS, goes to the row of B before that is split.  A thread takes 4 columns of 2 rows, 4 bytes each.  A byte b + 128 behind 0x64 is
 // the fp16 number 1024 + 128 + b.
-template <bool HELD>
+template <bool HELD, int NJ>
 __global__ void __launch_bounds__(256, 2)
 pair_tn_kernel(PairTn g) {
-    constexpr int PA = HELD ? 1 : 2, FRAGS = HELD ? 2 : 3;         // parts of A; 32-column tiles that a wavefront splits
-    constexpr int A_BYTES = 4 * PA * 1024, STAGE = A_BYTES + 8 * kPairBytes;
+    constexpr int PA = HELD ? 1 : 2, BF = NJ / 2, FRAGS = HELD ? BF : 1 + BF;      // parts of A; 32-column tiles that a wavefront splits
+    constexpr int A_BYTES = 4 * PA * 1024, STAGE = A_BYTES + 2 * NJ * kPairBytes, COLS = 64 * NJ;
     __shared__ __align__(16) char even[STAGE];
     __shared__ __align__(16) char odd[STAGE];
-    __shared__ int s_exp[384];
+    __shared__ int s_exp[128 + COLS];
     __shared__ __align__(16) float s_rows[HELD ? kMostRows : 4];   // the scales of the chunk's rows, zeros to the end of the last step
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t / 64), lane = t % 64, l = lane % 32, half = lane / 32;
     // tiles of a chunk side by side: they read the same rows
     const long total = (long)g.tiles_m * g.tiles_n * g.splits, id = xcd_tile(total);
     if (id >= total) return;
     const int split = (int)(id / (g.tiles_m * g.tiles_n)), tile = (int)(id % (g.tiles_m * g.tiles_n));
-    const int bm = tile / g.tiles_n * 128, bn = tile % g.tiles_n * 256;
+    const int bm = tile / g.tiles_n * 128, bn = tile % g.tiles_n * COLS;
     const long k0 = split * g.chunk, k1 = min(g.K, k0 + g.chunk);
-    for (int i = t; i < 384; i += 256) {                   // the chunk's largest magnitudes
+    for (int i = t; i < 128 + COLS; i += 256) {                   // the chunk's largest magnitudes
         const bool a = i < 128;
         if (HELD && a) { s_exp[i] = 0; continue; }
         const long width = a ? g.M : g.N;
@@ -58,22 +58,22 @@ pair_tn_kernel(PairTn g) {
     }
     if constexpr (HELD)
         for (int i = t; i < (int)(k1 - k0 + KP - 1) / KP * KP; i += 256) s_rows[i] = k0 + i < k1 ? g.held.scale[k0 + i] : 0.f;
-    // 32-column tiles that this wavefront splits: FRAGS - 2 of A, then two of B.  Columns past the end re-read the last: their
+    // 32-column tiles that this wavefront splits: FRAGS - BF of A, then BF of B.  Columns past the end re-read the last: their
     // results are not stored.
     unsigned at[FRAGS];                                    // bytes to this lane's first float, from the step's first row
     float scale[FRAGS];
     __syncthreads();
 #pragma unroll
     for (int f = 0; f < FRAGS; ++f) {
-        const bool a = f < FRAGS - 2;
-        const int c = (a ? wave : 4 + 2 * wave + f - (FRAGS - 2)) * 32 + l;
+        const bool a = f < FRAGS - BF;
+        const int c = (a ? wave : 4 + BF * wave + f - (FRAGS - BF)) * 32 + l;
         at[f] = a ? 4 * ((unsigned)(8 * half) * g.M + min(bm + c, g.M - 1)) : 4 * ((unsigned)(8 * half) * g.N + min(bn + c - 128, g.N - 1));
         scale[f] = power_of_two(s_exp[c]);
     }
     const int ld = (int)rows8_stride(g.M);
     unsigned byte = 0;                                     // to this thread's four integers, from the step's first row
     if constexpr (HELD) byte = 2u * (t / 32) * ld + min(bm + 4 * (t % 32), ld - 4);
-    float sum[2] = {0.f, 0.f};
+    float sum[BF] = {};
     const bool sums = g.sums && bm == 0;                   // uniform
     const long whole = k0 + (k1 - k0) / KP * KP;           // end of the steps that are complete
 
@@ -85,7 +85,7 @@ pair_tn_kernel(PairTn g) {
         k = min(k, whole - KP);                            // the last complete step again after it: no branch, no use
 #pragma unroll
         for (int f = 0; f < FRAGS; ++f) {
-            const bool a = f < FRAGS - 2;
+            const bool a = f < FRAGS - BF;
             const float *p = a ? g.A + k * g.M : g.B + k * g.N;
             const long width = a ? g.M : g.N;
             unsigned mine = at[f];
@@ -106,7 +106,7 @@ pair_tn_kernel(PairTn g) {
         const int left = (int)(k1 - k);
 #pragma unroll
         for (int f = 0; f < FRAGS; ++f) {
-            const bool a = f < FRAGS - 2;
+            const bool a = f < FRAGS - BF;
             const float *p = a ? g.A + k * g.M : g.B + k * g.N;
             const long width = a ? g.M : g.N;
 #pragma unroll
@@ -122,13 +122,13 @@ pair_tn_kernel(PairTn g) {
     auto put = [&](long k, const Raw &r, char *to, bool count) __attribute__((always_inline)) {
 #pragma unroll
         for (int f = 0; f < FRAGS; ++f) {
-            const bool a = f < FRAGS - 2;
+            const bool a = f < FRAGS - BF;
             float x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = r.x[f][j];
             if (!a) {
                 const float s = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-                sum[f - (FRAGS - 2)] += count ? s : 0.f;
+                sum[f - (FRAGS - BF)] += count ? s : 0.f;
                 if constexpr (HELD) {
                     const float *s = s_rows + (count ? (int)(k - k0) : 0) + 8 * half;
                     const floatx4 u = *reinterpret_cast<const floatx4 *>(s), v = *reinterpret_cast<const floatx4 *>(s + 4);
@@ -138,7 +138,7 @@ pair_tn_kernel(PairTn g) {
             }
             half8 part[2];
             pairs8(x, scale[f], part);
-            char *own = to + (a ? wave * PA * 1024 : A_BYTES + (2 * wave + f - (FRAGS - 2)) * kPairBytes) + lane * 16;
+            char *own = to + (a ? wave * PA * 1024 : A_BYTES + (BF * wave + f - (FRAGS - BF)) * kPairBytes) + lane * 16;
 #pragma unroll
             for (int p = 0; p < 2; ++p) *reinterpret_cast<half8 *>(own + p * 1024) = part[p];
         }
@@ -155,14 +155,14 @@ pair_tn_kernel(PairTn g) {
             }
         }
     };
-    floatx16 acc[2][4];
+    floatx16 acc[2][NJ];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-    const int wm = wave / 2, wn = wave % 2;                // the wavefront's outputs: rows 64 wm .., columns 128 wn ..
+    const int wm = wave / 2, wn = wave % 2;                // the wavefront's outputs: rows 64 wm .., columns 32 NJ wn ..
     auto multiply = [&](const char *buf) __attribute__((always_inline)) {
         half8 a[2][PA];
 #pragma unroll
@@ -170,10 +170,10 @@ pair_tn_kernel(PairTn g) {
 #pragma unroll
             for (int p = 0; p < PA; ++p) a[i][p] = *reinterpret_cast<const half8 *>(buf + ((2 * wm + i) * PA + p) * 1024 + lane * 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NJ; ++j) {
             half8 b[2];
 #pragma unroll
-            for (int p = 0; p < 2; ++p) b[p] = *reinterpret_cast<const half8 *>(buf + A_BYTES + (4 * wn + j) * kPairBytes + p * 1024 + lane * 16);
+            for (int p = 0; p < 2; ++p) b[p] = *reinterpret_cast<const half8 *>(buf + A_BYTES + (NJ * wn + j) * kPairBytes + p * 1024 + lane * 16);
             if constexpr (!HELD)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][PA - 1], b[0], acc[i][j], 0, 0, 0);
@@ -214,16 +214,16 @@ pair_tn_kernel(PairTn g) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) finite = fmaf(acc[i][j][v], 0.f, finite);
-    const int m0 = bm + 64 * wm, n0 = bn + 128 * wn;
+    const int m0 = bm + 64 * wm, n0 = bn + 32 * NJ * wn;
     float *part = g.part + (size_t)split * g.M * g.N;
     if (__any(finite != 0.f)) {                            // 0 x (inf or NaN) is NaN: one tile after the other on the fp32 instruction
 #pragma unroll 1
         for (int i = 0; i < 2; ++i)
 #pragma unroll 1
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < NJ; ++j) {
                 const int m = min(m0 + 32 * i + l, g.M - 1), n = min(n0 + 32 * j + l, g.N - 1);
                 floatx16 f;
 #pragma unroll
@@ -254,17 +254,17 @@ pair_tn_kernel(PairTn g) {
             for (int v = 0; v < 16; ++v) {
                 const int dm = 32 * i + 8 * (v / 4) + 4 * half + v % 4, ea = HELD ? 0 : s_exp[64 * wm + dm];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int dn = 32 * j + l, eb = s_exp[128 + 128 * wn + dn];
+                for (int j = 0; j < NJ; ++j) {
+                    const int dn = 32 * j + l, eb = s_exp[128 + 32 * NJ * wn + dn];
                     if (m0 + dm < g.M && n0 + dn < g.N) part[(size_t)(m0 + dm) * g.N + n0 + dn] = ldexpf(acc[i][j][v], -(ea + eb));
                 }
             }
     }
     if (sums) {                                            // the two lane halves of a column
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
+        for (int f = 0; f < BF; ++f) {
             const float s = sum[f] + __shfl_xor(sum[f], 32, 64);
-            const int n = bn + (2 * wave + f) * 32 + l;
+            const int n = bn + (BF * wave + f) * 32 + l;
             if (half == 0 && n < g.N) g.sums[(size_t)split * g.N + n] = s;
         }
     }
@@ -309,9 +309,11 @@ pair_reduce_kernel(long count, int N, int splits, const float *__restrict__ part
     }
 }
 
+int tile_n(int64_t N) { return N <= 128 ? 128 : 256; }
+
 // Chunks: enough blocks for the chip, at least eight steps each, at most kMostRows indices.
 int64_t pair_chunks(int64_t M, int64_t N, int64_t K) {
-    const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 256);
+    const int64_t tiles = ceil_div(M, 128) * ceil_div(N, tile_n(N));
     int64_t chunks = ceil_div(512, tiles);
     const int64_t most = ceil_div(K, kChunkStep), least = ceil_div(K, kMostRows);
     if (chunks > most) chunks = most;
@@ -321,13 +323,13 @@ int64_t pair_chunks(int64_t M, int64_t N, int64_t K) {
 
 }  // namespace
 
-// Tiles of 128 x 256 of which not too much is empty, and enough of them times chunks of some length for the chip.  Fewer than four tiles are
-// so many chunks that their sums count: 128 x 256 over 2^17 rows 52 + 22 us, 51 + 12 in tiles of 128 x 128 (gemm_half_tn.hip); but with A
-// in 8 bits that would need it in floats first, and their largest magnitudes.
+// Tiles of which not too much is empty, and enough of them times chunks of some length for the chip.  Fewer than four are so many chunks
+// that their sums count: 128 x 256 over 2^17 rows 52 + 22 us, 51 + 12 in tiles of 128 x 128 (gemm_half_tn.hip); but with A in 8 bits
+// that would need it in floats first, and their largest magnitudes.
 bool pair_tn_fits(int64_t M, int64_t N, int64_t K, bool held) {
-    if (M > INT32_MAX / 4 || N > INT32_MAX / 4 || M <= 64 || N <= 128) return false;
-    if (!held && ceil_div(M, 128) * ceil_div(N, 256) < 4) return false;
-    const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 256), most = (int64_t)1 << 24;
+    if (M > INT32_MAX / 4 || N > INT32_MAX / 4 || M <= 64 || N <= (held ? 64 : 128)) return false;
+    const int64_t tiles = ceil_div(M, 128) * ceil_div(N, tile_n(N)), most = (int64_t)1 << 24;
+    if (!held && tiles < 4) return false;
     return tiles * ceil_div(K, kChunkStep) >= 256 && tiles * pair_chunks(M, N, K) < most - 8 && ceil_div(M * N, 32) + ceil_div(N, 32) < most;
 }
 
@@ -345,13 +347,14 @@ gnn_status_t pair_tn_launch(int64_t M, int64_t N, int64_t K, const float *A, con
     g.chunk = ceil_div(ceil_div(K, chunks), kChunkStep) * kChunkStep;
     g.splits = (int)ceil_div(K, g.chunk);
     g.A = A; g.held = held; g.B = B; g.a_tops = a_tops; g.b_tops = b_tops;
-    g.tiles_m = (int)ceil_div(M, 128); g.tiles_n = (int)ceil_div(N, 256);
+    g.tiles_m = (int)ceil_div(M, 128); g.tiles_n = (int)ceil_div(N, tile_n(N));
     Carver carve(workspace);
     g.part = carve.take<float>((size_t)chunks * M * N);
     float *part2 = carve.take<float>((size_t)chunks * N);
     g.sums = sums ? part2 : nullptr;
     const dim3 grid((unsigned)(8 * ceil_div((int64_t)g.tiles_m * g.tiles_n * g.splits, 8)));
-    hipLaunchKernelGGL(A ? pair_tn_kernel<false> : pair_tn_kernel<true>, grid, dim3(256), 0, st, g);
+    auto kernel = A ? pair_tn_kernel<false, 4> : tile_n(N) == 256 ? pair_tn_kernel<true, 4> : pair_tn_kernel<true, 2>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, g);
     GNN_TRY(launch_status());
     const long count = (long)M * N, count2 = sums ? N : 0;
     const int vec = N % 4 == 0 ? 4 : 1;                    // the chunks lie N and M N floats apart in an aligned workspace
