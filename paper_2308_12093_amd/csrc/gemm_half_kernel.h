@@ -273,48 +273,62 @@ gemm_half_kernel(HalfProduct g) {
             }
         }
     } else if constexpr (OUT == kLinearForward) {
-        // two tiles at a time, the part of R that they need under way at once.  Addresses are a scalar base and the lane's own 32-bit offset;
-        // only blocks at an edge compare rows and columns.
-        auto finish = [&](auto whole) __attribute__((always_inline)) {
-            constexpr bool WHOLE = decltype(whole)::value;
-            const size_t corner = (size_t)row0 * g.N + ct0 * 32;
-            const unsigned mine = 4u * half * (unsigned)g.N + l;
-            auto there = [&](int c, int v) __attribute__((always_inline)) {
-                return WHOLE || (row0 + 8 * (v / 4) + 4 * half + v % 4 < g.M && (ct0 + c) * 32 + l < g.N);
-            };
-            auto at = [&](int c, int v) __attribute__((always_inline)) { return corner + (size_t)(8 * (v / 4) + v % 4) * g.N + 32 * c; };
+        // Two tiles at a time, the part of R that they need under way at once.  Addresses are a scalar base and the lane's own 32-bit
+        // offset.  Where columns end inside, lanes are off for a tile; where rows do, element by element.
+        const size_t corner = (size_t)row0 * g.N + ct0 * 32;
+        const unsigned mine = 4u * half * (unsigned)g.N + l;
+        auto at = [&](int c, int v) __attribute__((always_inline)) { return corner + (size_t)(8 * (v / 4) + v % 4) * g.N + 32 * c; };
+        auto put = [&](int c, int v, float bias, float r) __attribute__((always_inline)) {
+            const float z = value(c, v) + bias;
+            float y, slope;
+            activate<GATE, false>(z, y, slope);
+            if (g.linear.Z) (g.linear.Z + at(c, v))[mine] = z;
+            (g.linear.Y + at(c, v))[mine] = y + r;
+        };
+        auto finish = [&](auto rows_inside, auto columns) __attribute__((always_inline)) {
+            constexpr bool INSIDE = decltype(rows_inside)::value, COLUMNS = decltype(columns)::value;
 #pragma unroll
             for (int c0 = 0; c0 < NT; c0 += 2) {
                 float r[2][16], bias[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) bias[i] = g.bias ? g.bias[min((ct0 + c0 + i) * 32 + l, g.N - 1)] : 0.f;
-                if constexpr (WHOLE) {
+                for (int i = 0; i < 2; ++i) {
+                    bias[i] = g.bias ? g.bias[min((ct0 + c0 + i) * 32 + l, g.N - 1)] : 0.f;
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) r[i][v] = 0.f;
+                    for (int v = 0; v < 16; ++v) r[i][v] = 0.f;
+                }
+                if constexpr (INSIDE && COLUMNS) {
                     if (g.linear.R)
 #pragma unroll
                         for (int v = 0; v < 16; ++v)
 #pragma unroll
                             for (int i = 0; i < 2; ++i) r[i][v] = (g.linear.R + at(c0 + i, v))[mine];
-                }
 #pragma unroll
-                for (int v = 0; v < 16; ++v)
+                    for (int v = 0; v < 16; ++v)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) put(c0 + i, v, bias[i], r[i][v]);
+                } else {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int c = c0 + i;
-                        const float z = value(c, v) + bias[i];
-                        float y, slope;
-                        activate<GATE, false>(z, y, slope);
-                        if (!there(c, v)) continue;
-                        if (g.linear.Z) (g.linear.Z + at(c, v))[mine] = z;
-                        (g.linear.Y + at(c, v))[mine] = y + (WHOLE ? r[i][v] : g.linear.R ? (g.linear.R + at(c, v))[mine] : 0.f);
+                        if ((ct0 + c0 + i) * 32 + l >= g.N) continue;
+                        if constexpr (INSIDE) {
+                            if (g.linear.R)
+#pragma unroll
+                                for (int v = 0; v < 16; ++v) r[i][v] = (g.linear.R + at(c0 + i, v))[mine];
+#pragma unroll
+                            for (int v = 0; v < 16; ++v) put(c0 + i, v, bias[i], r[i][v]);
+                        } else {
+#pragma unroll
+                            for (int v = 0; v < 16; ++v)
+                                if (row0 + 8 * (v / 4) + 4 * half + v % 4 < g.M)
+                                    put(c0 + i, v, bias[i], g.linear.R ? (g.linear.R + at(c0 + i, v))[mine] : 0.f);
+                        }
                     }
+                }
             }
         };
-        if (g.M - row0 >= 32 && g.N - ct0 * 32 >= 32 * NT) finish(std::true_type());
-        else finish(std::false_type());
+        if (g.M - row0 < 32) finish(std::false_type(), std::false_type());
+        else if (g.N - ct0 * 32 < 32 * NT) finish(std::true_type(), std::false_type());
+        else finish(std::true_type(), std::true_type());
     } else {
         const int k = GATED ? g.gated.half : g.N, width = GATED ? 2 * k : k;   // of D
         unsigned col_top[NT], row_top[16];

@@ -18,11 +18,12 @@ gnn_status_t linear_half_launch(int act, int64_t M, int64_t N, int64_t K, const 
 // The same products on parts in one scale (half_pair.h), where pair_product_fits: of many aligned rows.
 bool pair_product_fits(int64_t M, int64_t N, int64_t K, const float *A);
 size_t pair_workspace_bytes(int64_t N, int64_t K);
-// C [M][N] = A [M][K] B^T, B [N][K]; row_tops: of A, `parts` of them
-gnn_status_t pair_plain_launch(int64_t M, int64_t N, int64_t K, const float *A, const unsigned *row_tops, int parts, const float *B, float *C,
+// A and X have rows of K floats, a multiple of 4, of which the KB first are those of B and W and the others zeros.
+// C [M][N] = A [M][K] B^T, B [N][KB]; row_tops: of A, `parts` of them
+gnn_status_t pair_plain_launch(int64_t M, int64_t N, int64_t K, int64_t KB, const float *A, const unsigned *row_tops, int parts, const float *B, float *C,
                                void *workspace, hipStream_t st);
 int pair_row_parts(int64_t N);
-gnn_status_t pair_linear_launch(int act, int64_t M, int64_t N, int64_t K, const float *X, const unsigned *row_tops, const float *W,
+gnn_status_t pair_linear_launch(int act, int64_t M, int64_t N, int64_t K, int64_t KB, const float *X, const unsigned *row_tops, int parts, const float *W,
                                 const float *bias, const Linear &out, const Tops &tops, void *workspace, hipStream_t st);
 
 // C [M][N] = A^T B, A [K][M], or NULL: `held` with its columns; B [K][N]; sums [N] = the column sums of B unless it is NULL; a_tops (not of

@@ -361,12 +361,69 @@ size_t product_bytes(int64_t k, int64_t m) {
     return pair > half ? pair : half;
 }
 
-// act(X W + b) + R, or D and its largest magnitudes, `parts` a row
-gnn_status_t product(int act, int64_t n, int64_t m, int64_t k, const float *X, const unsigned *row_tops, const float *W, const float *b,
-                     const Linear &g, const Tops &tops, int *parts, void *workspace, hipStream_t st) {
-    const bool pair = pair_product_fits(n, k, m, X);
+int64_t four(int64_t width) { return (width + 3) / 4 * 4; }
+// floats of a row of X in 8 bits brought to floats, of X or of D with zeros behind it
+int64_t space_width(int64_t m, int64_t k) { return four(m) > four(k) ? four(m) : four(k); }
+
+// Rows of `m` floats with zeros behind them up to a multiple of four, and their largest magnitudes unless `tops` is NULL: [part of 256
+// columns][row].  `lanes` lanes a row, four columns each.
+__global__ void __launch_bounds__(256)
+pad_rows_kernel(long n, int m, int lanes, int rows, int parts, const float *__restrict__ X, float *__restrict__ out, unsigned *__restrict__ tops) {
+    const int gl = threadIdx.x & (lanes - 1), grp = threadIdx.x / lanes, groups = 256 / lanes;
+    const int part = blockIdx.x % parts, c = (part * 64 + gl) * 4;
+    const long r0 = (long)(blockIdx.x / parts) * rows, r1 = min(n, r0 + rows), ld = (m + 3) / 4 * 4;
+    constexpr int U = 4;                                   // rows under way
+    for (long first = r0; first < r1; first += U * groups) {
+        float4 x[U];
+        unsigned most[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp;
+            x[i] = row < r1 && c < m ? rows::load4(X + row * m, c, m) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp;
+            if (row < r1 && c < m) *reinterpret_cast<float4 *>(out + row * ld + c) = x[i];
+            most[i] = largest(x[i]);
+        }
+        if (!tops) continue;
+        for (int q = lanes >> 1; q > 0; q >>= 1)
+#pragma unroll
+            for (int i = 0; i < U; ++i) most[i] = max(most[i], (unsigned)__shfl_xor((int)most[i], q, 64));
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const long row = first + i * groups + grp;
+            if (gl == 0 && row < r1) tops[(size_t)part * n + row] = most[i];
+        }
+    }
+}
+
+gnn_status_t pad_rows(int64_t n, int m, const float *X, float *out, unsigned *tops, hipStream_t st) {
+    int lanes = 1;
+    while (lanes < 64 && lanes * 4 < m) lanes <<= 1;
+    const int parts = (int)ceil_div(m, 256), rows = (int)free_rows(n, lanes, parts);
+    hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)(ceil_div(n, rows) * parts)), dim3(256), 0, st, (long)n, m, lanes, rows, parts, X, out, tops);
+    return launch_status();
+}
+
+// Whether a product of rows that are no multiple of four floats is one of rows that are, in `space`: 30000 x 301 -> 1000 forward 199 us
+// from the rows as they are (gemm_half_kernel.h, which lanes read themselves).
+bool padded(int64_t M, int64_t N, int64_t K, const float *space) {
+    return K % 4 != 0 && K >= kShortReduction && pair_product_fits(M, N, four(K), space);
+}
+
+// act(X W + b) + R, or D and its largest magnitudes, `parts` a row.  x_rows: room for the largest magnitudes of X's rows, filled where
+// `known`; space: n four(m) floats, used where m is no multiple of four.
+gnn_status_t product(int act, int64_t n, int64_t m, int64_t k, const float *X, unsigned *x_rows, bool known, const float *W, const float *b,
+                     const Linear &g, const Tops &tops, int *parts, float *space, void *workspace, hipStream_t st) {
+    const bool pad = padded(n, k, m, space), pair = pad || pair_product_fits(n, k, m, X);
     *parts = pair ? pair_row_parts(k) : linear_row_parts(n, k);
-    return (pair ? pair_linear_launch : linear_half_launch)(act, n, k, m, X, row_tops, W, b, g, tops, workspace, st);
+    if (pad) GNN_TRY(pad_rows(n, (int)m, X, space, known ? nullptr : x_rows, st));
+    else if (!known && m >= kShortReduction) GNN_TRY(tops_launch(n, (int)m, X, Tops{x_rows, nullptr}, st));
+    const int x_parts = pad && !known ? (int)ceil_div(m, 256) : top_parts(m, X);
+    if (pair) return pair_linear_launch(act, n, k, four(m), m, pad ? space : X, x_rows, x_parts, W, b, g, tops, workspace, st);
+    return linear_half_launch(act, n, k, m, X, x_rows, W, b, g, tops, workspace, st);
 }
 
 // Rows and widths up to which one launch is the faster; its time goes with n times the blocks.  One launch / the others in us, SiLU from
@@ -400,8 +457,8 @@ struct Backward {
         d_rows = carve.take<unsigned>(n * (ceil_div(k, 64) + 1));  // those of `product`, of `gradient` or top_parts
         d_cols = carve.take<unsigned>(most_top_blocks(n) * k);
         rest = carve.take<char>(0);
-        size_t most = product_bytes(k, m);
-        for (size_t b : {pair_workspace_bytes(m, k), pair_tn_workspace_bytes(m, k, n), gemm_half_workspace_bytes(m, k), gemm_half_tn_workspace_bytes(m, k, n), gemm_workspace_bytes(0, 1, n, m, k)})
+        size_t most = product_bytes(k, four(m));
+        for (size_t b : {pair_workspace_bytes(m, four(k)), pair_tn_workspace_bytes(m, k, n), gemm_half_workspace_bytes(m, k), gemm_half_tn_workspace_bytes(m, k, n), gemm_workspace_bytes(0, 1, n, m, k)})
             if (b > most) most = b;
         bytes = carve.off + most;
     }
@@ -422,8 +479,11 @@ bool linear_fits(bool backward, int64_t n, int64_t m, int64_t k) {
 
 // What n rows take, or fewer: a product of few rows needs less.
 size_t linear_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k) {
-    if (!backward) return linear_few(false, n, m, k) ? kAlign : align_up((size_t)n * ceil_div(m, 64) * sizeof(unsigned)) + product_bytes(k, m);
-    const size_t d = align_up((size_t)n * k * sizeof(float)) + align_up((size_t)n * m * sizeof(float));
+    if (!backward)
+        return linear_few(false, n, m, k) ? kAlign
+                                          : align_up((size_t)n * ceil_div(m, 64) * sizeof(unsigned)) +
+                                                align_up(m % 4 ? (size_t)n * four(m) * sizeof(float) : 0) + product_bytes(k, four(m));
+    const size_t d = align_up((size_t)n * k * sizeof(float)) + align_up((size_t)n * space_width(m, k) * sizeof(float));
     size_t most = 0;
     const int64_t small = few_rows(n, m, k);
     if (small > 0 && !wide_weights(m, k)) {
@@ -445,10 +505,10 @@ gnn_status_t linear_forward_launch(int act, int n, int m, int k, const float *X,
     const Linear g{R, Y, Z, nullptr, nullptr};
     if (linear_few(false, n, m, k)) return few(act, n, m, k, X, W, b, g, st);
     Carver carve(workspace);
-    const Tops tops{carve.take<unsigned>((size_t)n * ceil_div(m, 64)), nullptr};
-    if (m >= kShortReduction) GNN_TRY(tops_launch(n, m, X, tops, st));
+    unsigned *x_rows = carve.take<unsigned>((size_t)n * ceil_div(m, 64));
+    float *space = carve.take<float>(m % 4 ? (size_t)n * four(m) : 0);
     int parts;
-    return product(act, n, m, k, X, tops.rows, W, b, g, Tops{nullptr, nullptr}, &parts, carve.take<char>(0), st);
+    return product(act, n, m, k, X, x_rows, false, W, b, g, Tops{nullptr, nullptr}, &parts, space, carve.take<char>(0), st);
 }
 
 gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X, const Rows8 &X8, const float *W, const float *b,
@@ -459,7 +519,7 @@ gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X
         return db ? fill_zero_launch(k, db, st) : GNN_OK;
     }
     Carver carve(workspace);
-    float *d_space = carve.take<float>((size_t)n * k), *x_space = carve.take<float>((size_t)n * m);
+    float *d_space = carve.take<float>((size_t)n * k), *x_space = carve.take<float>((size_t)n * space_width(m, k));
     const bool plain = act == GNN_ACT_NONE, kept = Z || Z8.q;
     const float *d = plain ? dY : d_space;
     const Linear g{nullptr, nullptr, nullptr, dY, d_space};
@@ -508,11 +568,16 @@ gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X
     } else if (plain || kept) {
         GNN_TRY(gradient(act, n, k, Z, Z8, dY, row_scale, plain ? nullptr : d_space, of_d, &parts, st));
     } else {
-        GNN_TRY(product(act, n, m, k, X, w.x_rows, W, b, g, of_d, &parts, w.rest, st));
+        GNN_TRY(product(act, n, m, k, X, w.x_rows, of_x.rows != nullptr, W, b, g, of_d, &parts, x_space, w.rest, st));
     }
-    if (dX && short_columns(k)) GNN_TRY(gemm_launch(0, 1, n, m, k, d, W, dX, nullptr, 0, w.rest, st));
-    else if (dX && pair_product_fits(n, m, k, d)) GNN_TRY(pair_plain_launch(n, m, k, d, w.d_rows, parts, W, dX, w.rest, st));
-    else if (dX) GNN_TRY(gemm_half_launch(n, m, k, d, w.d_rows, parts, W, dX, w.rest, st));
+    if (dX && short_columns(k)) {
+        GNN_TRY(gemm_launch(0, 1, n, m, k, d, W, dX, nullptr, 0, w.rest, st));
+    } else if (dX && X != x_space && padded(n, m, k, x_space)) {
+        GNN_TRY(pad_rows(n, k, d, x_space, nullptr, st));
+        GNN_TRY(pair_plain_launch(n, m, four(k), k, x_space, w.d_rows, parts, W, dX, w.rest, st));
+    } else if (dX && pair_product_fits(n, m, k, d)) {
+        GNN_TRY(pair_plain_launch(n, m, k, k, d, w.d_rows, parts, W, dX, w.rest, st));
+    } else if (dX) GNN_TRY(gemm_half_launch(n, m, k, d, w.d_rows, parts, W, dX, w.rest, st));
     if (pair_tn) return pair_tn_launch(m, k, n, X, X8, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
     return gemm_half_tn_launch(m, k, n, X, w.x_cols, d, w.d_cols, dW, db, w.rest, st);
 }

@@ -111,51 +111,66 @@ linear8_kernel(Product8 g) {
     }
     // accumulator register v of lane (half, l): row 8 (v / 4) + 4 half + v % 4, column l of its 32 x 32 tile.  Addresses are a scalar
     // base and the lane's own 32-bit offset; only blocks at an edge compare rows and columns.
-    auto finish = [&](auto whole) __attribute__((always_inline)) {
-        constexpr bool WHOLE = decltype(whole)::value;
-        const int row0 = m0 + 64 * wm, col0 = n0 + 64 * wn;
-        const size_t corner = (size_t)row0 * g.N + col0;
-        const unsigned mine = 4u * half * (unsigned)g.N + l;
-        auto there = [&](int i, int v, int j) __attribute__((always_inline)) {
-            return WHOLE || (row0 + 32 * i + 8 * (v / 4) + 4 * half + v % 4 < g.M && col0 + 32 * j + l < g.N);
-        };
-        auto at = [&](int i, int v, int j) __attribute__((always_inline)) { return corner + (size_t)(32 * i + 8 * (v / 4) + v % 4) * g.N + 32 * j; };
-        float scale[2], bias[2];
+    const int row0 = m0 + 64 * wm, col0 = n0 + 64 * wn;
+    const size_t corner = (size_t)row0 * g.N + col0;
+    const unsigned mine = 4u * half * (unsigned)g.N + l;
+    auto at = [&](int i, int v, int j) __attribute__((always_inline)) { return corner + (size_t)(32 * i + 8 * (v / 4) + v % 4) * g.N + 32 * j; };
+    float scale[2], bias[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int n = min(col0 + 32 * j + l, g.N - 1);
-            scale[j] = g.W.scale[n];
-            bias[j] = g.bias ? g.bias[n] : 0.f;
-        }
+    for (int j = 0; j < 2; ++j) {
+        const int n = min(col0 + 32 * j + l, g.N - 1);
+        scale[j] = g.W.scale[n];
+        bias[j] = g.bias ? g.bias[n] : 0.f;
+    }
+    auto put = [&](int i, int v, int j, float r) __attribute__((always_inline)) {
+        const float x = x_scale[64 * wm + 32 * i + 8 * (v / 4) + 4 * half + v % 4];
+        float y, slope;
+        activate<ACT, false>(fmaf((float)acc[i][j][v] * x, scale[j], bias[j]), y, slope);
+        (g.Y + at(i, v, j))[mine] = y + r;
+    };
+    // The part of R that two tiles need is under way at once.  Where columns end inside, lanes are off for a tile; where rows do, element by
+    // element.
+    auto finish = [&](auto rows, auto columns) __attribute__((always_inline)) {
+        constexpr bool ROWS = decltype(rows)::value, COLUMNS = decltype(columns)::value;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            float r[2][16];                                // of R, all under way at once
-            if constexpr (WHOLE) {
+            float r[2][16];
 #pragma unroll
-                for (int v = 0; v < 16; ++v)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) r[j][v] = 0.f;
+                for (int v = 0; v < 16; ++v) r[j][v] = 0.f;
+            if constexpr (ROWS && COLUMNS) {
                 if (g.R)
 #pragma unroll
                     for (int v = 0; v < 16; ++v)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) r[j][v] = (g.R + at(i, v, j))[mine];
-            }
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const float x = x_scale[64 * wm + 32 * i + 8 * (v / 4) + 4 * half + v % 4];
+                for (int v = 0; v < 16; ++v)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) put(i, v, j, r[j][v]);
+            } else {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float y, slope;
-                    activate<ACT, false>(fmaf((float)acc[i][j][v] * x, scale[j], bias[j]), y, slope);
-                    if (!there(i, v, j)) continue;
-                    (g.Y + at(i, v, j))[mine] = y + (WHOLE ? r[j][v] : g.R ? (g.R + at(i, v, j))[mine] : 0.f);
+                    if (col0 + 32 * j + l >= g.N) continue;
+                    if constexpr (ROWS) {
+                        if (g.R)
+#pragma unroll
+                            for (int v = 0; v < 16; ++v) r[j][v] = (g.R + at(i, v, j))[mine];
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) put(i, v, j, r[j][v]);
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            if (row0 + 32 * i + 8 * (v / 4) + 4 * half + v % 4 < g.M) put(i, v, j, g.R ? (g.R + at(i, v, j))[mine] : 0.f);
+                    }
                 }
             }
         }
     };
-    if (m0 + 128 <= g.M && n0 + 128 <= g.N) finish(std::true_type());
-    else finish(std::false_type());
+    if (row0 + 64 > g.M) finish(std::false_type(), std::false_type());
+    else if (col0 + 64 > g.N) finish(std::true_type(), std::false_type());
+    else finish(std::true_type(), std::true_type());
 }
 
 // Four wavefronts per 32 rows and 32 columns of Y share the reduction: a lane takes 16 consecutive bytes of its row of X and of its row

@@ -83,7 +83,8 @@ pair_weights_kernel(int N, int K, int steps, HalfOperand b, char *__restrict__ o
 
 // ---- rows times weights -----------------------------------------------------------------------------------
 struct PairProduct {
-    int M, N, K, steps;
+    int M, N, K, steps;                // K: floats between rows of A, zeros behind the first KB of them
+    int KB;                            // indices that B has
     const float *A;
     const unsigned *row_tops;          // [top_parts][M]
     int top_parts;
@@ -253,7 +254,7 @@ pair_product_kernel(PairProduct g) {
                 for (int v = 0; v < 16; ++v) f[v] = 0.f;
 #pragma unroll 1
                 for (int k = 0; k < g.K; k += 2)           // K is even
-                    f = __builtin_amdgcn_mfma_f32_32x32x2f32(x[k + half], n < g.N ? w[(k + half) * g.B.sk] : 0.f, f, 0, 0, 0);
+                    f = __builtin_amdgcn_mfma_f32_32x32x2f32(x[k + half], n < g.N && k + half < g.KB ? w[(k + half) * g.B.sk] : 0.f, f, 0, 0, 0);
                 unsigned col_top = 0;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
@@ -287,59 +288,77 @@ pair_product_kernel(PairProduct g) {
         auto value = [&](int i, int j, int v) __attribute__((always_inline)) {
             return ldexpf(acc[i][j][v], -(s_exp[64 * wm + 32 * i + 8 * (v / 4) + 4 * half + v % 4] + eb[j]));
         };
-        auto finish = [&](auto whole) __attribute__((always_inline)) {
-            constexpr bool WHOLE = decltype(whole)::value;
-            constexpr int Q = 2;                           // tiles at a time, what they need of R or dY under way at once
+        // one output, `other` its element of R or dY
+        auto put = [&](int i, int j, int v, float other, unsigned &row_top, unsigned &col_top) __attribute__((always_inline)) {
+            const float z = value(i, j, v) + bias[j];
+            float y, slope = 0.f;
+            activate<ACT, OUT == kBackward>(z, y, slope);
+            if constexpr (OUT == kBackward) {
+                const float d = other * slope;
+                (g.linear.D + at(i, j, v))[own] = d;
+                row_top = max(row_top, __float_as_uint(d) & 0x7fffffffu);
+                col_top = max(col_top, __float_as_uint(d) & 0x7fffffffu);
+            } else {
+                if (OUT == kForward && g.linear.Z) (g.linear.Z + at(i, j, v))[own] = z;
+                (g.linear.Y + at(i, j, v))[own] = OUT == kForward ? y + other : y;
+            }
+        };
+        const float *from = OUT == kForward ? g.linear.R : g.linear.dY;
+        // Two tiles at a time, what they need of R or dY under way at once.  Where columns end inside, lanes are off for a tile; where rows
+        // do, element by element.
+        auto finish = [&](auto rows, auto columns) __attribute__((always_inline)) {
+            constexpr bool ROWS = decltype(rows)::value, COLUMNS = decltype(columns)::value;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 unsigned row_top[16];
 #pragma unroll
                 for (int v = 0; v < 16; ++v) row_top[v] = 0;
 #pragma unroll
-                for (int j0 = 0; j0 < NJ; j0 += Q) {
-                    float r[Q][16];
-                    const float *from = OUT == kForward ? g.linear.R : g.linear.dY;
-                    unsigned col_top[Q] = {};
-                    if constexpr (WHOLE && OUT != kPlain) {
+                for (int j0 = 0; j0 < NJ; j0 += 2) {
+                    unsigned col_top[2] = {0, 0};
+                    float r[2][16];
 #pragma unroll
-                        for (int v = 0; v < 16; ++v)
+                    for (int q = 0; q < 2; ++q)
 #pragma unroll
-                            for (int q = 0; q < Q; ++q) r[q][v] = 0.f;
-                        if (from)
+                        for (int v = 0; v < 16; ++v) r[q][v] = 0.f;
+                    if constexpr (ROWS && COLUMNS) {
+                        if (OUT != kPlain && from)
 #pragma unroll
                             for (int v = 0; v < 16; ++v)
 #pragma unroll
-                                for (int q = 0; q < Q; ++q) r[q][v] = (from + at(i, j0 + q, v))[own];
-                    }
+                                for (int q = 0; q < 2; ++q) r[q][v] = (from + at(i, j0 + q, v))[own];
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
+                        for (int v = 0; v < 16; ++v)
 #pragma unroll
-                        for (int q = 0; q < Q; ++q) {
-                            const int j = j0 + q;
-                            const float z = value(i, j, v) + bias[j];
-                            float y, slope = 0.f;
-                            activate<ACT, OUT == kBackward>(z, y, slope);
-                            if (!WHOLE && !there(i, j, v)) continue;
-                            const float other = OUT == kPlain ? 0.f : WHOLE ? r[q][v] : from ? (from + at(i, j, v))[own] : 0.f;
-                            if constexpr (OUT == kBackward) {
-                                const float d = other * slope;
-                                (g.linear.D + at(i, j, v))[own] = d;
-                                row_top[v] = max(row_top[v], __float_as_uint(d) & 0x7fffffffu);
-                                col_top[q] = max(col_top[q], __float_as_uint(d) & 0x7fffffffu);
+                            for (int q = 0; q < 2; ++q) put(i, j0 + q, v, r[q][v], row_top[v], col_top[q]);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            if (col0 + 32 * (j0 + q) + l >= g.N) continue;
+                            if constexpr (ROWS) {
+                                if (OUT != kPlain && from)
+#pragma unroll
+                                    for (int v = 0; v < 16; ++v) r[q][v] = (from + at(i, j0 + q, v))[own];
+#pragma unroll
+                                for (int v = 0; v < 16; ++v) put(i, j0 + q, v, r[q][v], row_top[v], col_top[q]);
                             } else {
-                                if (OUT == kForward && g.linear.Z) (g.linear.Z + at(i, j, v))[own] = z;
-                                (g.linear.Y + at(i, j, v))[own] = OUT == kForward ? y + other : y;
+#pragma unroll
+                                for (int v = 0; v < 16; ++v)
+                                    if (there(i, j0 + q, v))
+                                        put(i, j0 + q, v, OUT != kPlain && from ? (from + at(i, j0 + q, v))[own] : 0.f, row_top[v], col_top[q]);
                             }
                         }
+                    }
                     if constexpr (OUT == kBackward)
 #pragma unroll
-                        for (int q = 0; q < Q; ++q) put_cols(col_top[q], i, j0 + q);
+                        for (int q = 0; q < 2; ++q) put_cols(col_top[q], i, j0 + q);
                 }
                 if constexpr (OUT == kBackward) put_rows(row_top, i);
             }
         };
-        if (row0 + 64 <= g.M && col0 + 32 * NJ <= g.N) finish(std::true_type());
-        else finish(std::false_type());
+        if (row0 + 64 > g.M) finish(std::false_type(), std::false_type());
+        else if (col0 + 32 * NJ > g.N) finish(std::true_type(), std::false_type());
+        else finish(std::true_type(), std::true_type());
     }
     if constexpr (OUT == kBackward) {
         if (top_rows(g.M) == 32) return;
@@ -353,9 +372,9 @@ pair_product_kernel(PairProduct g) {
 int pair_tiles(int64_t N) { return N % 256 == 0 || N % 256 > 128 ? 4 : 2; }
 size_t parts_bytes(int64_t N, int64_t K) { return align_up((size_t)ceil_div(N, 256) * 8 * ceil_div(K, KP) * kPairBytes); }
 
-gnn_status_t set_pair(PairProduct &g, int nj, int64_t M, int64_t N, int64_t K, const float *A, const unsigned *row_tops, int parts, const HalfOperand &B,
+gnn_status_t set_pair(PairProduct &g, int nj, int64_t M, int64_t N, int64_t K, int64_t KB, const float *A, const unsigned *row_tops, int parts, const HalfOperand &B,
                       void *workspace, hipStream_t st) {
-    g.M = (int)M; g.N = (int)N; g.K = (int)K; g.steps = (int)ceil_div(K, KP);
+    g.M = (int)M; g.N = (int)N; g.K = (int)K; g.KB = (int)KB; g.steps = (int)ceil_div(K, KP);
     g.A = A; g.row_tops = row_tops; g.top_parts = parts;
     g.B = B;
     char *at = static_cast<char *>(workspace);
@@ -363,7 +382,7 @@ gnn_status_t set_pair(PairProduct &g, int nj, int64_t M, int64_t N, int64_t K, c
     g.parts = at; g.exps = exps;
     g.tiles_m = (int)ceil_div(M, 128); g.tiles_n = (int)ceil_div(N, 64 * nj);
     const dim3 grid((unsigned)(g.tiles_n * 2 * nj), (unsigned)ceil_div(g.steps, kPartSteps));
-    hipLaunchKernelGGL(B.sk == 1 ? pair_weights_kernel<true> : pair_weights_kernel<false>, grid, dim3(1024), 0, st, g.N, g.K, g.steps, B, at, exps);
+    hipLaunchKernelGGL(B.sk == 1 ? pair_weights_kernel<true> : pair_weights_kernel<false>, grid, dim3(1024), 0, st, g.N, g.KB, g.steps, B, at, exps);
     return launch_status();
 }
 
@@ -382,21 +401,21 @@ size_t pair_workspace_bytes(int64_t N, int64_t K) { return parts_bytes(N, K) + a
 
 int pair_row_parts(int64_t N) { return 2 * (int)ceil_div(N, 128); }
 
-gnn_status_t pair_plain_launch(int64_t M, int64_t N, int64_t K, const float *A, const unsigned *row_tops, int parts, const float *B, float *C,
+gnn_status_t pair_plain_launch(int64_t M, int64_t N, int64_t K, int64_t KB, const float *A, const unsigned *row_tops, int parts, const float *B, float *C,
                                void *workspace, hipStream_t st) {
     PairProduct g{};
-    GNN_TRY(set_pair(g, pair_tiles(N), M, N, K, A, row_tops, parts, HalfOperand{B, 1, (long)K}, workspace, st));
+    GNN_TRY(set_pair(g, pair_tiles(N), M, N, K, KB, A, row_tops, parts, HalfOperand{B, 1, (long)KB}, workspace, st));
     g.linear.Y = C;
     auto kernel = pair_tiles(N) == 4 ? pair_product_kernel<4, kPlain, GNN_ACT_NONE> : pair_product_kernel<2, kPlain, GNN_ACT_NONE>;
     hipLaunchKernelGGL(kernel, pair_grid(g), dim3(256), 0, st, g);
     return launch_status();
 }
 
-gnn_status_t pair_linear_launch(int act, int64_t M, int64_t N, int64_t K, const float *X, const unsigned *row_tops, const float *W,
+gnn_status_t pair_linear_launch(int act, int64_t M, int64_t N, int64_t K, int64_t KB, const float *X, const unsigned *row_tops, int parts, const float *W,
                                 const float *bias, const Linear &out, const Tops &tops, void *workspace, hipStream_t st) {
     PairProduct g{};
     const bool back = out.D != nullptr, four = !back && pair_tiles(N) == 4;
-    GNN_TRY(set_pair(g, four ? 4 : 2, M, N, K, X, row_tops, top_parts(K, X), HalfOperand{W, (long)N, 1}, workspace, st));
+    GNN_TRY(set_pair(g, four ? 4 : 2, M, N, K, KB, X, row_tops, parts, HalfOperand{W, (long)N, 1}, workspace, st));
     g.bias = bias;
     g.linear = out;
     g.tops = tops;

@@ -122,7 +122,7 @@ SHAPES = [(1, 1, 1), (1, 256, 512), (2, 3, 5), (5, 16, 16), (7, 64, 33), (31, 10
           (300000, 4, 20), (260000, 5, 30), (60000, 64, 513), (4097, 1000, 300),
           # pairs in one scale: tiles of 128 x 128 and 128 x 256, ragged rows, columns and reductions, chunks that end inside a step
           (33001, 132, 256), (17003, 260, 390), (17000, 68, 516), (8200, 100, 1028), (32769, 36, 640), (45000, 200, 200), (16400, 516, 260),
-          (33001, 131, 257), (9001, 400, 900)]
+          (33001, 131, 257), (9001, 400, 900), (40001, 33, 258), (40003, 30, 130), (36000, 259, 133), (70001, 65, 96), (33001, 1030, 67)]
 
 
 @pytest.mark.parametrize("i", range(len(SHAPES)))
@@ -137,7 +137,7 @@ def test_activations(n, m, k, act):
 
 
 UNALIGNED = [(1, 40, 30), (33, 33, 65), (300, 203, 259), (3001, 130, 70), (20011, 40, 129), (40000, 128, 256), (66001, 24, 36),
-             (9000, 300, 515), (3000, 41, 1201), (40000, 7, 65), (60000, 16, 260)]
+             (9000, 300, 515), (3000, 41, 1201), (40000, 7, 65), (60000, 16, 260), (33001, 131, 257), (33001, 132, 256), (45000, 35, 210)]
 
 
 @pytest.mark.parametrize("i", range(len(UNALIGNED)))
@@ -174,7 +174,7 @@ def test_outputs_that_are_not_wanted_and_outputs_over_the_residual(n, m, k):
 
 
 @pytest.mark.parametrize("n,m,k", [(3, 24, 20), (500, 64, 96), (20000, 64, 320), (3000, 40, 2400), (60000, 64, 200), (3000, 41, 2401), (70000, 16, 320),
-                                   (33001, 132, 256), (16400, 260, 516)])
+                                   (33001, 132, 256), (16400, 260, 516), (33001, 131, 257)])
 def test_what_is_not_finite_stays_where_it_belongs(n, m, k):
     """An infinite or NaN input spoils its row of Y, a NaN gradient its row of dX and the weights that it meets; every other one is exact."""
     c = Case(n, m, k, "silu")
@@ -242,7 +242,7 @@ def twelve_bits(rng, *shape):
 
 @pytest.mark.parametrize("n,m,k", [(32, 512, 1030), (33, 512, 600), (200, 512, 1100), (4096, 300, 515), (4097, 300, 515), (9001, 130, 1201),
                                    (40000, 128, 256), (33000, 50, 30), (66001, 52, 68), (3000, 40, 2400), (33001, 132, 256), (17003, 260, 390),
-                                   (16400, 516, 260)])
+                                   (16400, 516, 260), (33001, 131, 257)])
 def test_second_parts_reach_every_sum(n, m, k):
     """Whole numbers of twelve bits times +-1: every sum is exact (below 2^24 where few enough stand in it), bit for bit, from floats and
     from rows in 8 bits (+-127 .. of scale 1), whichever operand has the second parts."""
