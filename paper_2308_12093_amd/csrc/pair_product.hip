@@ -103,11 +103,15 @@ enum { kPlain, kForward, kBackward };
 // block copies its rows (64 bytes each, 16 rows an instruction) and the parts of its columns to LDS, without touching registers, a step ahead;
 // one barrier a step.  A row's four 16-byte pieces lie in the order piece ^ (row / 4 mod 4), so that the reads of sixteen rows fall on
 // different banks.  A lane reads eight consecutive floats of its two rows back and splits them.
-// With NJ = 4 a step is 24 matrix instructions of 32 cycles to 6 + 8 reads of 1 KB, 6 copies and about 70 vector instructions of 4
-// cycles; with NJ = 2 LDS is as long at work as the matrix cores.
+// With NJ = 4 a step is 24 matrix instructions of 32 cycles to 4 + 8 reads of 1 KB, 6 copies and about 70 vector instructions of 4
+// cycles; with NJ = 2 LDS is as long at work as the matrix cores.  65536 x 2048 -> 512 plain: 400 us when the card is cool, 344 TFLOP/s of the
+// product and 1.03 PFLOP/s on the instruction, 465 us after some more of them: the clock falls to 1.8 GHz and below, the instruction is
+// busy for 54 % of the cycles.  (In half_parts.h's two scales: 458 and 496.)  65536 x 512 -> 2048 with SiLU, residual and Z, 1.7 GB besides:
+// 570 to 640 us.  Pairs of the next step between the matrix instructions, with three buffers in LDS: 399 and 461, D of 2^17 x 128 -> 256
+// 105 instead of 98.
 // K is a multiple of 4, below 2^22, and A 16-byte aligned.
 template <int NJ, int OUT, int ACT>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, NJ == 2 && OUT != kBackward ? 3 : 2)
 pair_product_kernel(PairProduct g) {
     __shared__ __align__(16) char a_even[8192];
     __shared__ __align__(16) char a_odd[8192];
@@ -368,8 +372,13 @@ pair_product_kernel(PairProduct g) {
     }
 }
 
-// 32-column tiles of a wavefront; the epilogue of a backward pass has registers for two
-int pair_tiles(int64_t N) { return N % 256 == 0 || N % 256 > 128 ? 4 : 2; }
+// 32-column tiles of a wavefront; the epilogue of a backward pass has registers for two.  Blocks that begin together also end together, and
+// a short reduction leaves much of the time to memory at the end: more and smaller blocks fall out of step (2^17 x 128 -> 256 with ELU 71 ->
+// 61 us, 30000 x 301 -> 1000 with SiLU, residual and Z 164 -> 146).
+int pair_tiles(int64_t M, int64_t N, int64_t K) {
+    const bool many = K > 512 || ceil_div(M, 128) * ceil_div(N, 256) >= 2048;
+    return many && (N % 256 == 0 || N % 256 > 128) ? 4 : 2;
+}
 size_t parts_bytes(int64_t N, int64_t K) { return align_up((size_t)ceil_div(N, 256) * 8 * ceil_div(K, KP) * kPairBytes); }
 
 gnn_status_t set_pair(PairProduct &g, int nj, int64_t M, int64_t N, int64_t K, int64_t KB, const float *A, const unsigned *row_tops, int parts, const HalfOperand &B,
@@ -393,7 +402,7 @@ dim3 pair_grid(const PairProduct &g) { return dim3((unsigned)(8 * ceil_div((int6
 // Blocks enough for the chip, whole lines of aligned rows, and reductions that parts are exact enough for.
 bool pair_product_fits(int64_t M, int64_t N, int64_t K, const float *A) {
     if (K < kShortReduction || K % 4 != 0 || K >= 1 << 22 || !aligned16(A) || N <= 64 || N > 1 << 22 || M > INT32_MAX - 256) return false;
-    const int64_t blocks = ceil_div(M, 128) * ceil_div(N, 64 * pair_tiles(N));
+    const int64_t blocks = ceil_div(M, 128) * ceil_div(N, 64 * pair_tiles(M, N, K));
     return blocks >= 256 && blocks < ((int64_t)1 << 24) - 8;
 }
 
@@ -404,9 +413,9 @@ int pair_row_parts(int64_t N) { return 2 * (int)ceil_div(N, 128); }
 gnn_status_t pair_plain_launch(int64_t M, int64_t N, int64_t K, int64_t KB, const float *A, const unsigned *row_tops, int parts, const float *B, float *C,
                                void *workspace, hipStream_t st) {
     PairProduct g{};
-    GNN_TRY(set_pair(g, pair_tiles(N), M, N, K, KB, A, row_tops, parts, HalfOperand{B, 1, (long)KB}, workspace, st));
+    GNN_TRY(set_pair(g, pair_tiles(M, N, K), M, N, K, KB, A, row_tops, parts, HalfOperand{B, 1, (long)KB}, workspace, st));
     g.linear.Y = C;
-    auto kernel = pair_tiles(N) == 4 ? pair_product_kernel<4, kPlain, GNN_ACT_NONE> : pair_product_kernel<2, kPlain, GNN_ACT_NONE>;
+    auto kernel = pair_tiles(M, N, K) == 4 ? pair_product_kernel<4, kPlain, GNN_ACT_NONE> : pair_product_kernel<2, kPlain, GNN_ACT_NONE>;
     hipLaunchKernelGGL(kernel, pair_grid(g), dim3(256), 0, st, g);
     return launch_status();
 }
@@ -414,7 +423,7 @@ gnn_status_t pair_plain_launch(int64_t M, int64_t N, int64_t K, int64_t KB, cons
 gnn_status_t pair_linear_launch(int act, int64_t M, int64_t N, int64_t K, int64_t KB, const float *X, const unsigned *row_tops, int parts, const float *W,
                                 const float *bias, const Linear &out, const Tops &tops, void *workspace, hipStream_t st) {
     PairProduct g{};
-    const bool back = out.D != nullptr, four = !back && pair_tiles(N) == 4;
+    const bool back = out.D != nullptr, four = !back && pair_tiles(M, N, K) == 4;
     GNN_TRY(set_pair(g, four ? 4 : 2, M, N, K, KB, X, row_tops, parts, HalfOperand{W, (long)N, 1}, workspace, st));
     g.bias = bias;
     g.linear = out;

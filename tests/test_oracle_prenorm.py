@@ -64,3 +64,35 @@ def test_product_against_autograd_and_differences(kind):
     slope = (value(X + e * vx, W + e * vw) - value(X - e * vx, W - e * vw)) / (2 * e)
     assert np.abs(Z).min() > 1e-4                          # no kink between
     assert slope == pytest.approx(float((dX * vx).sum() + (dW * vw).sum()), rel=1e-6)
+
+
+@pytest.mark.parametrize("kept", [False, True])
+def test_the_composed_block_against_autograd(kept):
+    """tests/prenorm_case.py, gradients by autograd; what is kept in 8 bits is there an input of its own."""
+    from tests import prenorm_case as PC
+    n, f, q = 9, 12, 20
+    t = PC.inputs(n, f, q, 5)
+    r = PC.forward(t, 2)
+    v = {name: torch.tensor(a.astype(np.float64), requires_grad=name != "T") for name, a in t.items()}
+    m = torch.tensor(blocks.dropout_factor(n, f, PC.P_DROP, PC.SEED, 2))
+    h = v["R"] + m * v["X"]
+    rstd = 1 / torch.sqrt((h * h).mean(1, keepdim=True) + PC.EPS)
+    z = (h * rstd * v["gamma"]) @ v["W1"] + v["b1"]
+    a = torch.nn.functional.silu(z)
+    o = a @ v["W2"] + v["b2"] + h
+    np.testing.assert_allclose(r["O"], o.detach().numpy(), rtol=1e-12, atol=1e-12)
+    if not kept:
+        loss = 0.5 * ((o - v["T"]) ** 2).sum()
+        loss.backward()
+        xhat, s = blocks.rms_norm(r["H"], PC.EPS)
+        g = PC.backward(t, 2, xhat, s, r["Z"], r["A"], r["O"] - t["T"])
+        for name, grad in dict(X="dX", R="dR", gamma="dgamma", W1="dW1", b1="db1", W2="dW2", b2="db2").items():
+            np.testing.assert_allclose(g[grad], v[name].grad.numpy(), rtol=1e-9, atol=1e-10, err_msg=name)
+        return
+    # 8 bits in place of xhat: the gradients differ by parts of a hundredth, not by a factor
+    xhat, s = blocks.rms_norm(r["H"], PC.EPS)
+    held = lambda x: (lambda q8, u: q8 * u[:, None])(*blocks.held8(x))  # noqa: E731
+    plain = PC.backward(t, 2, xhat, s, r["Z"], r["A"], r["O"] - t["T"])
+    g = PC.backward(t, 2, held(xhat), s, held(r["Z"]), held(r["A"]), r["O"] - t["T"])
+    for name in plain:
+        assert np.linalg.norm(g[name] - plain[name]) < 0.05 * np.linalg.norm(plain[name]), name
