@@ -487,7 +487,11 @@ gnn_status_t gnn_rng_advance(uint64_t *state, uint64_t by, void *hip_stream);
 gnn_status_t gnn_dropout(int32_t n, int32_t f, const float *X, const float *R, const gnn_dropout_t *drop, float *Y,
                          void *hip_stream);
 
-/* ELU with alpha = 1; the last three are those of gnn_gate_t, for the products below (gnn_linear_..): a layer norm takes the first three. */
+/*
+ * ELU with alpha = 1; the last three are those of gnn_gate_t, for the products below (gnn_linear_..): a layer norm takes the first three.
+ * In these products a sigmoid and the normal distribution's integral are off by what one unit in the last place of their argument is worth
+ * and a few units of their own; arguments beyond some 87 (of GELU some 13) below zero give 0.
+ */
 typedef enum {
     GNN_ACT_NONE = 0, GNN_ACT_RELU = 1, GNN_ACT_ELU = 2, GNN_ACT_SIGMOID = 3, GNN_ACT_SILU = 4, GNN_ACT_GELU = 5
 } gnn_act_t;
@@ -621,7 +625,11 @@ size_t gnn_rms_norm_workspace_bytes(int32_t n, int32_t f);
  *   X, or X8: the rows in 8 bits, columns included; one of them is NULL.
  *   Z as forward left it, or Z8: the same in 8 bits, columns included, or neither: Z is formed again from X, W and b, and X8 will not do.
  *   GNN_ACT_NONE reads neither of them.
- *   Sums and their operands are as in gnn_gated_fwd / _bwd, f_out in place of 2 f_out.  From X8 they are as exact: an integer is one fp16
+ *   Sums are fp32 or better everywhere.  Products of many rows over 32 and more indices (f_in of them forward, f_out in dX, n in dW)
+ *   take a float as two fp16 numbers: one is off by up to 8 u (u = 2^-24; a float product by u), and by an operand's loss of 2^-40 of the
+ *   largest of its row (of X, D) or column (of W; of X and D in dW, in chunks of 4096 rows), which shows where operands lie below
+ *   2^-16 of it.  Root mean square errors are no larger than those of a chain of float multiplications and additions.  Few rows and
+ *   shorter products: those of floats, in chains of 1024 rows at most in dW, or doubles.  From X8 dW is as exact: an integer is one fp16
  *   number, and its row's scale goes to the row of D.
  *   Outputs must not overlap inputs or each other, but for Y and R.
  *   workspace: gnn_linear_workspace_bytes(backward, n, f_in, f_out), backward 0 or 1; what it returns does not fall as n grows.

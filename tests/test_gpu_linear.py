@@ -322,6 +322,46 @@ def test_a_captured_step_replays(n, m, k):
         assert all(torch.equal(o[name], want[name]) for name in o)
 
 
+def test_arrays_of_more_than_two_to_the_32_bytes():
+    """Y, Z, dY and D of 4.5 GB: rows at both ends and around 2^32 bytes, and the weights' gradient, which every row is in, from floats and
+    from 8 bits."""
+    n, m, k = 1_100_003, 64, 1024
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    X, W, b, dY = rand(n, m), rand(m, k) / 8, rand(k) / 4, rand(n, k)
+    Y, Z, dW, dX = torch.empty(n, k, device="cuda"), torch.empty(n, k, device="cuda"), torch.empty(m, k, device="cuda"), torch.empty(n, m, device="cuda")
+    ws = B.alloc(max(B.gnn_linear_workspace_bytes(back, n, m, k) for back in (0, 1)))
+    B.gnn_linear_fwd(ID["silu"], n, m, k, X, W, b, None, Y, Z, ws)
+    at = torch.tensor([0, 1, n // 2, 1_048_575, 1_048_576, 1_048_577, n - 2, n - 1], device="cuda")
+    w = host(W).astype(np.float64)
+    y, z = blocks.linear_forward(host(X[at]), w, host(b), "silu")
+    assert np.abs(host(Y[at]) - y).max() < 1e-5 and np.abs(host(Z[at]) - z).max() < 1e-5
+    X8 = B.alloc_rows8(n, m)
+    B.gnn_quantize_rows(n, m, X, None, X8)
+    held = X8.q.double() * X8.scale.double()[:, None]
+    for x, given in ((X.double(), (X, None)), (held, (None, X8))):
+        dX.fill_(NAN)
+        B.gnn_linear_bwd(ID["silu"], n, m, k, *given, W, b, Z, None, dY, dW, None, dX, ws)
+        _, _, want, _ = blocks.linear_backward(host(x[at]), w, host(Z[at]).astype(np.float64), host(dY[at]), "silu")
+        assert np.abs(host(dX[at]) - want).max() < 1e-4
+        ref = torch.zeros(m, k, dtype=torch.float64, device="cuda")
+        mag = torch.zeros(m, k, dtype=torch.float64, device="cuda")
+        for first in range(0, n, 1 << 17):
+            rows = slice(first, first + (1 << 17))
+            s = torch.sigmoid(Z[rows].double())
+            d = dY[rows].double() * s * (1 + Z[rows].double() * (1 - s))
+            ref += x[rows].t() @ d
+            mag += x[rows].abs().t() @ d.abs()
+        assert bool(((dW.double() - ref).abs() <= (64 + 8 * 256) * U * mag).all())
+    # served in 8 bits
+    W8 = B.alloc_rows8(k, m)
+    B.gnn_quantize_rows(k, m, W.t().contiguous(), None, W8)
+    B.gnn_linear8_fwd(ID["silu"], n, m, k, X8, W8, b, None, Y)
+    w8 = (host(W8.q) * host(W8.scale).astype(np.float64)[:, None]).T
+    y, _ = blocks.linear_forward(host(held[at]), w8, host(b), "silu")
+    assert np.abs(host(Y[at]) - y).max() < 1e-5
+
+
 # ---- both operands in 8 bits ---------------------------------------------------------------------------------
 def check8(n, m, k, act, bias=True, residual=True, seed=0, over=False):
     rng = np.random.default_rng(n + 3 * m + 5 * k + seed)
