@@ -286,6 +286,29 @@ def test_elements_far_below_the_largest_are_held_to_a_part_of_it(n, m, k):
     within(dW, X.T @ dY, C * U * (np.abs(X).T @ np.abs(dY)) + held * np.abs(dY).sum(0), "dW")
 
 
+@pytest.mark.parametrize("n", [20, 31, 32])
+def test_few_rows_of_wide_weights(n):
+    """Weights of so many tiles that rows of one step go with the kernels for many: the reduction over them is that of floats below 32."""
+    m, k = 16384, 6016
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    X, W, dY = rand(n, m), rand(m, k), rand(n, k)
+    X8 = B.alloc_rows8(n, m)
+    B.gnn_quantize_rows(n, m, X, None, X8)
+    dW, db, dX = torch.empty(m, k, device="cuda"), torch.empty(k, device="cuda"), torch.empty(n, m, device="cuda")
+    ws = B.alloc(B.gnn_linear_workspace_bytes(True, n, m, k))
+    held = (X8.q.double() * X8.scale.double()[:, None])[:, :m]
+    for x, given, off in ((X.double(), (X, None), 0.0), (held, (None, X8), 3 * U)):
+        ws.fill_(255)
+        dW.fill_(NAN)
+        B.gnn_linear_bwd(0, n, m, k, *given, W, None, None, None, dY, dW, db, dX, ws)
+        d = dY.double()
+        C = n if n < 32 else 64 + 8 * 2
+        assert bool(((dW.double() - x.t() @ d).abs() <= (C * U + off) * (x.abs().t() @ d.abs())).all())
+        assert bool(((db.double() - d.sum(0)).abs() <= C * U * d.abs().sum(0)).all())
+        assert bool(((dX.double() - d @ W.double().t()).abs() <= (8 * (k // 16) + 8) * U * (d.abs() @ W.abs().double().t())).all())
+
+
 def test_no_rows():
     dW, db = torch.full((5, 6), NAN, device="cuda"), torch.full((6,), NAN, device="cuda")
     B.gnn_linear_bwd(ID["silu"], 0, 5, 6, None, None, None, None, None, None, None, dW, db, None, B.alloc(B.gnn_linear_workspace_bytes(True, 0, 5, 6)))
