@@ -34,6 +34,10 @@ __device__ __forceinline__ intx4 before(intx4 a, int k, int K) {
 // A block of four wavefronts owns 128 rows and 128 columns of Y, a wavefront 64 x 64.  Per step of 64 indices the block copies its rows of
 // X and of W to LDS, 16 rows of 64 bytes an instruction, without touching registers, a step ahead; one barrier a step.  A row's four
 // 16-byte pieces lie in the order piece ^ (row / 4 mod 4), so that the reads of sixteen rows fall on different banks.
+// Four blocks a CU, which fall out of step: while some read and multiply others write.  65536 x 512 -> 2048 with SiLU and residual 1.1 GB
+// in 231 us, 4.8 TB/s, the matrix cores busy for 13 %; of 4096 indices 1.5 POP/s, for LDS is longer at work than they.  What it spent
+// its time on before: R's loads behind branches (801 -> 351 us, with LDS in place of lanes' own loads), then 64-bit addresses, comparisons
+// of rows and columns for each element and an exact sigmoid (2400 vector instructions a wavefront, now 750).
 template <int ACT>
 __global__ void __launch_bounds__(256, ACT == GNN_ACT_GELU ? 3 : 4)
 linear8_kernel(Product8 g) {
@@ -175,6 +179,7 @@ linear8_kernel(Product8 g) {
 
 // Four wavefronts per 32 rows and 32 columns of Y share the reduction: a lane takes 16 consecutive bytes of its row of X and of its row
 // of W straight into registers (the lane halves the first and the second 16 of 32), what lies behind K in them is made zero in X.
+// 1 x 512 -> 1024 3.0 us, 2.5 a launch in a graph of fifty.
 template <int ACT>
 __global__ void __launch_bounds__(256)
 linear8_few_kernel(Product8 g) {
