@@ -196,6 +196,50 @@ def test_what_is_not_finite_stays_where_it_belongs(n, m, k):
     c.dY = clean
 
 
+@pytest.mark.parametrize("n,m,k", [(1, 100, 60), (3, 24, 20), (500, 64, 96), (20000, 64, 320), (3000, 40, 2400), (60000, 64, 200), (3000, 41, 2401),
+                                   (70000, 16, 320), (33001, 132, 256), (16400, 260, 516), (33001, 131, 257), (20000, 3, 40)])
+def test_weights_that_are_not_finite_stay_where_they_belong(n, m, k):
+    """A NaN weight spoils its column of Y and its column of dX, an infinite one makes them infinite with the sign of what it meets."""
+    c = Case(n, m, k, "none", residual=False)
+    clean, c.W = c.W, c.W.copy()
+    c.W[2, 3], c.W[0, 5] = np.nan, np.inf
+    Y, Z = (host(t) for t in forward(c))
+    rest = [j for j in range(k) if j not in (3, 5)]
+    for got in (Y, Z):
+        assert np.isnan(got[:, 3]).all() and np.array_equal(got[:, 5], np.copysign(np.inf, c.X[:, 0]))
+        assert (np.abs(got[:, rest] - c.Y[:, rest]) <= c.Y_most[:, rest]).all()
+    dW, db, dX = (host(t) for t in backward(c, dev(c.X)))
+    c.W = clean
+    check(c, (dev(dW), dev(db)), ("dW", "db"))
+    rest = [j for j in range(m) if j not in (0, 2)]
+    assert np.isnan(dX[:, 2]).all() and np.array_equal(dX[:, 0], np.copysign(np.inf, c.dY[:, 5]))
+    assert (np.abs(dX[:, rest] - c.dX[:, rest]) <= c.dX_most[:, rest]).all()
+
+
+@pytest.mark.parametrize("n,m,k", [(1, 100, 60), (500, 64, 96), (20000, 64, 320), (3000, 41, 2401), (70000, 16, 320), (33001, 132, 256), (33001, 131, 257)])
+def test_zeros_stay_zeros(n, m, k):
+    """Rows, columns and whole arrays of zeros have no largest magnitude: what only they meet is zero to the bit, the rest as ever."""
+    c = Case(n, m, k, "none", bias=False, residual=False)
+    c.X[::3], c.X[:, 1] = 0, 0
+    c.W[:, 2], c.W[4] = 0, 0
+    c.dY[1::3], c.dY[:, 5] = 0, 0
+    c.define()
+    X8, held = rows8(c.X)
+    for x, x8 in ((dev(c.X), None), (None, X8)):
+        Y, Z = forward(c)
+        check(c, (Y, Z), ("Y", "Z"))
+        assert not Y[::3].any() and not Y[:, 2].any()
+        if x8 is not None:
+            c.gradients(held, c.Z, 0.0, 3 * U)
+        got = backward(c, x, x8)
+        check(c, got)
+        assert not got[0][1].any() and not got[0][:, 5].any() and not got[1][5].any() and not got[2][1::3].any() and not got[2][:, 4].any()
+    c.dY[:] = 0
+    assert not any(bool(t.any()) for t in backward(c, dev(c.X))) and not any(bool(t.any()) for t in backward(c, None, X8))
+    c.X[:] = 0
+    assert not forward(c)[0].any()
+
+
 @pytest.mark.parametrize("n,m,k", [(300, 40, 60), (3000, 40, 1200), (60000, 64, 200), (5000, 700, 1000), (33001, 132, 256)])
 def test_a_lost_row_in_8_bits_spoils_every_weight(n, m, k):
     """Its scale is NaN, and it is in every sum over the rows; as with the same row in floats."""
