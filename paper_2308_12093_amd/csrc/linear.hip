@@ -11,7 +11,8 @@ using namespace half_parts;
 // Few rows: four wavefronts per 32 rows and 32 columns of Y share the reduction, operands straight from memory into
 // registers two steps ahead (the two lane halves of v_mfma_f32_32x32x2_f32 take P consecutive indices each), one launch, no scratch.
 // While tiles are few, bound by the launch and two waits for memory (1 x 256 -> 512 4.0 us, 3.4 a launch in a graph of fifty); then by the
-// loads, 32 rows at a time by lanes, and the instruction on the fullest CU (3001 x 203 -> 259 with GELU and residual 13.5 us).
+// loads, 32 rows at a time by lanes, and the instruction on the fullest CU (3001 x 203 -> 259 with GELU and residual 12.4 us, 13.7 with R
+// loaded behind the sums).
 template <bool BACK, int ACT>
 __global__ void __launch_bounds__(256)
 linear_few_kernel(int M, int N, int K, const float *__restrict__ X, const float *__restrict__ W, const float *__restrict__ bias, Linear g,
@@ -48,6 +49,16 @@ linear_few_kernel(int M, int N, int K, const float *__restrict__ X, const float 
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s)
         if (first + s < total) load(first + s, s);
+    // a wavefront finishes a quarter of the tile: accumulator register v of lane (half, l) is row 8 (v / 4) + 4 half + v % 4; what it adds
+    // or multiplies by is under way beside the sums
+    const int row = m0 + 8 * wave + 4 * half, col = min(j, N - 1);
+    const float *beside = BACK ? g.dY : g.R;
+    float with[4] = {0.f, 0.f, 0.f, 0.f};
+    const float b = bias ? bias[col] : 0.f;
+    if (beside) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) with[v] = beside[(size_t)min(row + v, M - 1) * N + col];
+    }
     for (int step = first; step < total; step += AHEAD) {
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s) {
@@ -62,20 +73,18 @@ linear_few_kernel(int M, int N, int K, const float *__restrict__ X, const float 
     for (int i = 0; i < 4; ++i) sums[wave][i][lane] = floatx4{acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]};
     __syncthreads();
     if (j >= N) return;
-    // a wavefront finishes a quarter of the tile: accumulator register v of lane (half, l) is row 8 (v / 4) + 4 half + v % 4
-    const floatx4 z = (sums[0][wave][lane] + sums[1][wave][lane]) + (sums[2][wave][lane] + sums[3][wave][lane]) + (bias ? bias[j] : 0.f);
+    const floatx4 z = (sums[0][wave][lane] + sums[1][wave][lane]) + (sums[2][wave][lane] + sums[3][wave][lane]) + b;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-        const int m = m0 + 8 * wave + 4 * half + v;
-        if (m >= M) continue;
+        if (row + v >= M) continue;
         float y, slope;
         activate<ACT, BACK>(z[v], y, slope);
-        const size_t at = (size_t)m * N + j;
+        const size_t at = (size_t)(row + v) * N + j;
         if constexpr (BACK) {
-            g.D[at] = g.dY[at] * slope;
+            g.D[at] = with[v] * slope;
         } else {
             if (g.Z) g.Z[at] = z[v];
-            g.Y[at] = g.R ? y + g.R[at] : y;
+            g.Y[at] = g.R ? y + with[v] : y;
         }
     }
 }

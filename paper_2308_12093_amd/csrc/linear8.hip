@@ -179,7 +179,8 @@ linear8_kernel(Product8 g) {
 
 // Four wavefronts per 32 rows and 32 columns of Y share the reduction: a lane takes 16 consecutive bytes of its row of X and of its row
 // of W straight into registers (the lane halves the first and the second 16 of 32), what lies behind K in them is made zero in X.
-// 1 x 512 -> 1024 3.0 us, 2.5 a launch in a graph of fifty.
+// 1 x 512 -> 1024 3.0 us, 2.5 a launch in a graph of fifty.  1024 x 512 -> 512 with residual 5.2, 5.9 with R and the scales
+// loaded behind the sums; four steps under way gain nothing and cost 0.3 to 2 us where there are one or two.
 template <int ACT>
 __global__ void __launch_bounds__(256)
 linear8_few_kernel(Product8 g) {
@@ -191,6 +192,16 @@ linear8_few_kernel(Product8 g) {
     intx16 acc;
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[v] = 0;
+    // a wavefront finishes a quarter of the tile; what it needs besides the sums is under way beside them
+    const int row = m0 + 8 * wave + 4 * half, col = min(j, g.N - 1);
+    float x_scale[4], with[4] = {0.f, 0.f, 0.f, 0.f};
+    const float scale = g.W.scale[col], bias = g.bias ? g.bias[col] : 0.f;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x_scale[v] = g.X.scale[min(row + v, g.M - 1)];
+    if (g.R) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) with[v] = g.R[(size_t)min(row + v, g.M - 1) * g.N + col];
+    }
     for (int step = first; step < total; ++step) {
         const int k = step * 32 + 16 * half, at = min(k, (int)g.ld - 16);
         intx4 a = *reinterpret_cast<const intx4 *>(x + at);
@@ -203,15 +214,12 @@ linear8_few_kernel(Product8 g) {
     __syncthreads();
     if (j >= g.N) return;
     const intx4 z = (sums[0][wave][lane] + sums[1][wave][lane]) + (sums[2][wave][lane] + sums[3][wave][lane]);
-    const float scale = g.W.scale[j], bias = g.bias ? g.bias[j] : 0.f;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-        const int m = m0 + 8 * wave + 4 * half + v;
-        if (m >= g.M) continue;
+        if (row + v >= g.M) continue;
         float y, slope;
-        activate<ACT, false>(fmaf((float)z[v] * g.X.scale[m], scale, bias), y, slope);
-        const size_t at = (size_t)m * g.N + j;
-        g.Y[at] = g.R ? y + g.R[at] : y;
+        activate<ACT, false>(fmaf((float)z[v] * x_scale[v], scale, bias), y, slope);
+        g.Y[(size_t)(row + v) * g.N + j] = g.R ? y + with[v] : y;
     }
 }
 
