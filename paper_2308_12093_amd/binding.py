@@ -465,16 +465,33 @@ def gnn_gated_bwd(gate, n, f_in, f_out, X, W, b, Z, dH, dW, db, dX, workspace):
 
 # ---- rows in 8 bits; root-mean-square norm; products with their epilogue ------------------
 class Rows8:
-    """A ``gnn_rows8_t`` and the device tensors it points to: ``q`` int8 [n, gnn_rows8_stride(f)], ``scale`` float32 [n],
-    ``columns`` float32 [f] or None."""
+    """A ``gnn_rows8_t`` and the device tensors it points to: ``q`` int8 [n, gnn_rows8_stride(f)] (or all of it in one dimension),
+    ``scale`` float32 [n], ``columns`` float32 [f] or None, each contiguous.  Kernels read and write whole strides of q, so that tensors
+    of another type or layout are refused, here and by a call that needs more rows or another stride (GNN_ERR_INVALID_ARG)."""
 
     def __init__(self, q, scale, columns=None):
+        given = [(q, torch.int8), (scale, torch.float32)] + ([] if columns is None else [(columns, torch.float32)])
+        if any(t is None or t.dtype != dtype or not t.is_contiguous() for t, dtype in given):
+            raise GnnError(GNN_ERR_INVALID_ARG, "Rows8")
         self.q, self.scale, self.columns = q, scale, columns
         self.c = gnn_rows8_t(_ptr(q), _ptr(scale), _ptr(columns))
+        self._ref = ctypes.byref(self.c)
+        self._serves = None            # the last (n, f) that was looked at
+
+    def _look(self, n, f):
+        stride = gnn_rows8_stride(f)
+        short = self.q.numel() < n * stride or self.scale.numel() < n or (self.columns is not None and self.columns.numel() < f)
+        if short or (self.q.dim() > 1 and self.q.shape[-1] != stride):
+            raise GnnError(GNN_ERR_INVALID_ARG, f"Rows8 as [{n}, {f}]")
+        self._serves = n, f
 
 
-def _rows8(rows):
-    return None if rows is None else ctypes.byref(rows.c)
+def _rows8(rows, n, f):
+    if rows is None:
+        return None
+    if rows._serves != (n, f):
+        rows._look(n, f)
+    return rows._ref
 
 
 def gnn_rows8_stride(f) -> int:
@@ -488,11 +505,11 @@ def alloc_rows8(n, f, device="cuda"):
 
 
 def gnn_quantize_rows(n, f, X, columns, out):
-    _check(lib.gnn_quantize_rows(n, f, _ptr(X), _ptr(columns), _rows8(out), _stream()), "gnn_quantize_rows")
+    _check(lib.gnn_quantize_rows(n, f, _ptr(X), _ptr(columns), _rows8(out, n, f), _stream()), "gnn_quantize_rows")
 
 
 def gnn_dequantize_rows(n, f, rows, Y):
-    _check(lib.gnn_dequantize_rows(n, f, _rows8(rows), _ptr(Y), _stream()), "gnn_dequantize_rows")
+    _check(lib.gnn_dequantize_rows(n, f, _rows8(rows, n, f), _ptr(Y), _stream()), "gnn_dequantize_rows")
 
 
 def gnn_rms_norm_workspace_bytes(n, f):
@@ -500,12 +517,12 @@ def gnn_rms_norm_workspace_bytes(n, f):
 
 
 def gnn_rms_norm_fwd(n, f, X, R, drop, gamma, eps, H, Y, xhat8, rstd_out):
-    _check(lib.gnn_rms_norm_fwd(n, f, _ptr(X), _ptr(R), _drop(drop), _ptr(gamma), float(eps), _ptr(H), _ptr(Y), _rows8(xhat8),
+    _check(lib.gnn_rms_norm_fwd(n, f, _ptr(X), _ptr(R), _drop(drop), _ptr(gamma), float(eps), _ptr(H), _ptr(Y), _rows8(xhat8, n, f),
                                 _ptr(rstd_out), _stream()), "gnn_rms_norm_fwd")
 
 
 def gnn_rms_norm_bwd(n, f, H, xhat8, rstd, gamma, drop, dY, dH, dR, dX, dgamma, workspace):
-    _check(lib.gnn_rms_norm_bwd(n, f, _ptr(H), _rows8(xhat8), _ptr(rstd), _ptr(gamma), _drop(drop), _ptr(dY), _ptr(dH), _ptr(dR),
+    _check(lib.gnn_rms_norm_bwd(n, f, _ptr(H), _rows8(xhat8, n, f), _ptr(rstd), _ptr(gamma), _drop(drop), _ptr(dY), _ptr(dH), _ptr(dR),
                                 _ptr(dX), _ptr(dgamma), _ptr(workspace), _nbytes(workspace), _stream()), "gnn_rms_norm_bwd")
 
 
@@ -519,10 +536,10 @@ def gnn_linear_fwd(act, n, f_in, f_out, X, W, b, R, Y, Z, workspace):
 
 
 def gnn_linear_bwd(act, n, f_in, f_out, X, X8, W, b, Z, Z8, dY, dW, db, dX, workspace):
-    _check(lib.gnn_linear_bwd(int(act), n, f_in, f_out, _ptr(X), _rows8(X8), _ptr(W), _ptr(b), _ptr(Z), _rows8(Z8), _ptr(dY),
-                              _ptr(dW), _ptr(db), _ptr(dX), _ptr(workspace), _nbytes(workspace), _stream()), "gnn_linear_bwd")
+    _check(lib.gnn_linear_bwd(int(act), n, f_in, f_out, _ptr(X), _rows8(X8, n, f_in), _ptr(W), _ptr(b), _ptr(Z),
+                              _rows8(Z8, n, f_out), _ptr(dY), _ptr(dW), _ptr(db), _ptr(dX), _ptr(workspace), _nbytes(workspace), _stream()), "gnn_linear_bwd")
 
 
 def gnn_linear8_fwd(act, n, f_in, f_out, X, W, b, R, Y):
-    _check(lib.gnn_linear8_fwd(int(act), n, f_in, f_out, _rows8(X), _rows8(W), _ptr(b), _ptr(R), _ptr(Y), _stream()),
-           "gnn_linear8_fwd")
+    _check(lib.gnn_linear8_fwd(int(act), n, f_in, f_out, _rows8(X, n, f_in), _rows8(W, f_out, f_in), _ptr(b), _ptr(R), _ptr(Y),
+                               _stream()), "gnn_linear8_fwd")
