@@ -470,13 +470,20 @@ class Rows8:
     of another type or layout are refused, here and by a call that needs more rows or another stride (GNN_ERR_INVALID_ARG)."""
 
     def __init__(self, q, scale, columns=None):
-        given = [(q, torch.int8), (scale, torch.float32)] + ([] if columns is None else [(columns, torch.float32)])
-        if any(t is None or t.dtype != dtype or not t.is_contiguous() for t, dtype in given):
-            raise GnnError(GNN_ERR_INVALID_ARG, "Rows8")
-        self.q, self.scale, self.columns = q, scale, columns
-        self.c = gnn_rows8_t(_ptr(q), _ptr(scale), _ptr(columns))
+        self.c = gnn_rows8_t()
         self._ref = ctypes.byref(self.c)
-        self._serves = None            # the last (n, f) that was looked at
+        self.q, self.scale, self.columns = q, scale, columns
+
+    def __setattr__(self, name, value):
+        """A tensor that takes another's place is what the next call reads."""
+        if name in ("q", "scale", "columns"):
+            dtype = torch.int8 if name == "q" else torch.float32
+            missing = value is None and name != "columns"
+            if missing or (value is not None and (value.dtype != dtype or not value.is_contiguous())):
+                raise GnnError(GNN_ERR_INVALID_ARG, f"Rows8.{name}")
+            setattr(self.c, name, _ptr(value))
+            self._serves = None        # the last (n, f) that was looked at
+        super().__setattr__(name, value)
 
     def _look(self, n, f):
         stride = gnn_rows8_stride(f)
