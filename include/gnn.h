@@ -502,7 +502,7 @@ typedef enum {
  *   ELU with alpha = 1; drop NULL: no dropout; stat_out [n][2] = (mean, rstd), which backward reads.  Y may be X (where no
  *   backward pass follows: that needs X).
  * gnn_layer_norm_bwd - from X, stat and dY [n, f] the gradients dX [n, f], dgamma and dbeta [f]; any of them may be NULL.  The
- *   activation's derivative is taken from gamma xhat + beta, formed again as in forward (ReLU' = 0 at 0), the mask of dropout
+ *   activation's derivative is taken from gamma xhat + beta, formed again as in forward (ReLU' = 0 at 0, NaN at NaN), the mask of dropout
  *   likewise: act, drop, gamma and beta as in forward.  dX may be dY.  The sums over the rows have a fixed order.
  *   workspace: gnn_layer_norm_workspace_bytes(n, f), which does not fall as n grows; not used where dgamma and dbeta are NULL
  *   (then it may be NULL).
@@ -621,7 +621,7 @@ size_t gnn_rms_norm_workspace_bytes(int32_t n, int32_t f);
  * gnn_linear_fwd - Y = act(Z) + R, Z = X W + 1 b^T.  X [n, f_in], W [f_in, f_out], b [f_out] or NULL, R [n, f_out] or NULL, Y [n, f_out].
  *   Z [n, f_out] or NULL: receives X W + b, which backward may read instead of forming it again.  Y may be R.
  * gnn_linear_bwd - with D = dY .* act'(Z):  dW = X^T D [f_in, f_out], db = D^T 1 [f_out] (NULL: not wanted), dX = D W^T [n, f_in] (NULL: not
- *   wanted).  (The gradient of R is dY.)  ReLU' = 0 at 0.
+ *   wanted).  (The gradient of R is dY.)  ReLU' = 0 at 0, NaN at NaN.
  *   X, or X8: the rows in 8 bits, columns included; one of them is NULL.
  *   Z as forward left it, or Z8: the same in 8 bits, columns included, or neither: Z is formed again from X, W and b, and X8 will not do.
  *   GNN_ACT_NONE reads neither of them.

@@ -43,7 +43,7 @@ def dropout(X, factor):
 
 def _activation(z, act):
     if act == "relu":
-        return np.maximum(z, 0.0), (z > 0).astype(np.float64)
+        return np.maximum(z, 0.0), np.where(np.isnan(z), z, z > 0)
     if act == "elu":
         return np.where(z > 0, z, np.expm1(np.minimum(z, 0.0))), np.exp(np.minimum(z, 0.0))
     return z, np.ones_like(z)

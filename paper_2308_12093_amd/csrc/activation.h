@@ -23,7 +23,7 @@ __device__ __forceinline__ float activation(float z) {
 }
 template <int ACT>
 __device__ __forceinline__ float slope(float z) {
-    if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : 0.f;
+    if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;       // NaN stays
     if constexpr (ACT == kActElu) return z > 0.f ? 1.f : exp_down(z);      // NaN stays
     return 1.f;
 }
