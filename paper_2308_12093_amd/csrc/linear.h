@@ -29,6 +29,7 @@ gnn_status_t pair_linear_launch(int act, int64_t M, int64_t N, int64_t K, int64_
 // C [M][N] = A^T B, A [K][M], or NULL: `held` with its columns; B [K][N]; sums [N] = the column sums of B unless it is NULL; a_tops (not of
 // `held`), b_tops: largest magnitudes of their columns, of B with each row times held's scale.
 bool pair_tn_fits(int64_t M, int64_t N, int64_t K, bool held);
+int64_t pair_tn_least_rows(int64_t M, int64_t N);      // no K below this fits
 size_t pair_tn_workspace_bytes(int64_t M, int64_t N, int64_t K);
 gnn_status_t pair_tn_launch(int64_t M, int64_t N, int64_t K, const float *A, const Rows8 &held, const unsigned *a_tops, const float *B,
                             const unsigned *b_tops, float *C, float *sums, void *workspace, hipStream_t st);

@@ -373,8 +373,6 @@ size_t product_bytes(int64_t k, int64_t m) {
 }
 
 int64_t four(int64_t width) { return (width + 3) / 4 * 4; }
-// floats of a row of X in 8 bits brought to floats, of X or of D with zeros behind it
-int64_t space_width(int64_t m, int64_t k) { return four(m) > four(k) ? four(m) : four(k); }
 
 // Rows of `m` floats with zeros behind them up to a multiple of four, and their largest magnitudes unless `tops` is NULL: [part of 256
 // columns][row].  `lanes` lanes a row, four columns each.  30000 x 301, 72 MB: 17 us with the magnitudes, from and to the caches.
@@ -424,8 +422,25 @@ bool padded(int64_t M, int64_t N, int64_t K, const float *space) {
     return K % 4 != 0 && K >= kShortReduction && pair_product_fits(M, N, four(K), space);
 }
 
+// forward's room for rows of X with zeros behind them, in floats
+int64_t forward_space(int64_t n, int64_t m, int64_t k) { return padded(n, k, m, nullptr) ? n * four(m) : 0; }
+
+// Backward's room beside D, in floats, for one of these after the other: X in 8 bits brought to floats, of as many rows as do not go to
+// dW as the integers they are (all up to some number); rows of X, and of D, with zeros behind them.  No less for a larger n.
+int64_t backward_space(int64_t n, int64_t m, int64_t k) {
+    int64_t rows = n;
+    if (!linear_few(true, n, m, k) && pair_tn_fits(m, k, n, true)) {
+        rows = pair_tn_least_rows(m, k) - 1;
+        if (few_rows(n, m, k) > rows) rows = few_rows(n, m, k);
+    }
+    int64_t most = rows * m;
+    if (padded(n, k, m, nullptr) && n * four(m) > most) most = n * four(m);
+    if (padded(n, m, k, nullptr) && n * four(k) > most) most = n * four(k);
+    return most;
+}
+
 // act(X W + b) + R, or D and its largest magnitudes, `parts` a row.  x_rows: room for the largest magnitudes of X's rows, filled where
-// `known`; space: n four(m) floats, used where m is no multiple of four.
+// `known`; space: n four(m) floats where X is padded.
 gnn_status_t product(int act, int64_t n, int64_t m, int64_t k, const float *X, unsigned *x_rows, bool known, const float *W, const float *b,
                      const Linear &g, const Tops &tops, int *parts, float *space, void *workspace, hipStream_t st) {
     const bool pad = padded(n, k, m, space), pair = pad || pair_product_fits(n, k, m, X);
@@ -493,8 +508,8 @@ size_t linear_workspace_bytes(bool backward, int64_t n, int64_t m, int64_t k) {
     if (!backward)
         return linear_few(false, n, m, k) ? kAlign
                                           : align_up((size_t)n * ceil_div(m, 64) * sizeof(unsigned)) +
-                                                align_up(m % 4 ? (size_t)n * four(m) * sizeof(float) : 0) + product_bytes(k, four(m));
-    const size_t d = align_up((size_t)n * k * sizeof(float)) + align_up((size_t)n * space_width(m, k) * sizeof(float));
+                                                align_up((size_t)forward_space(n, m, k) * sizeof(float)) + product_bytes(k, four(m));
+    const size_t d = align_up((size_t)n * k * sizeof(float)) + align_up((size_t)backward_space(n, m, k) * sizeof(float));
     size_t most = 0;
     const int64_t small = few_rows(n, m, k);
     if (small > 0 && !wide_weights(m, k)) {
@@ -517,7 +532,7 @@ gnn_status_t linear_forward_launch(int act, int n, int m, int k, const float *X,
     if (linear_few(false, n, m, k)) return few(act, n, m, k, X, W, b, g, st);
     Carver carve(workspace);
     unsigned *x_rows = carve.take<unsigned>((size_t)n * ceil_div(m, 64));
-    float *space = carve.take<float>(m % 4 ? (size_t)n * four(m) : 0);
+    float *space = carve.take<float>(forward_space(n, m, k));
     int parts;
     return product(act, n, m, k, X, x_rows, false, W, b, g, Tops{nullptr, nullptr}, &parts, space, carve.take<char>(0), st);
 }
@@ -530,7 +545,7 @@ gnn_status_t linear_backward_launch(int act, int n, int m, int k, const float *X
         return db ? fill_zero_launch(k, db, st) : GNN_OK;
     }
     Carver carve(workspace);
-    float *d_space = carve.take<float>((size_t)n * k), *x_space = carve.take<float>((size_t)n * space_width(m, k));
+    float *d_space = carve.take<float>((size_t)n * k), *x_space = carve.take<float>(backward_space(n, m, k));
     const bool plain = act == GNN_ACT_NONE, kept = Z || Z8.q;
     const float *d = plain ? dY : d_space;
     const Linear g{nullptr, nullptr, nullptr, dY, d_space};

@@ -326,14 +326,20 @@ int64_t pair_chunks(int64_t M, int64_t N, int64_t K) {
 
 }  // namespace
 
+// so many rows that the chip's 256 CUs have a tile and a kChunkStep each
+int64_t pair_tn_least_rows(int64_t M, int64_t N) {
+    const int64_t rows = (ceil_div(256, ceil_div(M, 128) * ceil_div(N, tile_n(N))) - 1) * kChunkStep + 1;
+    return rows > kShortReduction ? rows : kShortReduction;
+}
+
 // Reductions that parts are exact enough for, tiles of which not too much is empty, and enough of them times chunks of some length for
 // the chip.  Fewer than four are so many chunks that their sums count: 128 x 256 over 2^17 rows 52 + 22 us, 51 + 12 in tiles of 128 x 128
 // (gemm_half_tn.hip); but with A in 8 bits that would need it in floats first, and their largest magnitudes.
 bool pair_tn_fits(int64_t M, int64_t N, int64_t K, bool held) {
-    if (K < kShortReduction || M > INT32_MAX / 4 || N > INT32_MAX / 4 || M <= 64 || N <= (held ? 64 : 128)) return false;
+    if (M > INT32_MAX / 4 || N > INT32_MAX / 4 || M <= 64 || N <= (held ? 64 : 128)) return false;
     const int64_t tiles = ceil_div(M, 128) * ceil_div(N, tile_n(N)), most = (int64_t)1 << 24;
     if (!held && tiles < 4) return false;
-    return tiles * ceil_div(K, kChunkStep) >= 256 && tiles * pair_chunks(M, N, K) < most - 8 && ceil_div(M * N, 32) + ceil_div(N, 32) < most;
+    return K >= pair_tn_least_rows(M, N) && tiles * pair_chunks(M, N, K) < most - 8 && ceil_div(M * N, 32) + ceil_div(N, 32) < most;
 }
 
 // no less for a larger K
