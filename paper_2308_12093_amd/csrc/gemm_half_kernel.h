@@ -30,7 +30,7 @@ struct HalfProduct {
     float *C;
     int splits, split_steps;           // kPlain: the reduction's parts, C [split][M][N] then
     const float *bias;
-    bool stream;                       // outputs beyond the caches: non-temporal stores
+    bool stream;                       // kPlain, kGateForward: outputs beyond the caches, non-temporal stores
     int tiles_m, tiles_n;
     Gated gated;
     Linear linear;

