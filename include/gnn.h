@@ -627,10 +627,11 @@ size_t gnn_rms_norm_workspace_bytes(int32_t n, int32_t f);
  *   GNN_ACT_NONE reads neither of them.
  *   Sums are fp32 or better everywhere.  Products of many rows over 32 and more indices (f_in of them forward, f_out in dX, n in dW)
  *   take a float as two fp16 numbers: one is off by up to 8 u (u = 2^-24; a float product by u), and by an operand's loss of 2^-40 of the
- *   largest of its row (of X, D) or column (of W; of X and D in dW, in chunks of 4096 rows), or of 2^-151 where that is more, which shows
- *   where operands lie below 2^-16 of it.  Root mean square errors are no larger than those of a chain of float multiplications and
- *   additions.  Few rows and shorter products: those of floats, in chains of 1024 rows at most in dW, or doubles.  From X8 dW is as exact: an integer is one fp16
- *   number, and its row's scale goes to the row of D.
+ *   largest of its row (of X, D) or column (of W; of X and D in dW, in chunks of 4096 rows), or of 2^-151 where that is more.  The loss
+ *   shows where operands lie below 2^-16 of that largest; above it root mean square errors are no larger than those of a chain of float
+ *   multiplications and additions.  (Some of them lose 2^-50, from 2^-27 on: those of few columns, and X W where an X whose f_in is a
+ *   multiple of four is not 16-byte aligned.)  Few rows and shorter products: those of floats, in chains of 1024 rows at most in dW, or
+ *   doubles.  From X8 dW is as exact: an integer is one fp16 number, and its row's scale goes to the row of D.
  *   Outputs must not overlap inputs or each other, but for Y and R.
  *   workspace: gnn_linear_workspace_bytes(backward, n, f_in, f_out), backward 0 or 1; what it returns does not fall as n grows.
  * Errors: INVALID_ARG (NULL X / W / Y / dY / dW, X and X8 both or neither, Z and Z8 both, X8 without Z or Z8 where act is not

@@ -35,9 +35,10 @@ __device__ __forceinline__ float slope(float z, int act) {
 }
 
 // Phi(z) of the normal distribution, and exp(-z^2 / 2).  Below zero Phi(-a) = exp(-a^2 / 2) Q(t) with t = 1 / (1 + 0.345 a), and Q is t
-// times the polynomial of degree 8 whose largest relative error over 0 <= a <= 14 is least (2.0e-8, a third of a unit in the last place;
-// found by reweighted least squares on Chebyshev points).  In float Phi is off by at most 1.5 (4 + z^2) units below zero, of which z^2
-// are what one unit of z is worth, and by 3 above.
+// times a polynomial of degree 8 (found by reweighted least squares on Chebyshev points over 0 <= a <= 14: largest relative error 2.0e-8, and
+// 5.7e-8, 0.95 x 2^-24, with the coefficients rounded to floats).  In units of 2^-24 of it Phi is off by at most 15 + 1.5 z^2 below zero,
+// of which 1.5 z^2 are three roundings of -z^2 / 2, 7 those of t and 7 the other steps', and above zero by 16.  Measured, z Phi(z): 7.3 near
+// zero on either side, 14 at -3.5, 128 at -12.4, 3.4 from 0.5 on and 2.2 from 1 on.
 __device__ __forceinline__ void normal_integral(float z, float &phi, float &bell) {
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.345f, 1.f));
     float q = fmaf(-0.02838203945231031f, t, 0.14528229325785152f);

@@ -2,11 +2,14 @@
 //
 // A row of one operand and a column of the other are taken times a power of two each that brings their largest magnitude to
 // 2^14 .. 2^15 (to 1 at least where it is below 2^-112 and no subnormal), and every element is then h + l: h rounds it to 11 bits and l
-// rounds the rest to 11 bits.  What is left out is at most 2^-23 of the element, 2^-25.5 in the mean.  Three of the four products are formed (l l, at most 2^-22 of the whole, is not), all into
-// one sum: v_mfma_f32_32x32x16_f16 three times for 16 indices.  half_parts.h, which takes l times 2^11 and needs a sum of its own for
-// h l + l h, holds small elements to 2^-50 of the largest of their row (column); here it is 2^-40: l is no finer than 2^-25 beside 2^14, which
-// begins at 2^-16 of the largest, and where that is below 2^-112 what is left out is at most 2^-151, a quarter of the least float.  (The instruction and the conversions take subnormal fp16 numbers as they are.)  For that a step of 32
-// indices spares 32 of its 128 vector instructions, and a wavefront the registers for twice the sums.
+// rounds the rest to 11 bits.  What is left out is at most 2^-23 of the element, 2^-25.5 in the mean.  Three of the four products are
+// formed (l l, at most 2^-22 of the whole, is not), all into one sum: v_mfma_f32_32x32x16_f16 three times for 16 indices.  half_parts.h,
+// which takes l times 2^11 and needs a sum of its own for h l + l h, holds small elements to 2^-50 of the largest of their row (column);
+// here it is 2^-40: l is no finer than 2^-25 beside 2^14, which begins at 2^-16 of the largest.  (Where that is below 2^-112 what is left
+// out is at most 2^-151, a quarter of the least float.  The instruction and the conversions take subnormal fp16 numbers as they are.)
+// X^T D over 4096 rows, eight of D's 2^16 times the others and met by zeros, emulated: 5.1e-7 off in the 2-norm, in two scales 4.8e-7, as a
+// chain of floats 1.1e-6; 2^20 times 1.4e-6, 4.7e-7, 1.1e-6; 2^24 times 2.2e-5.  For that a step of 32 indices spares 32 of its 128
+// vector instructions, and a wavefront the registers for twice the sums.
 // Infinities and NaN are taken as they are and come out as NaN, upon which a wavefront forms its tiles again with the fp32
 // instruction.
 #pragma once

@@ -1,5 +1,6 @@
-// The product with its epilogue, Y = act(X W + b) + R, forward and backward.  Its large products are those of gemm_half_kernel.h and
-// gemm_half_tn.hip; those of few rows are here and in gemm.hip.
+// The product with its epilogue, Y = act(X W + b) + R, forward and backward: which kernels a call takes, and its workspace.  Products of many
+// aligned rows are those of pair_product.hip and pair_tn.hip; of rows at any alignment, narrow outputs and reductions of one step those of
+// gemm_half_kernel.h (linear_half.hip) and gemm_half_tn.hip; of few rows they are here and in gemm.hip.
 #include "linear.h"
 #include "rows.h"
 
@@ -92,7 +93,8 @@ linear_few_kernel(int M, int N, int K, const float *__restrict__ X, const float 
 // D = dY .* act'(Z) from the Z that forward has kept, as it is or in 8 bits, and the largest magnitudes of its rows and of its columns,
 // those with each row times row_scale.  A block takes `rows` rows (top_rows where columns' are wanted) and 256 columns, `lanes` lanes a
 // row, four columns each; the `parts` blocks of the same rows stand side by side.  D NULL: not wanted (it is dY).  Bound by memory: 65536 x
-// 2048 with SiLU 1.6 GB in 304 us, 5.3 TB/s; Z and dY are read once and not into the place of D, which the products read next (335 us).
+// 2048 with SiLU 1.6 GB in 304 us, 5.3 TB/s; Z and dY are read past the caches, to leave the place to D, which the products read next (335 us; where D is dY they read it
+// from memory).
 template <bool ALIGNED, int ACT, bool HELD>
 __global__ void __launch_bounds__(256)
 linear_gradient_kernel(long n, int k, int lanes, int rows, int parts, const float *__restrict__ Z, Rows8 held, const float *__restrict__ dY,
