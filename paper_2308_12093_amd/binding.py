@@ -470,20 +470,22 @@ class Rows8:
     of another type or layout are refused, here and by a call that needs more rows or another stride (GNN_ERR_INVALID_ARG)."""
 
     def __init__(self, q, scale, columns=None):
-        self.c = gnn_rows8_t()
-        self._ref = ctypes.byref(self.c)
         self.q, self.scale, self.columns = q, scale, columns
 
     def __setattr__(self, name, value):
-        """A tensor that takes another's place is what the next call reads."""
+        """A tensor that takes another's place is what the next call reads: of this object alone, not of one that it was copied to."""
         if name in ("q", "scale", "columns"):
             dtype = torch.int8 if name == "q" else torch.float32
             missing = value is None and name != "columns"
             if missing or (value is not None and (value.dtype != dtype or not value.is_contiguous())):
                 raise GnnError(GNN_ERR_INVALID_ARG, f"Rows8.{name}")
-            setattr(self.c, name, _ptr(value))
+            super().__setattr__(name, value)
+            given = self.__dict__
+            self.c = gnn_rows8_t(*(_ptr(given.get(field)) for field in ("q", "scale", "columns")))
+            self._ref = ctypes.byref(self.c)
             self._serves = None        # the last (n, f) that was looked at
-        super().__setattr__(name, value)
+        else:
+            super().__setattr__(name, value)
 
     def _look(self, n, f):
         stride = gnn_rows8_stride(f)

@@ -1,5 +1,7 @@
 """``binding.Rows8``: what it refuses before a kernel could read or write outside of its tensors, and tensors put in others' place.  No
 launch but where marked, so no GPU is needed."""
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -101,6 +103,13 @@ def test_a_tensor_that_does_not_fit_is_refused_later_as_well(no_stream):
         room._look(N, F)
         setattr(room, name, value)
         assert refused(B.gnn_dequantize_rows, N, F, room, x), name
+
+
+def test_a_copy_has_columns_of_its_own():
+    room = rows()
+    other = copy.copy(room)
+    other.columns = torch.ones(F)
+    assert not room.c.columns and other.c.columns == other.columns.data_ptr() and other.c.q == room.c.q
 
 
 @pytest.mark.gpu
